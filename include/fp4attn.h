@@ -275,6 +275,135 @@ fp4attn_status fp4attn_forward_bf16(const void* q, const void* k, const void* v,
                                     float softmax_scale, void* out, int out_dtype, void* stream);
 
 /*
+ * Rotary positions.  Turns the first rotary_dim channels of every head of x, seen as
+ * [B, H, N, d], by its position: pair j, channels (a, b) = (j, j + rotary_dim / 2), or
+ * (2 j, 2 j + 1) with interleaved = 1, by the angle t = position * inv_freq[j]:
+ *
+ *   y_a = magnitude (x_a cos t - x_b sin t),  y_b = magnitude (x_a sin t + x_b cos t);
+ *
+ * channels from rotary_dim on are copied.  inverse = 1 turns by -t, which gives the
+ * gradient of x from that of y.  Angles are formed in fp64, so far positions keep theirs;
+ * the rotation is fp32, rounded once to `dtype` (FP4ATTN_F32 or FP4ATTN_BF16).
+ *
+ *   x_strides, out_strides  HOST arrays of three strides, of B, H and N, in elements; d
+ *              is contiguous.  [n, H, d] tokens are B = 1, N = n with strides {0, d, H d}.
+ *   positions  [B, N] int64, sequence b at positions + b * position_stride (0: shared)
+ *   inv_freq   [rotary_dim / 2] fp64, radians per position
+ *
+ * out may be x itself with the same strides (in place); otherwise it must not overlap x, nor
+ * itself.  Index arrays (positions, and below slots, page_table, lengths, q_starts,
+ * tree) and inv_freq need their natural alignment only.  A size of zero is no work.
+ *
+ * Errors: INVALID_ARG for null or misaligned pointers, negative sizes or strides,
+ * strides that are no multiple of 16 bytes, rotary_dim < 16, above d or not a
+ * multiple of 16, d not a multiple of 16, magnitude not finite, a bad dtype or flag;
+ * UNSUPPORTED for d above 512, N above 2^24, B above 65535 or H above 65535.
+ */
+fp4attn_status fp4attn_rotary(const void* x, void* out, int dtype, int64_t B, int64_t H, int64_t N, int64_t d,
+                              const int64_t* x_strides, const int64_t* out_strides, const int64_t* positions,
+                              int64_t position_stride, const double* inv_freq, int64_t rotary_dim, float magnitude,
+                              int interleaved, int inverse, void* stream);
+
+/*
+ * A paged cache of quantized keys and values: `pages` pages of page_size (a power of two
+ * >= 16) tokens for `heads` key heads of head_dim (64 or 128) channels.  Slot s is place
+ * s % page_size of page s / page_size.  A block of 32 values is one token's along d, under
+ * the rules of fp4attn_quantize_mxfp4, or with fp8 = 1 of fp4attn_quantize_mxfp8, so a
+ * token is written by itself.  With b = head_dim / 2 code bytes a token and head (fp8: head_dim):
+ *
+ *   k_codes  [pages, heads, page_size, b]            k_scales [pages, heads, page_size, head_dim/32]
+ *   v_codes  [pages, heads, page_size/8, 16, 8, b/16]: of eight tokens, first sixteenth
+ *            i of d (D/16 values), then the token: the attention's operand order
+ *   v_scales [pages, heads, page_size/8, head_dim/32, 8]
+ *
+ * struct_size must equal sizeof(fp4attn_cache).  Attention reads V blocks of amplitude 2^126
+ * or more (fp8: 2^120), and K values that pass the bf16 range at 6 times their size (fp8: at their
+ * size), as non-finite.
+ */
+typedef struct fp4attn_cache {
+  uint32_t struct_size;
+  int32_t fp8;
+  int64_t pages;
+  int64_t heads;
+  int64_t page_size;
+  int64_t head_dim;
+  uint8_t* k_codes;
+  uint8_t* k_scales;
+  uint8_t* v_codes;
+  uint8_t* v_scales;
+} fp4attn_cache;
+
+/*
+ * Quantizes n tokens into the cache: token i of k and v ([heads, head_dim] contiguous,
+ * tokens k_stride and v_stride elements apart) into slot slots[i].  A slot outside
+ * [0, pages * page_size) marks a padding token, which is skipped.  Other slots keep
+ * their bytes.  A slot that occurs twice in one call ends with bytes of either token, no
+ * other slot is touched by that.
+ *
+ * Errors: those of the cache (below), INVALID_ARG for null or misaligned pointers,
+ * n < 0, strides negative or no multiple of 16 bytes, a bad src_dtype; UNSUPPORTED for more
+ * than 2^30 blocks of 32.  Errors of the cache: INVALID_ARG for NULL, a wrong struct_size,
+ * fp8 not 0 or 1, sizes < 1, a page_size that is no power of two or below 16, null or
+ * misaligned pointers; UNSUPPORTED for head_dim not 64 or 128, heads above 65535, page_size
+ * above 2^20, or more than 2^40 slots.
+ */
+fp4attn_status fp4attn_cache_write(const fp4attn_cache* cache, const void* k, const void* v, int src_dtype, int64_t n,
+                                   int64_t k_stride, int64_t v_stride, const int64_t* slots, void* stream);
+
+/*
+ * Reads n slots back: k and v [n, heads, head_dim] of out_dtype, the values the codes
+ * stand for, rounded once (a block of E8M0 byte 255: NaN; a slot outside the cache: zeros).
+ * Errors: as fp4attn_cache_write.
+ */
+fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slots, int64_t n, void* k, void* v,
+                                  int out_dtype, void* stream);
+
+/*
+ * Attention of new tokens over the cache, the textbook softmax of eq. exact-attention on
+ * the values that the cache stands for.  The tokens' own keys and values are in the cache
+ * already (fp4attn_cache_write first).
+ *
+ *   q           [n, q_heads, head_dim] bf16, tokens q_stride elements apart; query head h
+ *               reads key head h / (q_heads / heads)
+ *   page_table  [B, max_pages] int32: key j of sequence b is in page
+ *               page_table[b][j / page_size], place j % page_size.  Only entries of pages
+ *               that hold keys are read; keys in a page outside the cache do not exist.
+ *   lengths     [B] int32: keys of each sequence, its new tokens included (below 0: 0;
+ *               keys past max_pages * page_size do not exist)
+ *   q_starts    [B + 1] int32, ascending: sequence b's tokens are rows q_starts[b] ..
+ *               q_starts[b + 1] - 1 of q, at most max_q of them (rows past that, and
+ *               rows of no sequence, stay as they were in out and lse).
+ *               NULL: n / B tokens each, and max_q must be n / B.
+ *   tree        [n, tree_words] int64 or NULL.  NULL: causal, token t of T sees the keys
+ *               at positions <= lengths[b] - T + t.  Else token t sees the keys before the new
+ *               tokens, and of these token u where bit u % 64 of word u / 64 of its row is
+ *               set (its ancestors and itself, in a tree of drafted tokens).
+ *   out         [n, q_heads, head_dim] of out_dtype
+ *   lse         [n, q_heads] fp32 natural-log normaliser, or NULL
+ *   workspace   at least fp4attn_cache_attention_workspace(...) bytes, 16-byte aligned (may be
+ *               NULL for 0 bytes); calls that may run at the same time need one each
+ *
+ * A row that sees no key gets zeros and -inf.  Keys that a row does not see never reach
+ * it, whatever they hold.  P is rounded to bf16 for the PV product.  n = 0: no work.
+ *
+ * Errors: those of the cache, INVALID_ARG for null or misaligned pointers, sizes < 1,
+ * q_heads no multiple of heads, a q_stride that is negative or no multiple of 8,
+ * n not B * max_q without q_starts, tree_words * 64 < max_q with a tree, softmax_scale not
+ * finite or <= 0, a bad out_dtype, a workspace that is too small; UNSUPPORTED for n * q_heads
+ * or max_q * q_heads of 2^31 or more, max_pages * page_size above 2^30, B above 65535, or more than 2^24 workgroups.
+ */
+fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
+                                       int64_t q_stride, int64_t B, const int32_t* page_table, int64_t max_pages,
+                                       const int32_t* lengths, const int32_t* q_starts, int64_t max_q,
+                                       const int64_t* tree, int64_t tree_words, float softmax_scale, void* out,
+                                       int out_dtype, float* lse, void* workspace, int64_t workspace_bytes,
+                                       void* stream);
+
+/* Bytes of workspace that such a call needs (0 for many); -1 for sizes that the call refuses. */
+int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_heads, int64_t B, int64_t max_pages,
+                                          int64_t max_q);
+
+/*
  * Test hook: runs exactly the forward kernel of fp4attn_forward_mxfp4_ex (same
  * launch configuration and arguments, `opts` NULL = the defaults, writes `out`
  * too) and additionally
@@ -342,7 +471,8 @@ const char* fp4attn_last_error(void);
 
 /* ABI version of this header, (major << 16) | minor: 2.1 (2.1 adds
  * fp4attn_quantize_qkv; 2.0: fp4attn_forward_bf16 takes V as [B, H, N, d], where
- * 1.x took V transposed). */
+ * 1.x took V transposed).  fp4attn_rotary and the fp4attn_cache entry points came without
+ * a new number: ask for them by symbol. */
 int fp4attn_abi_version(void);
 
 #ifdef __cplusplus

@@ -15,13 +15,20 @@ from ._lib import (  # noqa: F401
     lib,
 )
 from .api import (  # noqa: F401
+    KVCache,
     attention_mxfp4,
+    cache_attention,
+    cache_read,
+    cache_write,
     debug_directp_mxfp4,
     debug_mfma_stream,
     forward_bf16,
     forward_mxfp4,
     forward_options,
+    kv_cache,
     quantize_mxfp4,
     quantize_mxfp8,
     quantize_qkv,
+    rotary,
+    rotary_frequencies,
 )

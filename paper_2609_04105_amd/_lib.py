@@ -22,6 +22,13 @@ class ForwardOptions(ctypes.Structure):
                 ("lse", ctypes.c_void_p)]
 
 
+class Cache(ctypes.Structure):
+    """fp4attn_cache (include/fp4attn.h)."""
+    _fields_ = [("struct_size", ctypes.c_uint32), ("fp8", ctypes.c_int32), ("pages", _i64), ("heads", _i64),
+                ("page_size", _i64), ("head_dim", _i64), ("k_codes", _c_p), ("k_scales", _c_p), ("v_codes", _c_p),
+                ("v_scales", _c_p)]
+
+
 # name -> argtypes; entry points not in RESTYPES return a status int
 SIGNATURES = {
     "fp4attn_quantize_mxfp4": [_c_p, _int, _i64, _i64, _i64, _int, _c_p, _c_p, _c_p],
@@ -34,13 +41,20 @@ SIGNATURES = {
     "fp4attn_forward_mxfp4_ex": [_c_p] * 6 + [_i64] * 4 + [_f32, ctypes.POINTER(ForwardOptions), _c_p, _int, _c_p],
     "fp4attn_debug_directp_mxfp4": [_c_p] * 6 + [_i64] * 4 + [_f32, ctypes.POINTER(ForwardOptions)]
     + [_c_p, _int, _c_p, _i64] + [_c_p] * 5 + [_c_p],
+    "fp4attn_rotary": [_c_p, _c_p, _int] + [_i64] * 4 + [_c_p] * 3 + [_i64, _c_p, _i64, _f32, _int, _int, _c_p],
+    "fp4attn_cache_write": [ctypes.POINTER(Cache), _c_p, _c_p, _int, _i64, _i64, _i64, _c_p, _c_p],
+    "fp4attn_cache_read": [ctypes.POINTER(Cache), _c_p, _i64, _c_p, _c_p, _int, _c_p],
+    "fp4attn_cache_attention": [ctypes.POINTER(Cache), _c_p, _i64, _i64, _i64, _i64, _c_p, _i64, _c_p, _c_p, _i64, _c_p,
+                                _i64, _f32, _c_p, _int, _c_p, _c_p, _i64, _c_p],
+    "fp4attn_cache_attention_workspace": [ctypes.POINTER(Cache)] + [_i64] * 4,
     "fp4attn_debug_mfma_stream": [_c_p, _c_p, _int, _int, _c_p, _c_p],
     "fp4attn_status_string": [_int],
     "fp4attn_last_error": [],
     "fp4attn_abi_version": [],
 }
 RESTYPES = {"fp4attn_status_string": ctypes.c_char_p, "fp4attn_last_error": ctypes.c_char_p,
-            "fp4attn_abi_version": ctypes.c_int, "fp4attn_forward_options_init": None}
+            "fp4attn_abi_version": ctypes.c_int, "fp4attn_forward_options_init": None,
+            "fp4attn_cache_attention_workspace": ctypes.c_int64}
 
 
 class Fp4AttnError(RuntimeError):

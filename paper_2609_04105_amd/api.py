@@ -13,10 +13,11 @@ goes through the checks here, with the same results and about 7 us more host tim
 import ctypes
 import math
 import warnings
+from typing import NamedTuple
 
 import torch
 
-from ._lib import FP4ATTN_BF16, FP4ATTN_F32, ForwardOptions, check, lib
+from ._lib import FP4ATTN_BF16, FP4ATTN_F32, Cache, ForwardOptions, check, lib
 
 
 class _NoBinding:
@@ -333,4 +334,267 @@ def forward_bf16(q, k, v, softmax_scale=None, out=None, out_dtype=torch.float32)
     s = 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale
     _launch(dev, lib.fp4attn_forward_bf16, _ptr(q), _ptr(k), _ptr(v), B, H, N, d, s, _ptr(out), _DTYPES[out.dtype],
             _stream(out))
+    return out
+
+
+def _tokens(t, name, dtype, heads=None, d=None):
+    """Checks a [tokens, heads, d] tensor whose tokens may lie apart (a slice of a fused
+    projection); returns the stride of a token."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.ndim != 3 or (heads is not None and tuple(t.shape[1:]) != (heads, d)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [tokens, {heads or 'heads'}, {d or 'd'}]")
+    if t.numel() and not t[0].is_contiguous():
+        raise ValueError(f"the heads of a token of {name} must be contiguous, got strides {t.stride()}")
+    return t.stride(0)
+
+
+def _overlaps_itself(t):
+    """Whether two elements of ``t`` may share memory."""
+    reach = 1
+    for stride, size in sorted((st, n) for n, st in zip(t.shape, t.stride()) if n > 1):
+        if stride < reach:
+            return True
+        reach = stride * size
+    return False
+
+
+def rotary_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, original_length=None, fast_turns=32.0,
+                       slow_turns=1.0, device="cuda"):
+    """Radians per position of each pair of :func:`rotary`, ``base ** (-2 j / rotary_dim)`` in
+    fp64, and the magnitude that goes with them.  ``scaling`` stretches a model's context by
+    ``factor``:
+
+    * ``"linear"``: every angle divided by ``factor`` (position interpolation);
+    * ``"ntk"``: a larger base, ``base * factor ** (r / (r - 2))``, which keeps the fastest
+      pair and divides the slowest by ``factor``;
+    * ``"yarn"``: pairs that turn more than ``fast_turns`` times in ``original_length``
+      positions keep their angle, those under ``slow_turns`` are divided by ``factor``, those
+      between are mixed linearly; magnitude ``0.1 ln(factor) + 1``.
+    """
+    r = rotary_dim
+    if not isinstance(r, int) or r < 2 or r % 2:
+        raise ValueError(f"rotary_dim={r} must be a positive even number")
+    if not (base > 1.0 and math.isfinite(base) and factor >= 1.0 and math.isfinite(factor)):
+        raise ValueError(f"base={base} must be above 1 and factor={factor} at least 1")
+    j = torch.arange(r // 2, dtype=torch.float64)
+    magnitude = 1.0
+    if scaling == "ntk":
+        if r == 2:
+            raise ValueError("the ntk scaling needs more than one pair")
+        base = base * factor ** (r / (r - 2))
+    freq = base ** (-2.0 * j / r)
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "yarn":
+        if original_length is None or original_length < 1 or not fast_turns > slow_turns > 0:
+            raise ValueError("the yarn scaling needs original_length and fast_turns > slow_turns > 0")
+        # the pair that makes `turns` turns in original_length positions
+        low, high = (r * math.log(original_length / (2 * math.pi * turns)) / (2 * math.log(base))
+                     for turns in (fast_turns, slow_turns))
+        low, high = max(math.floor(low), 0), min(math.ceil(high), r - 1)
+        mix = ((j - low) / max(high - low, 1e-3)).clamp(0.0, 1.0)
+        freq = freq * (1.0 - mix) + freq / factor * mix
+        magnitude = 0.1 * math.log(factor) + 1.0
+    elif scaling not in (None, "ntk"):
+        raise ValueError(f"scaling {scaling!r} is not None, 'linear', 'ntk' or 'yarn'")
+    return freq.to(device), magnitude
+
+
+def rotary(x, positions, inv_freq, interleaved=False, magnitude=1.0, inverse=False, out=None):
+    """Rotary positions on ``x`` (bf16 or fp32): [n, H, d] with ``positions`` [n], or [B, H, N, d]
+    with ``positions`` [N] or [B, N] (int64).  The first ``2 * len(inv_freq)`` channels of
+    every head turn by ``position * inv_freq[j]`` (fp64, :func:`rotary_frequencies`); pairs are
+    (j, j + r / 2), or (2 j, 2 j + 1) with ``interleaved``.  ``inverse`` turns back: applied
+    to the gradient of the result it gives the gradient of ``x``.  ``x`` may have any strides
+    with d contiguous; ``out`` may be ``x`` (in place)."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("x must be a GPU tensor")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"x has dtype {x.dtype}, expected {tuple(_DTYPES)}")
+    if x.ndim not in (3, 4):
+        raise ValueError(f"x must be [n, H, d] or [B, H, N, d], got shape {tuple(x.shape)}")
+    _need(positions, "positions", torch.int64)
+    _need(inv_freq, "inv_freq", torch.float64, 1)
+    if x.ndim == 3:
+        (N, H, d), B = x.shape, 1
+    else:
+        B, H, N, d = x.shape
+    if tuple(positions.shape) not in (((N,),) if x.ndim == 3 else ((N,), (B, N))):
+        raise ValueError(f"positions have shape {tuple(positions.shape)} for x {tuple(x.shape)}")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        if not isinstance(out, torch.Tensor) or not out.is_cuda:
+            raise ValueError("out must be a GPU tensor")
+        if out.dtype != x.dtype or out.shape != x.shape:
+            raise ValueError(f"out is {out.dtype} {tuple(out.shape)}, expected {x.dtype} {tuple(x.shape)}")
+        if _overlaps_itself(out):
+            raise ValueError("elements of out share memory")
+        if out.numel() and out.data_ptr() == x.data_ptr() and out.stride() != x.stride():
+            raise ValueError("out begins where x does, with other strides")
+    dev = _same_device(x, positions, inv_freq, out)
+    if x.numel() == 0:
+        return out
+    for t, name in ((x, "x"), (out, "out")):
+        if t.stride(-1) != 1 and d != 1:
+            raise ValueError(f"the channels of {name} must be contiguous")
+
+    def strides(t):
+        st = (0, t.stride(1), t.stride(0)) if t.ndim == 3 else t.stride()[:3]
+        sizes = (1, H, N) if t.ndim == 3 else t.shape[:3]
+        return (ctypes.c_int64 * 3)(*(s if n > 1 else 0 for s, n in zip(st, sizes)))   # of one element: any
+
+    _launch(dev, lib.fp4attn_rotary, _ptr(x), _ptr(out), _DTYPES[x.dtype], B, H, N, d, strides(x), strides(out),
+            _ptr(positions), N if positions.ndim == 2 else 0, _ptr(inv_freq), 2 * inv_freq.numel(), magnitude,
+            int(bool(interleaved)), int(bool(inverse)), _stream(x))
+    return out
+
+
+class KVCache(NamedTuple):
+    """A paged cache of quantized keys and values (fp4attn_cache in include/fp4attn.h): uint8
+    tensors k_codes [pages, heads, page_size, b], k_scales [pages, heads, page_size, d / 32],
+    v_codes [pages, heads, page_size / 8, 16, 8, b / 16] and v_scales [pages, heads,
+    page_size / 8, d / 32, 8]; b = d / 2 for MXFP4, d for MXFP8."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def kv_cache(pages, heads, page_size, d, fp8=False, device="cuda"):
+    """An empty :class:`KVCache` (all bytes zero): MXFP4, or MXFP8 with ``fp8``."""
+    if d not in (64, 128) or pages < 1 or heads < 1 or page_size < 16 or page_size & (page_size - 1):
+        raise ValueError(f"no cache of {pages} pages of {page_size} tokens, {heads} heads of {d}: sizes from 1, page_size "
+                         "a power of two from 16, d 64 or 128")
+    b = d if fp8 else d // 2
+    return KVCache(*(torch.zeros((pages, heads) + s, dtype=torch.uint8, device=device)
+                     for s in ((page_size, b), (page_size, d // 32), (page_size // 8, 16, 8, b // 16),
+                               (page_size // 8, d // 32, 8))))
+
+
+def _cache(cache):
+    """The C description of a cache's tensors."""
+    if len(cache) != 4:
+        raise ValueError("a cache is (k_codes, k_scales, v_codes, v_scales)")
+    for t, name, ndim in zip(cache, KVCache._fields, (4, 4, 6, 5)):
+        _need(t, name, torch.uint8, ndim)
+    k_codes, k_scales, v_codes, v_scales = cache
+    pages, H, page, b = k_codes.shape
+    d = 32 * k_scales.shape[3]
+    shapes = ((pages, H, page, b), (pages, H, page, d // 32), (pages, H, page // 8, 16, 8, b // 16),
+              (pages, H, page // 8, d // 32, 8))
+    for t, name, shape in zip(cache, KVCache._fields, shapes):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if b not in (d, d // 2):
+        raise ValueError(f"k_codes has {b} bytes a token for d = {d}")
+    _same_device(*cache)
+    return Cache(ctypes.sizeof(Cache), int(b == d), pages, H, page, d, *(t.data_ptr() for t in cache))
+
+
+def cache_write(k, v, cache, slots):
+    """Quantize ``k`` and ``v`` ([n, heads, d], bf16 or fp32; tokens may lie apart, as slices of
+    a fused projection do) into ``slots`` (int64 [n], page * page_size + place) of ``cache``.
+    Slots outside the cache (-1) mark padding and are skipped."""
+    c = _cache(cache)
+    types = tuple(_DTYPES)
+    ks, vs = _tokens(k, "k", types, c.heads, c.head_dim), _tokens(v, "v", types, c.heads, c.head_dim)
+    if k.dtype != v.dtype:
+        raise TypeError(f"k is {k.dtype} and v {v.dtype}")
+    _need(slots, "slots", torch.int64, 1)
+    n = slots.numel()
+    if k.shape[0] != n or v.shape[0] != n:
+        raise ValueError(f"{k.shape[0]} keys and {v.shape[0]} values for {n} slots")
+    dev = _same_device(k, v, slots, cache[0])
+    if n:
+        _launch(dev, lib.fp4attn_cache_write, ctypes.byref(c), _ptr(k), _ptr(v), _DTYPES[k.dtype], n, ks if n > 1 else 0,
+                vs if n > 1 else 0, _ptr(slots), _stream(k))
+
+
+def cache_read(cache, slots, out_dtype=torch.float32):
+    """(k, v), each [n, heads, d]: the values that ``slots`` (int64 [n]) of ``cache`` stand for;
+    zeros for slots outside it."""
+    c = _cache(cache)
+    _need(slots, "slots", torch.int64, 1)
+    if out_dtype not in _DTYPES:
+        raise TypeError(f"out_dtype {out_dtype} is not one of {tuple(_DTYPES)}")
+    dev = _same_device(slots, cache[0])
+    n = slots.numel()
+    k, v = (torch.empty((n, c.heads, c.head_dim), dtype=out_dtype, device=dev) for _ in range(2))
+    if n:
+        _launch(dev, lib.fp4attn_cache_read, ctypes.byref(c), _ptr(slots), n, _ptr(k), _ptr(v), _DTYPES[out_dtype],
+                _stream(slots))
+    return k, v
+
+
+def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tree=None, softmax_scale=None, out=None,
+                    lse=None, out_dtype=torch.float32):
+    """Attention of new tokens over ``cache``; returns O [n, Hq, d] (``out_dtype``, or ``out``).
+
+    ``q`` [n, Hq, d] bf16 (tokens may lie apart), Hq a multiple of the cache's heads;
+    ``page_table`` [B, max_pages] and ``lengths`` [B] int32, the lengths with the new tokens,
+    whose keys and values are in the cache already.  Without ``q_starts`` every sequence
+    has n / B tokens; with it (int32 [B + 1]) sequence b has rows ``q_starts[b]`` to
+    ``q_starts[b + 1]``, at most ``max_q`` of them, and other rows of ``out`` and ``lse`` are left as they were.
+
+    Token t of T sees the keys up to its own, or with ``tree`` (int64 [n], or [n, words] for more
+    than 64 tokens) the keys before the new tokens and the new tokens u whose bit is set.
+    ``lse`` (fp32 [n, Hq]) receives the log normaliser.  A row that sees no key is 0 (-inf)."""
+    c = _cache(cache)
+    H, d = c.heads, c.head_dim
+    stride = _tokens(q, "q", (torch.bfloat16,))
+    n, Hq = q.shape[:2]
+    if q.shape[2] != d or Hq == 0 or Hq % H:
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected [tokens, a multiple of {H}, {d}]")
+    _need(page_table, "page_table", torch.int32, 2)
+    _need(lengths, "lengths", torch.int32, 1)
+    B = lengths.numel()
+    if B == 0 or page_table.shape[0] != B or page_table.shape[1] == 0:
+        raise ValueError(f"page_table has shape {tuple(page_table.shape)} for {B} sequences")
+    used = [q, page_table, lengths, cache[0]]
+    if q_starts is not None:
+        _need(q_starts, "q_starts", torch.int32, 1)
+        if q_starts.numel() != B + 1:
+            raise ValueError(f"q_starts has {q_starts.numel()} entries for {B} sequences")
+        if max_q is None:
+            raise ValueError("q_starts needs max_q, the tokens of the longest sequence")
+        used.append(q_starts)
+    else:
+        if n % B or max_q not in (None, n // B):
+            raise ValueError(f"{n} tokens are not {B} sequences of {max_q or 'one length'}: pass q_starts and max_q")
+        max_q = n // B
+    words = 0
+    if tree is not None:
+        _need(tree, "tree", torch.int64)
+        if tree.ndim not in (1, 2) or tree.shape[0] != n:
+            raise ValueError(f"tree has shape {tuple(tree.shape)}, expected [{n}] or [{n}, words]")
+        words = tree.shape[1] if tree.ndim == 2 else 1
+        used.append(tree)
+    if out is None:
+        if out_dtype not in _DTYPES:
+            raise TypeError(f"out_dtype {out_dtype} is not one of {tuple(_DTYPES)}")
+        out = torch.empty((n, Hq, d), dtype=out_dtype, device=q.device)
+    else:
+        _need(out, "out", tuple(_DTYPES), 3)
+        if tuple(out.shape) != (n, Hq, d):
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(n, Hq, d)}")
+    if lse is not None:
+        _need(lse, "lse", torch.float32, 2)
+        if tuple(lse.shape) != (n, Hq):
+            raise ValueError(f"lse has shape {tuple(lse.shape)}, expected {(n, Hq)}")
+        used.append(lse)
+    dev = _same_device(*used, out)
+    if n == 0:
+        return out
+    ref = ctypes.byref(c)
+    size = lib.fp4attn_cache_attention_workspace(ref, Hq, B, page_table.shape[1], max_q)
+    work = torch.empty(size, dtype=torch.uint8, device=dev) if size > 0 else None   # -1: the call says why
+    _launch(dev, lib.fp4attn_cache_attention, ref, _ptr(q), n, Hq, stride if n > 1 else 0, B, _ptr(page_table),
+            page_table.shape[1], _ptr(lengths), None if q_starts is None else _ptr(q_starts), max_q,
+            None if tree is None else _ptr(tree), words, 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale,
+            _ptr(out), _DTYPES[out.dtype], None if lse is None else _ptr(lse), None if work is None else _ptr(work),
+            max(size, 0), _stream(q))
     return out

@@ -7,6 +7,7 @@
 
 #include "../../include/fp4attn.h"
 #include "launch.hpp"
+#include "serving.hpp"
 
 namespace {
 
@@ -199,6 +200,81 @@ fp4attn_status quantize_common(const void* src, int src_dtype, int64_t batch, in
                   "quantize launch");
 }
 
+bool aligned_to(const void* p, uintptr_t n) { return p != nullptr && reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+#define REQUIRE_INDEX(p)                                                                              \
+  do {                                                                                                \
+    if (!aligned_to(p, sizeof(*(p)))) return fail(FP4ATTN_ERR_INVALID_ARG, "%s is null or misaligned", #p); \
+  } while (0)
+
+// A stride of tokens or heads: not negative, whole 16-byte units.
+fp4attn_status check_stride(int64_t stride, int dtype, const char* name) {
+  if (stride < 0 || stride % (dtype == FP4ATTN_BF16 ? 8 : 4) != 0)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "%s=%lld must be >= 0 and a multiple of 16 bytes", name, (long long)stride);
+  return FP4ATTN_OK;
+}
+
+fp4attn_status check_cache_sizes(const fp4attn_cache* c, fp4attn::CacheView* view) {
+  if (c == nullptr) return fail(FP4ATTN_ERR_INVALID_ARG, "cache is null");
+  if (c->struct_size != sizeof(fp4attn_cache))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "cache struct_size %u, expected %zu", c->struct_size, sizeof(fp4attn_cache));
+  if (c->fp8 != 0 && c->fp8 != 1) return fail(FP4ATTN_ERR_INVALID_ARG, "cache fp8 must be 0 or 1");
+  if (c->pages < 1 || c->heads < 1) return fail(FP4ATTN_ERR_INVALID_ARG, "cache pages and heads must be >= 1");
+  if (c->page_size < 16 || (c->page_size & (c->page_size - 1)) != 0)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "page_size=%lld must be a power of two >= 16", (long long)c->page_size);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "head dimension %lld is not 64 or 128", (long long)c->head_dim);
+  if (c->heads > 65535 || c->page_size > (1 << 20) || c->pages > (int64_t(1) << 40) / c->page_size)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "cache of %lld pages of %lld tokens, %lld heads is too large",
+                (long long)c->pages, (long long)c->page_size, (long long)c->heads);
+  view->k_codes = c->k_codes;
+  view->k_scales = c->k_scales;
+  view->v_codes = c->v_codes;
+  view->v_scales = c->v_scales;
+  view->pages = c->pages;
+  view->H = (int)c->heads;
+  view->d = (int)c->head_dim;
+  view->fp8 = c->fp8;
+  view->page_shift = __builtin_ctzll((unsigned long long)c->page_size);
+  return FP4ATTN_OK;
+}
+
+fp4attn_status check_cache(const fp4attn_cache* c, fp4attn::CacheView* view) {
+  const fp4attn_status st = check_cache_sizes(c, view);
+  if (st != FP4ATTN_OK) return st;
+  REQUIRE_PTR(c->k_codes);
+  REQUIRE_PTR(c->k_scales);
+  REQUIRE_PTR(c->v_codes);
+  REQUIRE_PTR(c->v_scales);
+  return FP4ATTN_OK;
+}
+
+fp4attn_status check_tokens(const fp4attn::CacheView& c, int64_t n) {
+  if (n < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "n=%lld must not be negative", (long long)n);
+  if (n > (int64_t(1) << 30) / (c.H * (c.d / 32)) - 8)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "n=%lld tokens of %d heads are too many for one launch", (long long)n, c.H);
+  return FP4ATTN_OK;
+}
+
+// The plan of an attention call whose cache is checked.
+fp4attn_status check_cache_attention(const fp4attn::CacheView& c, int64_t q_heads, int64_t B, int64_t max_pages,
+                                     int64_t max_q, fp4attn::CachePlan* plan) {
+  if (q_heads < 1 || B < 1 || max_pages < 1 || max_q < 1)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "q_heads, B, max_pages and max_q must be >= 1");
+  if (q_heads % c.H != 0)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "q_heads=%lld is no multiple of the cache's %d heads", (long long)q_heads, c.H);
+  if (B > 65535) return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld is above 65535", (long long)B);
+  if (max_pages > fp4attn::kMaxCacheKeys >> c.page_shift)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "max_pages=%lld: more than 2^30 keys a sequence", (long long)max_pages);
+  if (q_heads > 0x7fffffff || max_q > 0x7fffffff / q_heads)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "max_q=%lld tokens of %lld heads are too many", (long long)max_q,
+                (long long)q_heads);
+  *plan = fp4attn::cache_plan(B, c.H, q_heads / c.H, c.d, max_q, max_pages << c.page_shift);
+  if (plan->workgroups >= (1 << 24))
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "%lld workgroups are too many for one launch", (long long)plan->workgroups);
+  return FP4ATTN_OK;
+}
+
 }  // namespace
 
 namespace fp4attn {
@@ -354,6 +430,178 @@ fp4attn_status fp4attn_forward_bf16(const void* q, const void* k, const void* v,
   a.out_bf16 = out_dtype == FP4ATTN_BF16;
   a.softmax_scale = softmax_scale;
   return from_hip(fp4attn::launch_forward_bf16(a, static_cast<hipStream_t>(stream)), "bf16 forward launch");
+}
+
+fp4attn_status fp4attn_rotary(const void* x, void* out, int dtype, int64_t B, int64_t H, int64_t N, int64_t d,
+                              const int64_t* x_strides, const int64_t* out_strides, const int64_t* positions,
+                              int64_t position_stride, const double* inv_freq, int64_t rotary_dim, float magnitude,
+                              int interleaved, int inverse, void* stream) {
+  if (dtype != FP4ATTN_F32 && dtype != FP4ATTN_BF16)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "dtype %d is not FP4ATTN_F32 or FP4ATTN_BF16", dtype);
+  if (B < 0 || H < 0 || N < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "B, H and N must not be negative");
+  if (d < 16 || d % 16 != 0) return fail(FP4ATTN_ERR_INVALID_ARG, "d=%lld must be a multiple of 16", (long long)d);
+  if (rotary_dim < 16 || rotary_dim % 16 != 0 || rotary_dim > d)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "rotary_dim=%lld must be a multiple of 16 up to d=%lld", (long long)rotary_dim,
+                (long long)d);
+  if (!std::isfinite(magnitude)) return fail(FP4ATTN_ERR_INVALID_ARG, "magnitude must be finite");
+  if ((interleaved != 0 && interleaved != 1) || (inverse != 0 && inverse != 1))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "interleaved and inverse must be 0 or 1");
+  if (x_strides == nullptr || out_strides == nullptr) return fail(FP4ATTN_ERR_INVALID_ARG, "strides are null");
+  for (int i = 0; i < 3; ++i) {
+    fp4attn_status st = check_stride(x_strides[i], dtype, "x stride");
+    if (st == FP4ATTN_OK) st = check_stride(out_strides[i], dtype, "out stride");
+    if (st != FP4ATTN_OK) return st;
+  }
+  if (position_stride < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "position_stride must not be negative");
+  if (d > fp4attn::kRotaryMaxDim || N > (1 << 24) || B > 65535 || H > 65535)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld H=%lld N=%lld d=%lld: at most 65535, 65535, 2^24 and %d", (long long)B,
+                (long long)H, (long long)N, (long long)d, fp4attn::kRotaryMaxDim);
+  if (B == 0 || H == 0 || N == 0) return ok();
+  REQUIRE_PTR(x);
+  REQUIRE_PTR(out);
+  REQUIRE_INDEX(positions);
+  REQUIRE_INDEX(inv_freq);
+  fp4attn::RotaryArgs a{};
+  a.x = x;
+  a.out = out;
+  a.B = B;
+  a.H = H;
+  a.N = N;
+  a.xb = x_strides[0];
+  a.xh = x_strides[1];
+  a.xn = x_strides[2];
+  a.ob = out_strides[0];
+  a.oh = out_strides[1];
+  a.on = out_strides[2];
+  a.d = (int)d;
+  a.r = (int)rotary_dim;
+  a.positions = positions;
+  a.pos_stride = position_stride;
+  a.inv_freq = inv_freq;
+  a.magnitude = magnitude;
+  a.bf16 = dtype == FP4ATTN_BF16;
+  a.interleaved = interleaved;
+  a.inverse = inverse;
+  return from_hip(fp4attn::launch_rotary(a, static_cast<hipStream_t>(stream)), "rotary launch");
+}
+
+fp4attn_status fp4attn_cache_write(const fp4attn_cache* cache, const void* k, const void* v, int src_dtype, int64_t n,
+                                   int64_t k_stride, int64_t v_stride, const int64_t* slots, void* stream) {
+  fp4attn::CacheWriteArgs a{};
+  fp4attn_status st = check_cache(cache, &a.c);
+  if (st != FP4ATTN_OK) return st;
+  if (src_dtype != FP4ATTN_F32 && src_dtype != FP4ATTN_BF16)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "src_dtype %d is not FP4ATTN_F32 or FP4ATTN_BF16", src_dtype);
+  st = check_tokens(a.c, n);
+  if (st == FP4ATTN_OK) st = check_stride(k_stride, src_dtype, "k_stride");
+  if (st == FP4ATTN_OK) st = check_stride(v_stride, src_dtype, "v_stride");
+  if (st != FP4ATTN_OK) return st;
+  if (n == 0) return ok();
+  REQUIRE_PTR(k);
+  REQUIRE_PTR(v);
+  REQUIRE_INDEX(slots);
+  a.k = k;
+  a.v = v;
+  a.n = n;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.slots = slots;
+  a.bf16 = src_dtype == FP4ATTN_BF16;
+  return from_hip(fp4attn::launch_cache_write(a, static_cast<hipStream_t>(stream)), "cache write launch");
+}
+
+fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slots, int64_t n, void* k, void* v,
+                                  int out_dtype, void* stream) {
+  fp4attn::CacheReadArgs a{};
+  fp4attn_status st = check_cache(cache, &a.c);
+  if (st != FP4ATTN_OK) return st;
+  if (out_dtype != FP4ATTN_F32 && out_dtype != FP4ATTN_BF16)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "out_dtype %d is not FP4ATTN_F32 or FP4ATTN_BF16", out_dtype);
+  st = check_tokens(a.c, n);
+  if (st != FP4ATTN_OK) return st;
+  if (n == 0) return ok();
+  REQUIRE_INDEX(slots);
+  REQUIRE_PTR(k);
+  REQUIRE_PTR(v);
+  a.n = n;
+  a.slots = slots;
+  a.k = k;
+  a.v = v;
+  a.bf16 = out_dtype == FP4ATTN_BF16;
+  return from_hip(fp4attn::launch_cache_read(a, static_cast<hipStream_t>(stream)), "cache read launch");
+}
+
+int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_heads, int64_t B, int64_t max_pages,
+                                          int64_t max_q) {
+  fp4attn::CacheView c{};
+  fp4attn::CachePlan plan;
+  if (check_cache_sizes(cache, &c) != FP4ATTN_OK ||
+      check_cache_attention(c, q_heads, B, max_pages, max_q, &plan) != FP4ATTN_OK)
+    return -1;
+  ok();
+  return plan.workspace;
+}
+
+fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
+                                       int64_t q_stride, int64_t B, const int32_t* page_table, int64_t max_pages,
+                                       const int32_t* lengths, const int32_t* q_starts, int64_t max_q,
+                                       const int64_t* tree, int64_t tree_words, float softmax_scale, void* out,
+                                       int out_dtype, float* lse, void* workspace, int64_t workspace_bytes,
+                                       void* stream) {
+  fp4attn::CacheAttentionArgs a{};
+  fp4attn_status st = check_cache(cache, &a.c);
+  if (st != FP4ATTN_OK) return st;
+  if (n < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "n=%lld must not be negative", (long long)n);
+  if (out_dtype != FP4ATTN_F32 && out_dtype != FP4ATTN_BF16)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "out_dtype %d is not FP4ATTN_F32 or FP4ATTN_BF16", out_dtype);
+  if (!std::isfinite(softmax_scale) || softmax_scale <= 0.0f)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "softmax_scale must be finite and positive");
+  st = check_stride(q_stride, FP4ATTN_BF16, "q_stride");
+  if (st != FP4ATTN_OK) return st;
+  if (n == 0) return ok();
+  fp4attn::CachePlan plan;
+  st = check_cache_attention(a.c, q_heads, B, max_pages, max_q, &plan);
+  if (st != FP4ATTN_OK) return st;
+  if (n > 0x7fffffff / q_heads)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "n=%lld tokens of %lld heads are too many", (long long)n, (long long)q_heads);
+  if (q_starts == nullptr && n != B * max_q)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "n=%lld is not B * max_q = %lld * %lld, and there are no q_starts", (long long)n,
+                (long long)B, (long long)max_q);
+  if (tree != nullptr && (tree_words < 1 || tree_words > (1 << 24) || tree_words * 64 < max_q))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "tree_words=%lld must hold max_q=%lld bits", (long long)tree_words,
+                (long long)max_q);
+  REQUIRE_PTR(q);
+  REQUIRE_PTR(out);
+  REQUIRE_INDEX(page_table);
+  REQUIRE_INDEX(lengths);
+  if (q_starts != nullptr) REQUIRE_INDEX(q_starts);
+  if (tree != nullptr) REQUIRE_INDEX(tree);
+  if (lse != nullptr) REQUIRE_INDEX(lse);
+  if (plan.workspace > 0) {
+    REQUIRE_PTR(workspace);
+    if (workspace_bytes < plan.workspace)
+      return fail(FP4ATTN_ERR_INVALID_ARG, "workspace of %lld bytes, %lld are needed", (long long)workspace_bytes,
+                  (long long)plan.workspace);
+  }
+  a.q = q;
+  a.q_stride = q_stride;
+  a.n = n;
+  a.B = (int)B;
+  a.Hq = (int)q_heads;
+  a.G = (int)(q_heads / a.c.H);
+  a.max_q = (int)max_q;
+  a.max_pages = (int)max_pages;
+  a.page_table = page_table;
+  a.lengths = lengths;
+  a.q_starts = q_starts;
+  a.tree = tree;
+  a.tree_words = tree != nullptr ? (int)tree_words : 0;
+  a.softmax_scale = softmax_scale;
+  a.out = out;
+  a.out_bf16 = out_dtype == FP4ATTN_BF16;
+  a.lse = lse;
+  a.workspace = workspace;
+  return from_hip(fp4attn::launch_cache_attention(a, static_cast<hipStream_t>(stream)), "cache attention launch");
 }
 
 fp4attn_status fp4attn_debug_mfma_stream(const uint8_t* a_codes, const uint8_t* b_codes, int blocks, int iters,

@@ -1,0 +1,166 @@
+// Rotary positions.
+//
+// Pair j of a head's first r channels turns by t = position * inv_freq[j]:
+//   y_a = m (x_a cos t - x_b sin t),  y_b = m (x_a sin t + x_b cos t),
+// (a, b) = (j, j + r / 2) or, interleaved, (2 j, 2 j + 1); channels past r pass through.
+// The inverse turns by -t: m R^T, which is the gradient of the rotation.
+//
+// Angles of far positions need more than 24 bits (position 10^6 at one radian a step is
+// off by 0.06 in fp32), so t and its reduction to a quarter turn are fp64; what is
+// left, |t| <= pi / 4, is exact to 2^-26 quarter turns in fp32.  A workgroup takes four tokens
+// and forms each token's angles once, in LDS, for all its heads.
+#include <cmath>
+
+#include "gfx950.hpp"
+#include "serving.hpp"
+
+namespace fp4attn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnit = 16;  // elements that a thread turns at once: 8 pairs
+
+template <typename T>
+struct Unit;  // 16 elements in two runs of 8
+template <>
+struct Unit<uint16_t> {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const uint16_t* pa, const uint16_t* pb) {
+    a = *reinterpret_cast<const uint4*>(pa);
+    b = *reinterpret_cast<const uint4*>(pb);
+  }
+  __device__ __forceinline__ void store(uint16_t* pa, uint16_t* pb) const {
+    *reinterpret_cast<uint4*>(pa) = a;
+    *reinterpret_cast<uint4*>(pb) = b;
+  }
+  __device__ __forceinline__ void get(float (&v)[16]) const {
+    const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[2 * i] = as_float(w[i] << 16);
+      v[2 * i + 1] = as_float(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[16]) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    unsigned w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __builtin_bit_cast(unsigned, bf2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
+    a = uint4{w[0], w[1], w[2], w[3]};
+    b = uint4{w[4], w[5], w[6], w[7]};
+  }
+};
+template <>
+struct Unit<float> {
+  float4 q[4];
+  __device__ __forceinline__ void load(const float* pa, const float* pb) {
+    q[0] = reinterpret_cast<const float4*>(pa)[0];
+    q[1] = reinterpret_cast<const float4*>(pa)[1];
+    q[2] = reinterpret_cast<const float4*>(pb)[0];
+    q[3] = reinterpret_cast<const float4*>(pb)[1];
+  }
+  __device__ __forceinline__ void store(float* pa, float* pb) const {
+    reinterpret_cast<float4*>(pa)[0] = q[0];
+    reinterpret_cast<float4*>(pa)[1] = q[1];
+    reinterpret_cast<float4*>(pb)[0] = q[2];
+    reinterpret_cast<float4*>(pb)[1] = q[3];
+  }
+  __device__ __forceinline__ void get(float (&v)[16]) const { __builtin_memcpy(v, q, sizeof(v)); }
+  __device__ __forceinline__ void set(const float (&v)[16]) { __builtin_memcpy(q, v, sizeof(v)); }
+};
+
+// grid: (token groups, head groups of `heads`, B)
+template <typename T, bool INTERLEAVED>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, int heads) {
+  constexpr int kItems = sizeof(T) == 2 ? 4 : 2;  // units of a thread in flight
+  __shared__ __attribute__((aligned(16))) float table[2][kRotaryTokens][kRotaryMaxDim / 2];
+  const int tid = threadIdx.x, half = a.r / 2;
+  const int64_t n0 = (int64_t)blockIdx.x * kRotaryTokens;
+  const int64_t b = blockIdx.z;
+  const int tokens = a.N - n0 < kRotaryTokens ? (int)(a.N - n0) : kRotaryTokens;
+  for (int i = tid; i < tokens * half; i += kThreads) {
+    const int tok = i / half, j = i - tok * half;
+    const double t = (double)a.positions[b * a.pos_stride + n0 + tok] * a.inv_freq[j];
+    const double quarters = t * 0.63661977236758134308;  // 2 / pi
+    const double whole = rint(quarters);
+    float s, c;
+    sincospif(0.5f * (float)(quarters - whole), &s, &c);
+    const int k = (int)(whole - 4.0 * floor(0.25 * whole));  // quarter turns, 0 .. 3
+    const float cc = k & 1 ? s : c, ss = k & 1 ? c : s;
+    table[0][tok][j] = a.magnitude * (k == 1 || k == 2 ? -cc : cc);
+    table[1][tok][j] = a.magnitude * ((k >= 2) != (a.inverse != 0) ? -ss : ss);
+  }
+  __syncthreads();
+  const int h0 = blockIdx.y * heads;
+  const int nh = a.H - h0 < heads ? (int)(a.H - h0) : heads;
+  const int units = a.d / kUnit, turned = a.r / kUnit;
+  const int count = units * nh * kRotaryTokens;
+  const T* x = static_cast<const T*>(a.x) + b * a.xb + n0 * a.xn + h0 * a.xh;
+  T* out = static_cast<T*>(a.out) + b * a.ob + n0 * a.on + h0 * a.oh;
+  const bool in_place = a.x == a.out;
+  for (int first = tid; first < count; first += kThreads * kItems) {
+    Unit<T> v[kItems];
+    int64_t at[kItems];  // of the unit's first run in `out`
+    int tok[kItems], u[kItems], gap[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      const int idx = first + i * kThreads, row = idx / units, h = row / kRotaryTokens;
+      u[i] = idx - row * units;
+      tok[i] = row % kRotaryTokens;
+      const bool turn = u[i] < turned;
+      if (idx >= count || tok[i] >= tokens || (in_place && !turn)) tok[i] = -1;
+      const int c = turn && !INTERLEAVED ? 8 * u[i] : kUnit * u[i];
+      gap[i] = turn && !INTERLEAVED ? half : 8;
+      at[i] = h * a.oh + tok[i] * a.on + c;
+      if (tok[i] >= 0) {
+        const T* p = x + h * a.xh + tok[i] * a.xn + c;
+        v[i].load(p, p + gap[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+      if (tok[i] < 0) continue;
+      if (u[i] < turned) {
+        float f[16], y[16];
+        v[i].get(f);
+        const float4* cp = reinterpret_cast<const float4*>(&table[0][tok[i]][8 * u[i]]);
+        const float4* sp = reinterpret_cast<const float4*>(&table[1][tok[i]][8 * u[i]]);
+        const float4 c0 = cp[0], c1 = cp[1], s0 = sp[0], s1 = sp[1];
+        const float c[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+        const float s[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int p = INTERLEAVED ? 2 * j : j, q = INTERLEAVED ? 2 * j + 1 : j + 8;
+          y[p] = fmaf(f[p], c[j], -(f[q] * s[j]));
+          y[q] = fmaf(f[p], s[j], f[q] * c[j]);
+        }
+        v[i].set(y);
+      }
+      v[i].store(out + at[i], out + at[i] + gap[i]);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream) {
+  // Heads of a workgroup: enough units for four of each thread where the grid stays
+  // large, one of each where it is small.
+  const int units = a.d / kUnit;
+  const int64_t groups = (a.N + kRotaryTokens - 1) / kRotaryTokens;
+  auto heads_for = [&](int per_thread) {
+    int64_t h = (int64_t)kThreads * per_thread / (units * kRotaryTokens);
+    h = h < 1 ? 1 : h;
+    return h > a.H ? a.H : h;
+  };
+  int64_t heads = heads_for(4);
+  if (groups * a.B * ((a.H + heads - 1) / heads) < 512) heads = heads_for(1);
+  const dim3 grid((unsigned)groups, (unsigned)((a.H + heads - 1) / heads), (unsigned)a.B);
+  auto* kernel = a.bf16 ? (a.interleaved ? rotary_kernel<uint16_t, true> : rotary_kernel<uint16_t, false>)
+                        : (a.interleaved ? rotary_kernel<float, true> : rotary_kernel<float, false>);
+  kernel<<<grid, kThreads, 0, stream>>>(a, (int)heads);
+  return hipGetLastError();
+}
+
+}  // namespace fp4attn
