@@ -28,6 +28,7 @@ class _NoBinding:
         return None
 
     forward = quantize_qkv = attention = forward_bf16 = _leave
+    rotary = cache_write = cache_read = cache_attention = _leave
 
 
 try:
@@ -410,6 +411,9 @@ def rotary(x, positions, inv_freq, interleaved=False, magnitude=1.0, inverse=Fal
     (j, j + r / 2), or (2 j, 2 j + 1) with ``interleaved``.  ``inverse`` turns back: applied
     to the gradient of the result it gives the gradient of ``x``.  ``x`` may have any strides
     with d contiguous; ``out`` may be ``x`` (in place)."""
+    r = _binding.rotary(x, positions, inv_freq, interleaved, magnitude, inverse, out)
+    if r is not None:
+        return _native(r)
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("x must be a GPU tensor")
     if x.dtype not in _DTYPES:
@@ -499,6 +503,10 @@ def cache_write(k, v, cache, slots):
     """Quantize ``k`` and ``v`` ([n, heads, d], bf16 or fp32; tokens may lie apart, as slices of
     a fused projection do) into ``slots`` (int64 [n], page * page_size + place) of ``cache``.
     Slots outside the cache (-1) mark padding and are skipped."""
+    r = _binding.cache_write(k, v, cache, slots)
+    if r is not None:
+        _native(r)
+        return
     c = _cache(cache)
     types = tuple(_DTYPES)
     ks, vs = _tokens(k, "k", types, c.heads, c.head_dim), _tokens(v, "v", types, c.heads, c.head_dim)
@@ -517,6 +525,9 @@ def cache_write(k, v, cache, slots):
 def cache_read(cache, slots, out_dtype=torch.float32):
     """(k, v), each [n, heads, d]: the values that ``slots`` (int64 [n]) of ``cache`` stand for;
     zeros for slots outside it."""
+    r = _binding.cache_read(cache, slots, out_dtype)
+    if r is not None:
+        return _native(r)
     c = _cache(cache)
     _need(slots, "slots", torch.int64, 1)
     if out_dtype not in _DTYPES:
@@ -543,6 +554,9 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
     Token t of T sees the keys up to its own, or with ``tree`` (int64 [n], or [n, words] for more
     than 64 tokens) the keys before the new tokens and the new tokens u whose bit is set.
     ``lse`` (fp32 [n, Hq]) receives the log normaliser.  A row that sees no key is 0 (-inf)."""
+    r = _binding.cache_attention(q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype)
+    if r is not None:
+        return _native(r)
     c = _cache(cache)
     H, d = c.heads, c.head_dim
     stride = _tokens(q, "q", (torch.bfloat16,))

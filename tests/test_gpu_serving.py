@@ -658,3 +658,87 @@ def test_outputs_are_deterministic_and_bounded(fa):
     got = b.call(fa, out=buf[1:-1], lse=lse[1:-1])
     assert torch.equal(got, first)
     assert bool((buf[0] == 7).all() and (buf[-1] == 7).all() and (lse[0] == 7).all() and (lse[-1] == 7).all())
+
+
+def test_native_calls_equal_the_python_path(fa, monkeypatch):
+    """The native call path against the checks in Python: calls that it takes, leaves to them, and refuses."""
+    from test_gpu_binding import _outcome, _PythonOnly, _Refused, _same, _Watched
+    g = torch.Generator(device="cuda").manual_seed(7)
+    B, T, H, G, d = 3, 2, 2, 2, 64
+    n, Hq = B * T, H * G
+    cache = fa.kv_cache(B * 80, H, 16, d)
+    wide = fa.kv_cache(4, H, 16, d, fp8=True)
+    fill = torch.randn((B * 1280, H, d), device="cuda", generator=g).bfloat16()
+    fa.cache_write(fill, fill, cache, torch.arange(B * 1280, device="cuda"))
+    table = torch.arange(B * 80, device="cuda", dtype=torch.int32).view(B, 80)
+    lengths = torch.tensor([40, 3, 1200], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, 2, 4, 6], dtype=torch.int32, device="cuda")
+    fused = torch.randn((n, Hq + 2 * H, d), device="cuda", generator=g).bfloat16()
+    q, k, v = fused[:, :Hq], fused[:, Hq:Hq + H], fused[:, Hq + H:]
+    tree = torch.tensor([1, 3] * B, device="cuda")
+    slots = torch.arange(n, device="cuda")
+    out32, out16 = (torch.empty((n, Hq, d), device="cuda", dtype=t) for t in (torch.float32, torch.bfloat16))
+    lse = torch.empty((n, Hq), device="cuda")
+    x = torch.randn((2, 3, 5, d), device="cuda", generator=g)
+    at, freq = torch.arange(5, device="cuda"), fa.rotary_frequencies(d)[0]
+    turned = torch.empty_like(x)
+
+    def wrote(*a):
+        c = fa.KVCache(*(t.clone() for t in a[2]))
+        return (fa.cache_write(a[0], a[1], c, *a[3:]), *c)[1:]
+    att = (q, cache, table, lengths)
+    taken = [
+        lambda: fa.rotary(x, at, freq), lambda: fa.rotary(x, at, freq, out=turned, inverse=True, magnitude=0.5),
+        lambda: fa.rotary(x, at.expand(2, 5).contiguous(), freq, interleaved=True),
+        lambda: fa.rotary(x.transpose(1, 2), torch.arange(3, device="cuda"), freq), lambda: fa.rotary(q, slots, freq),
+        lambda: fa.rotary(x[:1], at, freq[:8]), lambda: wrote(k, v, cache, slots), lambda: wrote(k.float(), v.float(), wide, slots),
+        lambda: wrote(k, v, tuple(cache), slots), lambda: fa.cache_read(cache, slots),
+        lambda: fa.cache_read(wide, slots, out_dtype=torch.bfloat16), lambda: fa.cache_attention(*att),
+        lambda: fa.cache_attention(*att, q_starts=starts, max_q=2, tree=tree, out=out16, lse=lse),
+        lambda: fa.cache_attention(*att, tree=tree.view(n, 1), softmax_scale=0.3, out_dtype=torch.bfloat16),
+        lambda: fa.cache_attention(*att, max_q=2, out=out32), lambda: fa.cache_attention(q.contiguous(), *att[1:]),
+    ]
+    left = [
+        lambda: fa.rotary(x, at, freq, magnitude=1), lambda: fa.rotary(x[:0], at, freq),
+        lambda: fa.rotary(x, at, freq, interleaved=1), lambda: wrote(k[:0], v[:0], cache, slots[:0]),
+        lambda: fa.cache_read(cache, slots[:0]), lambda: fa.cache_attention(*att, softmax_scale=1),
+        lambda: fa.cache_attention(q[:0], *att[1:]), lambda: fa.cache_attention(q, list(cache), table, lengths),
+    ]
+    refused = [
+        lambda: fa.rotary(x.double(), at, freq), lambda: fa.rotary(x, at.int(), freq), lambda: fa.rotary(x, at[:3], freq),
+        lambda: fa.rotary(x, at, freq.float()), lambda: fa.rotary(x, at, freq[:5]), lambda: fa.rotary(x[..., ::2], at, freq),
+        lambda: fa.rotary(x, at, freq, out=turned[:1]), lambda: fa.rotary(x, at, freq, out=turned[:, :, :1].expand(2, 3, 5, d)),
+        lambda: fa.rotary(x, at, freq, out=turned.bfloat16()),
+        lambda: fa.rotary(x, at, torch.zeros(64, dtype=torch.float64, device="cuda")), lambda: fa.rotary(x, at.cpu(), freq),
+        lambda: fa.rotary(x, at, freq, magnitude=float("inf")), lambda: fa.rotary(x[..., 4:], at, freq[:16]),
+        lambda: wrote(k, v[:3], cache, slots), lambda: wrote(k, v.float(), cache, slots), lambda: wrote(k, v, cache, slots.int()),
+        lambda: wrote(k.half(), v.half(), cache, slots), lambda: wrote(q, q, cache, slots), lambda: wrote(k, v, cache, slots[:2]),
+        lambda: wrote(k, v, cache._replace(k_scales=cache.k_scales[:1]), slots),
+        lambda: wrote(k, v, cache._replace(v_codes=wide.v_codes), slots), lambda: wrote(k, v, cache[:3], slots),
+        lambda: fa.cache_read(cache, slots, out_dtype=torch.float16), lambda: fa.cache_read(cache, slots.view(2, 3)),
+        lambda: fa.cache_attention(q.float(), *att[1:]), lambda: fa.cache_attention(q[:, :3], *att[1:]),
+        lambda: fa.cache_attention(q[:, :, :32], *att[1:]), lambda: fa.cache_attention(q[:5], *att[1:]),
+        lambda: fa.cache_attention(q, cache, table.long(), lengths), lambda: fa.cache_attention(q, cache, table[:2], lengths),
+        lambda: fa.cache_attention(q, cache, table[:, ::2], lengths), lambda: fa.cache_attention(q, cache, table, lengths[:2]),
+        lambda: fa.cache_attention(*att, q_starts=starts), lambda: fa.cache_attention(*att, q_starts=starts[:3], max_q=2),
+        lambda: fa.cache_attention(*att, max_q=3), lambda: fa.cache_attention(*att, tree=tree[:4]),
+        lambda: fa.cache_attention(*att, tree=tree.int()), lambda: fa.cache_attention(*att, q_starts=starts, max_q=65, tree=tree),
+        lambda: fa.cache_attention(*att, q_starts=starts, max_q=0), lambda: fa.cache_attention(*att, softmax_scale=-0.5),
+        lambda: fa.cache_attention(*att, out=out32[:3]), lambda: fa.cache_attention(*att, out=out32.half()),
+        lambda: fa.cache_attention(*att, lse=lse[:, :1]), lambda: fa.cache_attention(*att, out_dtype=torch.float16),
+        lambda: fa.cache_attention(q.transpose(0, 1), *att[1:]), lambda: fa.cache_attention(q, cache, table.cpu(), lengths),
+    ]
+    native, buffers = fa.api._binding, (out32, out16, lse, turned)
+    for kind, calls in (("taken", taken), ("left", left), ("refused", refused)):
+        for i, call in enumerate(calls):
+            watched = _Watched(native)
+            got = []
+            for binding in (watched, _PythonOnly()):
+                monkeypatch.setattr(fa.api, "_binding", binding)
+                got.append(_outcome(call, buffers))
+            a, b = got
+            assert _same(a, b), f"{kind} call {i}: {a} through the native path, {b} through Python"
+            assert isinstance(a, _Refused) == (kind == "refused"), f"{kind} call {i}: {a}"
+            if kind != "refused":
+                assert watched.took == (kind == "taken"), f"{kind} call {i}"
+    monkeypatch.setattr(fa.api, "_binding", native)
