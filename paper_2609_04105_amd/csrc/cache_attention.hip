@@ -34,6 +34,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 32;       // keys of a wave's step
+constexpr int kUnit = kTile * kWaves;  // keys of a workgroup's step
 constexpr float kLag = 8.0f;    // binades that a row's reference may lag its maximum
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -86,88 +87,87 @@ __device__ __forceinline__ Sequence sequence(const CacheAttentionArgs& a, int b)
   return s;
 }
 
-// Chunk `ci` of the batch: its sequence, first key, end, and its place among the
-// sequence's chunks.  Every wave finds it by itself.
-struct Chunk {
-  int b, index, count, first_chunk;  // first_chunk: ci of the sequence's chunk 0
-  int begin, end;
-  bool none;
+// Units of kUnit keys of sequence s in row tile `tile`: none without rows there, else at
+// least one, so that rows without keys are written.
+__device__ __forceinline__ int units_of(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& s, int tile) {
+  if (s.tokens * a.G <= tile * 16 * plan.nr) return 0;
+  return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit;
+}
+
+// The units that range `w` of a row tile takes, of all sequences laid end to end in one
+// line of `total` units: equal parts for every workgroup, whatever the lengths.
+struct Range {
+  int64_t total, begin, end;
+  int64_t at;  // of unit 0 of sequence b
+  int ranges, b, units;
 };
-__device__ __forceinline__ Chunk find_chunk(const CacheAttentionArgs& a, const CachePlan& plan, int ci) {
-  Chunk r{};
+__device__ __forceinline__ int64_t range_begin(int64_t w, int64_t total, int ranges) { return w * total / ranges; }
+
+// Every wave finds its range by itself, 64 sequences at a time.
+__device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const CachePlan& plan, int w, int tile) {
   const int lane = threadIdx.x & 63;
-  if (!plan.split) {
-    r.b = ci;
-    const Sequence s = sequence(a, ci);
-    r.count = 1;
-    r.first_chunk = ci;
-    r.end = s.keys;
-    r.none = s.tokens == 0;
-    return r;
-  }
-  int64_t total = 0;
-  for (int b = lane; b < a.B; b += 64) {
-    const Sequence s = sequence(a, b);
-    total += s.tokens ? s.keys : 0;
-  }
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) total += __shfl_xor(total, i);
-  int64_t chunk64 = (total + plan.target - 1) / plan.target;
-  chunk64 = chunk64 < plan.min_chunk ? plan.min_chunk : (chunk64 > kMaxCacheKeys ? kMaxCacheKeys : chunk64);
-  const int chunk = uniform((int)((chunk64 + kTile * kWaves - 1) / (kTile * kWaves) * (kTile * kWaves)));
-  int before = 0;
-  r.none = true;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int count = 0, keys = 0;
-    if (b0 + lane < a.B) {
-      const Sequence s = sequence(a, b0 + lane);
-      keys = s.keys;
-      count = s.tokens == 0 ? 0 : (keys == 0 ? 1 : (int)(((int64_t)keys + chunk - 1) / chunk));
-    }
-    int sum = count;  // inclusive prefix
+  Range r{};
+  auto scan = [&](int b0, int* own) {  // inclusive prefix over the lanes' sequences
+    int n = b0 + lane < a.B ? units_of(a, plan, sequence(a, b0 + lane), tile) : 0;
+    *own = n;
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) {
-      const int up = __shfl_up(sum, i);
-      if (lane >= i) sum += up;
+      const int up = __shfl_up(n, i);
+      n += lane >= i ? up : 0;
     }
-    const int start = before + sum - count;
-    const bool mine = ci >= start && ci < start + count;
-    const uint64_t found = __ballot(mine);
+    return n;
+  };
+  int own = 0, sum = scan(0, &own);
+  r.total = uniform(__shfl(sum, 63));
+  for (int b0 = 64; b0 < a.B; b0 += 64) r.total += uniform(__shfl(scan(b0, &own), 63));
+  const int64_t wanted = (r.total + plan.min_units - 1) / plan.min_units;
+  r.ranges = uniform((int)(wanted < 1 ? 1 : (wanted > plan.ranges ? plan.ranges : wanted)));
+  if (w >= r.ranges || r.total == 0) return r;  // empty: begin = end
+  r.begin = range_begin(w, r.total, r.ranges);
+  r.end = range_begin(w + 1, r.total, r.ranges);
+  int64_t before = 0;
+  if (a.B > 64) sum = scan(0, &own);
+  for (int b0 = 0;; b0 += 64) {
+    const int64_t from = before + sum - own;
+    const uint64_t found = __ballot(own > 0 && r.begin >= from && r.begin < from + own);
     if (found) {
       const int src = __ffsll((unsigned long long)found) - 1;
       r.b = uniform(b0 + src);
-      r.count = uniform(__shfl(count, src));
-      r.first_chunk = uniform(__shfl(start, src));
-      keys = uniform(__shfl(keys, src));
-      r.index = ci - r.first_chunk;
-      r.begin = r.index * chunk;
-      r.end = r.count == 1 ? keys : (r.index + 1 == r.count ? keys : r.begin + chunk);
-      r.none = false;
+      r.units = uniform(__shfl(own, src));
+      r.at = before + uniform(__shfl(sum - own, src));
       return r;
     }
     before += uniform(__shfl(sum, 63));
+    if (b0 + 64 >= a.B) break;  // not reached: begin < total
+    sum = scan(b0 + 64, &own);
   }
+  r.end = r.begin;
   return r;
 }
 
-// Partial results in the workspace: per sequence {first chunk, chunks}, then per tile of
-// (chunk, key head, row tile) the accumulators [tile_rows, D] and {reference, sum, sum of
-// the rounded values} per row.
+// Partial results in the workspace.  A sequence that crosses from range to range leaves a
+// piece in each: a range's first sequence in slot 0, its last in slot 1 (if it has more than one).
+// joins[tile][w]: the sequence whose first crossing is into range w, its pieces and the slot of
+// the first; or b = -1.  Then per row of a slot (range, side, key head, row tile): {reference, sum, sum
+// of the rounded values}, and the accumulators.
 struct Partials {
-  int2* sequences;
-  float* acc;
+  int4* joins;
   float4* stat;
+  float* acc;
 };
-__host__ __device__ inline int64_t partial_tiles(const CachePlan& p, int H) { return p.chunks * H * p.row_tiles; }
-__device__ __forceinline__ Partials partials(const CacheAttentionArgs& a, const CachePlan& p, int D) {
+__device__ __forceinline__ Partials partials(const CacheAttentionArgs& a, const CachePlan& p) {
   char* w = static_cast<char*>(a.workspace);
   Partials r;
-  r.sequences = reinterpret_cast<int2*>(w);
-  w += ((int64_t)a.B * 8 + 255) / 256 * 256;
+  r.joins = reinterpret_cast<int4*>(w);
+  w += (int64_t)p.ranges * p.row_tiles * 16;
   r.stat = reinterpret_cast<float4*>(w);
-  w += partial_tiles(p, a.c.H) * p.tile_rows * 16;
+  w += (int64_t)p.ranges * 2 * a.c.H * p.row_tiles * p.tile_rows * 16;
   r.acc = reinterpret_cast<float*>(w);
   return r;
+}
+__device__ __forceinline__ int64_t partial_row(const CacheAttentionArgs& a, const CachePlan& p, int w, int side, int head,
+                                               int tile) {
+  return ((((int64_t)w * 2 + side) * a.c.H + head) * p.row_tiles + tile) * p.tile_rows;
 }
 
 // N consecutive values, 16 bytes at a time.
@@ -224,21 +224,13 @@ __device__ __forceinline__ void load_words(const uint8_t* p, unsigned (&w)[N]) {
   }
 }
 
-// What a lane holds of one 32-key tile.
-template <int D, bool FP8>
-struct Tile {
-  using F = Format<D, FP8>;
-  unsigned k[2][F::kKWords];  // [half] key 8 (m / 4) + 4 half + m % 4, m = lane % 16: values D / 4 * (lane / 16) ..
-  unsigned ks[2];             // their E8M0 byte
-  unsigned v[F::kVWords];     // keys 8 (lane / 16) .. + 7, values D / 16 * (lane % 16) ..
-  unsigned vs[2];             // their eight E8M0 bytes
-};
-
 // The two pages of a tile (the same one unless pages hold 16 keys); -1: no such page.
+// The table is read through the scalar path, whose waits leave the tile loads in flight.
 struct Pages {
   int p0, p1;
 };
-__device__ __forceinline__ Pages find_pages(const CacheAttentionArgs& a, const int* __restrict__ table, int key0) {
+typedef const __attribute__((address_space(4))) int* ScalarInts;
+__device__ __forceinline__ Pages find_pages(const CacheAttentionArgs& a, ScalarInts table, int key0) {
   Pages r;
   r.p0 = table[key0 >> a.c.page_shift];
   r.p1 = r.p0;
@@ -246,34 +238,63 @@ __device__ __forceinline__ Pages find_pages(const CacheAttentionArgs& a, const i
     const int at = (key0 >> 4) + 1;
     r.p1 = table[at < a.max_pages ? at : a.max_pages - 1];
   }
-  r.p0 = (unsigned)r.p0 < (uint64_t)a.c.pages ? r.p0 : -1;
-  r.p1 = (unsigned)r.p1 < (uint64_t)a.c.pages ? r.p1 : -1;
   return r;
 }
+__device__ __forceinline__ bool is_page(const CacheView& c, int p) { return (unsigned)p < (uint64_t)c.pages; }
 
+// What a lane holds of one 32-key tile, and where it finds it.
 template <int D, bool FP8>
-__device__ __forceinline__ void load_tile(const CacheView& c, Pages pages, int key0, int head, int lane, Tile<D, FP8>& t) {
+struct Tile {
   using F = Format<D, FP8>;
-  const int m = lane & 15, g = lane >> 4, shift = c.page_shift;
-  const int inside = key0 & ((1 << shift) - 1);
-  // rows (page, head, offset) of the tile's two halves of 16 keys; a missing page reads page 0
-  const int64_t r0 = (((int64_t)(pages.p0 < 0 ? 0 : pages.p0) * c.H + head) << shift) + inside;
-  const int64_t r1 = shift == 4 ? ((int64_t)(pages.p1 < 0 ? 0 : pages.p1) * c.H + head) << 4 : r0 + 16;
-  const int64_t krow = (m >= 8 ? r1 : r0) + (m & 4) * 2 + (m & 3);
-  const int64_t vgroup = ((g >= 2 ? r1 : r0) >> 3) + (g & 1);
-  constexpr int kKBytes = F::kKWords * 4, kVBytes = F::kVWords * 4;
-  const uint8_t* kp = c.k_codes + krow * (4 * kKBytes) + g * kKBytes;
-  const uint8_t* ksp = c.k_scales + krow * F::kBlocks + g * F::kBlocks / 4;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    load_words<F::kKWords>(kp + h * 4 * (4 * kKBytes), t.k[h]);
-    t.ks[h] = ksp[h * 4 * F::kBlocks];
+  unsigned k[2][F::kKWords];  // [half] key 8 (m / 4) + 4 half + m % 4, m = lane % 16: values D / 4 * (lane / 16) ..
+  unsigned ks[2];             // their E8M0 byte
+  unsigned v[F::kVWords];     // keys 8 (lane / 16) .. + 7, values D / 16 * (lane % 16) ..
+  unsigned vs[2];             // their eight E8M0 bytes
+  static constexpr int kKBytes = F::kKWords * 4, kVBytes = F::kVWords * 4;
+
+  // Row (page, head, place); a missing page reads page 0.
+  static __device__ __forceinline__ int64_t row_of(const CacheView& c, int page, int head, int place) {
+    return (((int64_t)(is_page(c, page) ? page : 0) * c.H + head) << c.page_shift) + place;
   }
-  load_words<F::kVWords>(c.v_codes + (vgroup * 16 + m) * kVBytes, t.v);
-  const uint2 s = *reinterpret_cast<const uint2*>(c.v_scales + (vgroup * F::kBlocks + m * F::kBlocks / 16) * 8);
-  t.vs[0] = s.x;
-  t.vs[1] = s.y;
-}
+  // First row of the tile for the lanes of its lower and of its upper 16 keys: the same
+  // one, or with pages of 16 keys 16 rows before the second page's, so that a lane's
+  // offset is the same either way.
+  static __device__ __forceinline__ int64_t base_row(const CacheView& c, const Pages& pages, int key0, int head, bool upper) {
+    const int64_t row = row_of(c, pages.p0, head, key0 & ((1 << c.page_shift) - 1));
+    if (c.page_shift != 4) return row;
+    return upper ? row_of(c, pages.p1, head, 0) - 16 : row;
+  }
+  // The lane's byte offsets in a tile.
+  struct Lane {
+    unsigned k, ks, v, vs;
+    bool k_upper, v_upper;
+    __device__ __forceinline__ Lane(int lane) {
+      const unsigned m = lane & 15, g = lane >> 4, key = (m >> 2) * 8 + (m & 3);
+      k = key * (4 * kKBytes) + g * kKBytes;
+      ks = key * F::kBlocks + g * F::kBlocks / 4;
+      v = (g * 16 + m) * kVBytes;
+      vs = (g * F::kBlocks + m * F::kBlocks / 16) * 8;
+      k_upper = m >= 8;
+      v_upper = g >= 2;
+    }
+  };
+  __device__ __forceinline__ void load_k(const CacheView& c, const Pages& pages, int key0, int head, const Lane& l) {
+    const int64_t row = base_row(c, pages, key0, head, l.k_upper);
+    const uint8_t *kp = c.k_codes + row * (4 * kKBytes) + l.k, *ksp = c.k_scales + row * F::kBlocks + l.ks;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      load_words<F::kKWords>(kp + h * 4 * (4 * kKBytes), k[h]);
+      ks[h] = ksp[h * 4 * F::kBlocks];
+    }
+  }
+  __device__ __forceinline__ void load_v(const CacheView& c, const Pages& pages, int key0, int head, const Lane& l) {
+    const int64_t row = base_row(c, pages, key0, head, l.v_upper);
+    load_words<F::kVWords>(c.v_codes + row * (2 * kVBytes) + l.v, v);
+    const uint2 s = *reinterpret_cast<const uint2*>(c.v_scales + row * F::kBlocks + l.vs);
+    vs[0] = s.x;
+    vs[1] = s.y;
+  }
+};
 
 // The E8M0 byte as the converter's scale operand: a float's exponent field.
 __device__ __forceinline__ float scale_of(unsigned byte) { return as_float(byte << 23); }
@@ -298,20 +319,16 @@ __device__ __forceinline__ unsigned code_pair(const unsigned* w, float scale) {
 template <bool FP8>
 constexpr unsigned kHugeScale = FP8 ? 247u : 253u;
 
-// Keys that a row sees: j < limit, or a bit of the tree.
-struct Row {
-  int limit;            // causal: keys below; tree: the prefix
-  const int64_t* bits;  // of the row's token, or null
-};
-__device__ __forceinline__ unsigned below(int n) { return (1u << (n < 0 ? 0 : (n > 8 ? 8 : n))) - 1u; }
-// Which of keys key .. key + 7 the row sees, as bits.  Straight-line code: loads are
+// Which of keys key .. key + 7 a row sees, as bits: those under `limit`, and of the new
+// tokens those in its words of the tree (none if words = 0).  Straight-line code: loads are
 // clamped to the row's words instead of branched around.
-__device__ __forceinline__ unsigned seen8(const Row& r, int key, int prefix, int tokens, int words) {
-  unsigned see = below(r.limit - key);
+__device__ __forceinline__ unsigned below(int n) { return (1u << (n < 0 ? 0 : (n > 8 ? 8 : n))) - 1u; }
+__device__ __forceinline__ unsigned seen8(int limit, const int64_t* bits, int key, int prefix, int tokens, int words) {
+  unsigned see = below(limit - key);
   if (words) {  // uniform
     const int u = key - prefix, at = u >> 6, shift = u & 63;
     const int i = at < 0 ? 0 : (at >= words ? words - 1 : at), k = i + 1 < words ? i + 1 : i;
-    const uint64_t lo = (uint64_t)r.bits[i], hi = (uint64_t)r.bits[k];
+    const uint64_t lo = (uint64_t)bits[i], hi = (uint64_t)bits[k];
     const unsigned inside = (unsigned)(lo >> shift) | (shift > 56 ? (unsigned)(hi << (64 - shift)) : 0u);
     const unsigned up = u > -8 ? (unsigned)lo << (-u & 7) : 0u;  // the first new token is key - u
     see |= (u < 0 ? up : inside) & below(tokens - u);
@@ -319,304 +336,356 @@ __device__ __forceinline__ unsigned seen8(const Row& r, int key, int prefix, int
   return see;
 }
 
+// Waves per SIMD that the registers are kept to.
+constexpr int waves_per_simd(int d, bool fp8, int nr) { return nr == 1 ? (d == 64 && !fp8 ? 4 : 3) : (nr == 4 && d == 128 ? 1 : 2); }
+
+// blockIdx.x: (range, key head, row tile)
 template <int D, bool FP8, int NR>
-__global__ __launch_bounds__(kThreads, NR == 1 ? 3 : 1) void cache_attention_kernel(const CacheAttentionArgs a, const CachePlan plan) {
+__global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_attention_kernel(const CacheAttentionArgs a,
+                                                                                              const CachePlan plan) {
   using F = Format<D, FP8>;
-  constexpr int kV = D / 4;  // output values of a lane and row
+  constexpr int kV = D / 4;          // output values of a lane and row
+  constexpr bool kSharedQ = NR > 1;  // Q operands in LDS: NR * D / 8 registers less
+  // the joining waves' results, or Q before them
   __shared__ float4 lds_acc[kWaves / 2][NR * F::kDTiles][64];
   __shared__ float lds_stat[kWaves / 2][NR][3][64];
+  static_assert(!kSharedQ || sizeof(lds_acc) >= NR * F::kSteps * 64 * 16, "Q fits in the accumulators' place");
+  v4i(*lds_q)[64] = reinterpret_cast<v4i(*)[64]>(&lds_acc[0][0][0]);
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  // Row tiles of one (chunk, key head) go to one XCD (workgroups are dealt round-robin to
-  // eight), which then reads the chunk once for all of them.
+  // Row tiles of one (range, key head) go to one XCD (workgroups are dealt round-robin to
+  // eight), which then reads the keys once for all of them.
   int item = blockIdx.x, tile = 0;
   if (plan.row_tiles > 1) {
     const int q = item / 8;
     tile = q % plan.row_tiles;
     item = q / plan.row_tiles * 8 + item % 8;
   }
-  const int ci = item / a.c.H, head = item - ci * a.c.H;
-  if (ci >= plan.chunks) return;
-  const Chunk ch = find_chunk(a, plan, ci);
-  if (ch.none) return;
-  const Sequence seq = sequence(a, ch.b);
-  const int rows = seq.tokens * a.G, row0 = tile * 16 * NR;
-  if (plan.split && ch.index == 0 && head == 0 && tile == 0 && threadIdx.x == 0)
-    partials(a, plan, D).sequences[ch.b] = int2{ch.first_chunk, ch.count};
-  if (row0 >= rows) return;
+  const int w = item / a.c.H, head = item - w * a.c.H;
+  if (w >= plan.ranges) return;
 
-  // this lane's rows (the same for the four lane groups) and its part of their queries
-  Row row[NR];
-  v4i q[NR][F::kSteps];
-  int at[NR];  // row of q and out, as token * Hq + head
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1, t = ic / a.G;
-    const int token = seq.first + t, h = head * a.G + (ic - t * a.G);
-    at[r] = i < rows ? token * a.Hq + h : -1;
-    row[r].limit = a.tree ? seq.prefix : seq.prefix + t + 1;
-    row[r].limit = row[r].limit > seq.keys ? seq.keys : row[r].limit;
-    row[r].bits = a.tree ? a.tree + (int64_t)token * a.tree_words : nullptr;
-    const uint16_t* p = static_cast<const uint16_t*>(a.q) + token * a.q_stride + h * D + g * (D / 4);
-#pragma unroll
-    for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
-  }
-  // keys below `common` are seen by every row of the sequence
-  int common = a.tree ? seq.prefix : seq.prefix + 1;
-  common = common > seq.keys ? seq.keys : common;
-  int seen_tokens = seq.keys - seq.prefix;  // that have a bit in the tree
-  seen_tokens = seen_tokens > 64 * a.tree_words ? 64 * a.tree_words : seen_tokens;
-
-  v4f acc[NR][F::kDTiles], sum16[NR];  // sum16: the rounded probabilities, in every register
-  float ref[NR], sum[NR];              // base 2, lags the maximum by at most kLag; this lane's own keys
-  const v4i ones = {0x3f803f80, 0x3f803f80, 0x3f803f80, 0x3f803f80};
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-#pragma unroll
-    for (int t = 0; t < F::kDTiles; ++t) acc[r][t] = v4f{0, 0, 0, 0};
-    sum16[r] = v4f{0, 0, 0, 0};
-    ref[r] = -__builtin_inff();
-    sum[r] = 0.0f;
+  Range range{};
+  if (plan.split) {
+    range = find_range(a, plan, w, tile);
+    if (head == 0 && threadIdx.x == 0) {  // the sequence that crosses into this range for the first time
+      int4 join = {-1, 0, 0, 0};
+      if (range.begin < range.end && range.begin > range.at) {
+        const int64_t before = range_begin(w - 1, range.total, range.ranges), last = range.at + range.units;
+        if (range.at >= before)
+          join = int4{range.b, (int)((last * range.ranges + range.total - 1) / range.total - 1) - w + 2,
+                      range.at > before ? 1 : 0, 0};
+      }
+      partials(a, plan).joins[tile * plan.ranges + w] = join;
+    }
+    if (range.begin >= range.end) return;
+  } else {
+    range.b = w;
+    range.units = units_of(a, plan, sequence(a, w), tile);
+    range.end = range.units;
+    if (range.units == 0) return;
   }
   const float factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
-  const int* __restrict__ table = a.page_table + (int64_t)ch.b * a.max_pages;
+  const int64_t first_at = range.begin;
 
-  auto step = [&](Tile<D, FP8>& t, const Pages& pages, int key0) {
-    const bool masked = key0 + kTile > common || pages.p0 < 0 || pages.p1 < 0;  // uniform
-    if (masked) {
-      // Keys that no row sees hold anything: their V codes and scales become zero.  A
-      // non-finite V block that some row sees becomes zero too, and turns the outputs of
-      // the rows that see it to NaN here.
-      bool huge = false;
-      const int base = key0 + 8 * g;
-      const bool page_ok = (g >= 2 ? pages.p1 : pages.p0) >= 0;
+  while (true) {
+    // Units [range.begin, range.end) of the line, of which sequence range.b has [at, at + units).
+    const Sequence seq = sequence(a, range.b);
+    const int64_t seq_end = range.at + range.units;
+    const int64_t stop = seq_end < range.end ? seq_end : range.end;
+    const int begin = (int)(range.begin - range.at) * kUnit;
+    const int end = stop < seq_end ? (int)(stop - range.at) * kUnit : seq.keys;
+    const bool whole = range.begin == range.at && stop == seq_end;
+    const int rows = seq.tokens * a.G, row0 = tile * 16 * NR;
+
+    // this lane's rows (the same for the four lane groups) and its part of their queries
+    int token[NR];  // of the sequence
+    v4i q[kSharedQ ? 1 : NR][F::kSteps];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool there = page_ok && base + j < seq.keys;
-        const unsigned byte = t.vs[j / 4] >> (8 * (j % 4)) & 255u;
-        huge |= there && byte >= kHugeScale<FP8>;
-        if (!there || byte >= kHugeScale<FP8>) {
-          t.vs[j / 4] &= ~(255u << (8 * (j % 4)));
-          if constexpr (F::kVWords >= 8) {
+    for (int r = 0; r < NR; ++r) {
+      const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
+      token[r] = ic / a.G;
+      const int h = head * a.G + (ic - token[r] * a.G);
+      const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
+      if constexpr (kSharedQ) {
+        if (r % kWaves == wave || NR < kWaves)
 #pragma unroll
-            for (int w = 0; w < F::kVWords / 8; ++w) t.v[j * (F::kVWords / 8) + w] = 0u;
-          } else {
-            t.v[j / 2] &= j % 2 ? 0x0000ffffu : 0xffff0000u;
+          for (int s = 0; s < F::kSteps; ++s) lds_q[r * F::kSteps + s][lane] = reinterpret_cast<const v4i*>(p)[s];
+      } else {
+#pragma unroll
+        for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
+      }
+    }
+    if constexpr (kSharedQ) __syncthreads();
+    // keys below `common` are seen by every row of the sequence
+    int common = a.tree ? seq.prefix : seq.prefix + 1;
+    common = common > seq.keys ? seq.keys : common;
+    int seen_tokens = seq.keys - seq.prefix;  // that have a bit in the tree
+    seen_tokens = seen_tokens > 64 * a.tree_words ? 64 * a.tree_words : seen_tokens;
+    auto seen = [&](int r, int key) {
+      int limit = a.tree ? seq.prefix : seq.prefix + token[r] + 1;
+      limit = limit > seq.keys ? seq.keys : limit;
+      return seen8(limit, a.tree + (int64_t)(seq.first + token[r]) * a.tree_words, key, seq.prefix, seen_tokens, a.tree_words);
+    };
+
+    v4f acc[NR][F::kDTiles];
+    v4f sum16 = {0, 0, 0, 0};  // register r: the rounded probabilities of row tile r
+    unsigned poisoned = 0;     // bit r: this lane's columns of row r see a non-finite V block
+    float ref[NR], sum[NR];    // base 2, lags the maximum by at most kLag; this lane's own keys
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+#pragma unroll
+      for (int t = 0; t < F::kDTiles; ++t) acc[r][t] = v4f{0, 0, 0, 0};
+      ref[r] = -__builtin_inff();
+      sum[r] = 0.0f;
+    }
+    const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
+
+    // The wave's tiles.  One set of registers: a tile's K is loaded when the one before has
+    // become scores, its V when the one before is in the accumulators.
+    constexpr int kStride = kTile * kWaves;
+    int key0 = begin + kTile * wave;
+    if (key0 < end) {
+      Tile<D, FP8> t;
+      const typename Tile<D, FP8>::Lane part(lane);
+      Pages pages = find_pages(a, table, key0), next = pages;
+      t.load_k(a.c, pages, key0, head, part);
+      t.load_v(a.c, pages, key0, head, part);
+      if (key0 + kStride < end) next = find_pages(a, table, key0 + kStride);
+      while (true) {
+        const int ahead = key0 + kStride;
+        const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
+        const bool masked = key0 + kTile > common || !page0 || !page1;  // uniform
+        // S^T: register i of half h is key 8 g + 4 h + i
+        v4f s[NR][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float scale = scale_of(t.ks[h]);
+#pragma unroll
+          for (int r = 0; r < NR; ++r) s[r][h] = v4f{0, 0, 0, 0};
+          static_for<F::kSteps>([&](auto S_) {
+            constexpr int st = decltype(S_)::value;
+            v4i kk;
+            static_for<4>([&](auto I_) {
+              constexpr int i = decltype(I_)::value;
+              kk[i] = (int)code_pair<4 * st + i, FP8>(t.k[h], scale);
+            });
+#pragma unroll
+            for (int r = 0; r < NR; ++r) s[r][h] = mfma_16x16x32(kk, kSharedQ ? lds_q[r * F::kSteps + st][lane] : q[kSharedQ ? 0 : r][st], s[r][h]);
+          });
+        }
+        if (ahead < end) t.load_k(a.c, next, ahead, head, part);
+        if (masked) {
+          const int base = key0 + 8 * g;
+          const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - base) : 0u;
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const unsigned see = there & seen(r, base);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = see >> j & 1 ? s[r][j / 4][j % 4] : -__builtin_inff();
+          }
+        }
+        float top[NR];
+        bool rise = false;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          float x = fmaxf(fmaxf(s[r][0][0], s[r][0][1]), s[r][0][2]);
+          x = fmaxf(fmaxf(x, s[r][0][3]), s[r][1][0]);
+          x = fmaxf(fmaxf(x, s[r][1][1]), s[r][1][2]);
+          top[r] = groups_max(fmaxf(x, s[r][1][3])) * factor;
+          rise |= top[r] > ref[r] + kLag;
+        }
+        if (__any(rise)) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const float now = fmaxf(ref[r], top[r]);
+            const float down = now == ref[r] ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);
+            ref[r] = now;
+            sum[r] *= down;
+            sum16[r] *= down;
+#pragma unroll
+            for (int tt = 0; tt < F::kDTiles; ++tt) acc[r][tt] *= down;
+          }
+        }
+        v4i p[NR];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          const float base = ref[r] == -__builtin_inff() ? 0.0f : -ref[r];
+          float e[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[r][j / 4][j % 4], factor, base));
+          sum[r] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            p[r][j] = (int)__builtin_bit_cast(unsigned, v2bf{(__bf16)e[2 * j], (__bf16)e[2 * j + 1]});
+          // ones in the rows r, r + 4, r + 8, r + 12 of A: register r of every lane group
+          const int one = (lane & 3) == r ? 0x3f803f80 : 0;
+          sum16 = mfma_16x16x32(v4i{one, one, one, one}, p[r], sum16);
+        }
+        if (masked) {
+          // Keys that no row sees hold anything: their V codes and scales become zero.  A
+          // non-finite V block that some row sees becomes zero too, and marks the rows that
+          // see it, whose outputs become NaN after the loop.
+          bool huge = false;
+          const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - (key0 + 8 * g)) : 0u;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool in = there >> j & 1;
+            const unsigned byte = t.vs[j / 4] >> (8 * (j % 4)) & 255u;
+            huge |= in && byte >= kHugeScale<FP8>;
+            if (!in || byte >= kHugeScale<FP8>) {
+              t.vs[j / 4] &= ~(255u << (8 * (j % 4)));
+              if constexpr (F::kVWords >= 8) {
+#pragma unroll
+                for (int i = 0; i < F::kVWords / 8; ++i) t.v[j * (F::kVWords / 8) + i] = 0u;
+              } else {
+                t.v[j / 2] &= j % 2 ? 0x0000ffffu : 0xffff0000u;
+              }
+            }
+          }
+          if (__any(huge)) {  // lane group g holds outputs of d block g (d = 64: g / 2)
+            const int blk = g * F::kBlocks / 4;
+            for (int k = 0; k < kTile; ++k) {
+              const int page = k >= 16 ? pages.p1 : pages.p0, key = key0 + k;
+              if (!is_page(a.c, page) || key >= seq.keys) continue;
+              const int64_t group = Tile<D, FP8>::row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
+              if (a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] < kHugeScale<FP8>) continue;
+#pragma unroll
+              for (int r = 0; r < NR; ++r) poisoned |= (seen(r, key & ~7) >> (key & 7) & 1) << r;
+            }
+          }
+        }
+        // O^T: product t takes value t of every lane's part, rows d = D / 16 * m + t
+        float vscale[8];
+        static_for<8>([&](auto J_) { vscale[decltype(J_)::value] = scale_of_key<decltype(J_)::value>(t.vs); });
+        static_for<F::kDTiles / 2>([&](auto E_) {
+          constexpr int e = decltype(E_)::value;  // values 2 e, 2 e + 1 of the part
+          unsigned x[8];
+          static_for<8>([&](auto J_) {
+            constexpr int j = decltype(J_)::value;
+            x[j] = code_pair<j * (F::kDTiles / 2) + e, FP8>(t.v, vscale[j]);  // pair e of key j
+          });
+          v4i lo, hi;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            lo[j] = (int)__builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x05040100u);
+            hi[j] = (int)__builtin_amdgcn_perm(x[2 * j + 1], x[2 * j], 0x07060302u);
+          }
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            acc[r][2 * e] = mfma_16x16x32(lo, p[r], acc[r][2 * e]);
+            acc[r][2 * e + 1] = mfma_16x16x32(hi, p[r], acc[r][2 * e + 1]);
+          }
+          if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
+        });
+        if (ahead >= end) break;
+        t.load_v(a.c, next, ahead, head, part);
+        key0 = ahead;
+        pages = next;
+        if (ahead + kStride < end) next = find_pages(a, table, ahead + kStride);
+      }
+    }
+
+    float rounded[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      sum[r] = groups_sum(sum[r]);
+      rounded[r] = sum16[r];
+#pragma unroll
+      for (int t = 0; t < F::kDTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[r][t][i] = poisoned >> r & 1 ? as_float(0x7fc00000u) : acc[r][t][i];
+    }
+    // Join the waves, half of them at a time: same lanes, same rows and columns.
+#pragma unroll
+    for (int n = kWaves / 2; n >= 1; n /= 2) {
+      __syncthreads();
+      if (wave >= n && wave < 2 * n) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          lds_stat[wave - n][r][0][lane] = ref[r];
+          lds_stat[wave - n][r][1][lane] = sum[r];
+          lds_stat[wave - n][r][2][lane] = rounded[r];
+#pragma unroll
+          for (int t = 0; t < F::kDTiles; ++t)
+            lds_acc[wave - n][r * F::kDTiles + t][lane] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
+        }
+      }
+      __syncthreads();
+      if (wave < n) {
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+          const float other = lds_stat[wave][r][0][lane], top = fmaxf(ref[r], other);
+          const float mine = ref[r] == top ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - top);
+          const float its = other == top ? 1.0f : __builtin_amdgcn_exp2f(other - top);
+          ref[r] = top;
+          sum[r] = sum[r] * mine + lds_stat[wave][r][1][lane] * its;
+          rounded[r] = rounded[r] * mine + lds_stat[wave][r][2][lane] * its;
+#pragma unroll
+          for (int t = 0; t < F::kDTiles; ++t) {
+            const float4 o = lds_acc[wave][r * F::kDTiles + t][lane];
+            acc[r][t] = v4f{acc[r][t][0] * mine + o.x * its, acc[r][t][1] * mine + o.y * its,
+                            acc[r][t][2] * mine + o.z * its, acc[r][t][3] * mine + o.w * its};
           }
         }
       }
-      if (__any(huge)) {  // lane group g holds outputs of d block g (d = 64: g / 2)
-        const int blk = g * F::kBlocks / 4;
-        for (int k = 0; k < kTile; ++k) {
-          const int page = k >= 16 ? pages.p1 : pages.p0, key = key0 + k;
-          if (page < 0 || key >= seq.keys) continue;
-          const int64_t r8 = ((((int64_t)page * a.c.H + head) << a.c.page_shift) + (key & ((1 << a.c.page_shift) - 1))) >> 3;
-          if (a.c.v_scales[(r8 * F::kBlocks + blk) * 8 + (k & 7)] < kHugeScale<FP8>) continue;
+    }
+    if (wave == 0) {
 #pragma unroll
-          for (int r = 0; r < NR; ++r)
-            if (seen8(row[r], key & ~7, seq.prefix, seen_tokens, a.tree_words) >> (key & 7) & 1)
+      for (int r = 0; r < NR; ++r) {
+        const int i = row0 + 16 * r + m;
+        if (i >= rows) continue;
+        float o[kV];  // columns D / 4 * g ..: register i of product t is column D / 16 * (4 g + i) + t
 #pragma unroll
-              for (int tt = 0; tt < F::kDTiles; ++tt)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[r][tt][i] = as_float(0x7fc00000u);
+          for (int t = 0; t < F::kDTiles; ++t) o[j * F::kDTiles + t] = acc[r][t][j];
+        if (whole) {
+          const int64_t at = (int64_t)(seq.first + token[r]) * a.Hq + head * a.G + (i - token[r] * a.G);
+          const bool empty = is_zero(rounded[r]);
+          const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / rounded[r];
+#pragma unroll
+          for (int j = 0; j < kV; ++j) o[j] = empty ? 0.0f : o[j] * norm;
+          if (a.out_bf16) store_row<kV>(static_cast<uint16_t*>(a.out) + at * D + g * kV, o);
+          else store_row<kV>(static_cast<float*>(a.out) + at * D + g * kV, o);
+          if (a.lse && g == 0) a.lse[at] = log_norm(ref[r], sum[r]);
+        } else {
+          const Partials part = partials(a, plan);
+          const int64_t at = partial_row(a, plan, w, range.begin == first_at ? 0 : 1, head, tile) + 16 * r + m;
+          store_row<kV>(part.acc + at * D + g * kV, o);
+          if (g == 0) part.stat[at] = float4{ref[r], sum[r], rounded[r], 0.0f};
         }
       }
     }
-    // S^T: register i of half h is key 8 g + 4 h + i
-    v4f s[NR][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float scale = scale_of(t.ks[h]);
-#pragma unroll
-      for (int r = 0; r < NR; ++r) s[r][h] = v4f{0, 0, 0, 0};
-      static_for<F::kSteps>([&](auto S_) {
-        constexpr int st = decltype(S_)::value;
-        v4i kk;
-        static_for<4>([&](auto I_) {
-          constexpr int i = decltype(I_)::value;
-          kk[i] = (int)code_pair<4 * st + i, FP8>(t.k[h], scale);
-        });
-#pragma unroll
-        for (int r = 0; r < NR; ++r) s[r][h] = mfma_16x16x32(kk, q[r][st], s[r][h]);
-      });
-    }
-    if (masked) {
-      const int base = key0 + 8 * g;
-      const unsigned there = (g >= 2 ? pages.p1 : pages.p0) >= 0 ? below(seq.keys - base) : 0u;
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        const unsigned see = there & seen8(row[r], base, seq.prefix, seen_tokens, a.tree_words);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = see >> j & 1 ? s[r][j / 4][j % 4] : -__builtin_inff();
-      }
-    }
-    float top[NR];
-    bool rise = false;
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      float x = fmaxf(fmaxf(s[r][0][0], s[r][0][1]), s[r][0][2]);
-      x = fmaxf(fmaxf(x, s[r][0][3]), s[r][1][0]);
-      x = fmaxf(fmaxf(x, s[r][1][1]), s[r][1][2]);
-      top[r] = groups_max(fmaxf(x, s[r][1][3])) * factor;
-      rise |= top[r] > ref[r] + kLag;
-    }
-    if (__any(rise)) {
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        const float now = fmaxf(ref[r], top[r]);
-        const float down = now == ref[r] ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);
-        ref[r] = now;
-        sum[r] *= down;
-        sum16[r] *= down;
-#pragma unroll
-        for (int tt = 0; tt < F::kDTiles; ++tt) acc[r][tt] *= down;
-      }
-    }
-    v4i p[NR];
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-      const float base = ref[r] == -__builtin_inff() ? 0.0f : -ref[r];
-      float e[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(s[r][j / 4][j % 4], factor, base));
-      sum[r] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[r][j] = (int)__builtin_bit_cast(unsigned, v2bf{(__bf16)e[2 * j], (__bf16)e[2 * j + 1]});
-      sum16[r] = mfma_16x16x32(ones, p[r], sum16[r]);
-    }
-    // O^T: product t takes value t of every lane's part, rows d = D / 16 * m + t
-    float vscale[8];
-    static_for<8>([&](auto J_) { vscale[decltype(J_)::value] = scale_of_key<decltype(J_)::value>(t.vs); });
-    static_for<F::kDTiles / 2>([&](auto E_) {
-      constexpr int e = decltype(E_)::value;  // values 2 e, 2 e + 1 of the part
-      unsigned w[8];
-      static_for<8>([&](auto J_) {
-        constexpr int j = decltype(J_)::value;
-        // pair index within the lane's run of eight keys
-        w[j] = code_pair<j * (F::kDTiles / 2) + e, FP8>(t.v, vscale[j]);
-      });
-      v4i lo, hi;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        lo[j] = (int)__builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x05040100u);
-        hi[j] = (int)__builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x07060302u);
-      }
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        acc[r][2 * e] = mfma_16x16x32(lo, p[r], acc[r][2 * e]);
-        acc[r][2 * e + 1] = mfma_16x16x32(hi, p[r], acc[r][2 * e + 1]);
-      }
-    });
-  };
-
-  // The wave's tiles, one loaded ahead; the page table two ahead.
-  constexpr int kStride = kTile * kWaves;
-  int key0 = ch.begin + kTile * wave;
-  if (key0 < ch.end) {
-    Tile<D, FP8> cur, next;
-    Pages now = find_pages(a, table, key0), then = now;
-    load_tile<D, FP8>(a.c, now, key0, head, lane, cur);
-    if (key0 + kStride < ch.end) then = find_pages(a, table, key0 + kStride);
-    while (true) {
-      const int ahead = key0 + kStride;
-      Pages after = then;
-      if (ahead < ch.end) {
-        load_tile<D, FP8>(a.c, then, ahead, head, lane, next);
-        if (ahead + kStride < ch.end) after = find_pages(a, table, ahead + kStride);
-      }
-      step(cur, now, key0);
-      if (ahead >= ch.end) break;
-      key0 = ahead;
-      cur = next;
-      now = then;
-      then = after;
-    }
-  }
-
-#pragma unroll
-  for (int r = 0; r < NR; ++r) sum[r] = groups_sum(sum[r]);
-
-  // Join the waves, half of them at a time: same lanes, same rows and columns.
-#pragma unroll
-  for (int n = kWaves / 2; n >= 1; n /= 2) {
+    if (stop >= range.end) break;
+    // the next sequence that has rows here; there is one, since the line goes on
+    range.begin = range.at = stop;
+    do {
+      ++range.b;
+      range.units = range.b < a.B ? units_of(a, plan, sequence(a, range.b), tile) : 1;
+    } while (range.units == 0);
+    if (range.b >= a.B) break;
     __syncthreads();
-    if (wave >= n && wave < 2 * n) {
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        lds_stat[wave - n][r][0][lane] = ref[r];
-        lds_stat[wave - n][r][1][lane] = sum[r];
-        lds_stat[wave - n][r][2][lane] = sum16[r][0];
-#pragma unroll
-        for (int t = 0; t < F::kDTiles; ++t)
-          lds_acc[wave - n][r * F::kDTiles + t][lane] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
-      }
-    }
-    __syncthreads();
-    if (wave < n) {
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        const float other = lds_stat[wave][r][0][lane], top = fmaxf(ref[r], other);
-        const float mine = ref[r] == top ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - top);
-        const float its = other == top ? 1.0f : __builtin_amdgcn_exp2f(other - top);
-        ref[r] = top;
-        sum[r] = sum[r] * mine + lds_stat[wave][r][1][lane] * its;
-        sum16[r][0] = sum16[r][0] * mine + lds_stat[wave][r][2][lane] * its;
-#pragma unroll
-        for (int t = 0; t < F::kDTiles; ++t) {
-          const float4 o = lds_acc[wave][r * F::kDTiles + t][lane];
-          acc[r][t] = v4f{acc[r][t][0] * mine + o.x * its, acc[r][t][1] * mine + o.y * its,
-                          acc[r][t][2] * mine + o.z * its, acc[r][t][3] * mine + o.w * its};
-        }
-      }
-    }
-  }
-  if (wave != 0) return;
-
-#pragma unroll
-  for (int r = 0; r < NR; ++r) {
-    if (at[r] < 0) continue;
-    float o[kV];  // columns D / 4 * g ..: register i of product t is column D / 16 * (4 g + i) + t
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t = 0; t < F::kDTiles; ++t) o[i * F::kDTiles + t] = acc[r][t][i];
-    if (ch.count == 1) {
-      const float norm = is_zero(sum16[r][0]) ? 0.0f : (FP8 ? 1.0f : 1.0f / 6.0f) / sum16[r][0];
-#pragma unroll
-      for (int i = 0; i < kV; ++i) o[i] = is_zero(sum16[r][0]) ? 0.0f : o[i] * norm;
-      const int64_t to = (int64_t)at[r] * D + g * kV;
-      if (a.out_bf16) store_row<kV>(static_cast<uint16_t*>(a.out) + to, o);
-      else store_row<kV>(static_cast<float*>(a.out) + to, o);
-      if (a.lse && g == 0) a.lse[at[r]] = log_norm(ref[r], sum[r]);
-    } else {
-      const Partials w = partials(a, plan, D);
-      const int64_t to = (((int64_t)ci * a.c.H + head) * plan.row_tiles + tile) * plan.tile_rows + 16 * r + m;
-      store_row<kV>(w.acc + to * D + g * kV, o);
-      if (g == 0) w.stat[to] = float4{ref[r], sum[r], sum16[r][0], 0.0f};
-    }
   }
 }
 
-// Joins the chunks of one row: eight waves take D / 4-lane groups of chunks each.
-// grid: (rows of the longest sequence and all heads, B)
-constexpr int kJoinThreads = 512;
-template <int D, bool FP8>
+// Joins the pieces of the sequences that cross ranges.  A row takes D / 4 lanes of 4
+// columns; kSpread = 1: every group of lanes has its own row and walks the pieces;
+// else one row a workgroup, the pieces dealt to the groups.
+// grid: (rows of a row tile and all key heads / rows of a workgroup, ranges - 1, row tiles)
+constexpr int kJoinThreads = 256;
+template <int D, bool FP8, bool SPREAD>
 __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttentionArgs a, const CachePlan plan) {
-  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;  // lanes of a row; chunks in flight
-  const Partials w = partials(a, plan, D);
-  const int b = blockIdx.y;
-  const Sequence seq = sequence(a, b);
-  const int t = blockIdx.x / a.Hq, hq = blockIdx.x - t * a.Hq;
-  if (t >= seq.tokens) return;
-  const int2 chunks = w.sequences[b];
-  if (chunks.y <= 1) return;
-  const int head = hq / a.G, i = t * a.G + (hq - head * a.G);
-  const int tile = i / (16 * plan.nr), in_tile = i - tile * 16 * plan.nr;
-  const int64_t step = (int64_t)a.c.H * plan.row_tiles * plan.tile_rows;
-  const int64_t first = (((int64_t)chunks.x * a.c.H + head) * plan.row_tiles + tile) * plan.tile_rows + in_tile;
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+  const Partials part = partials(a, plan);
+  const int w = blockIdx.y + 1, tile = blockIdx.z;
+  const int4 job = part.joins[tile * plan.ranges + w];  // sequence, pieces, slot of the first
+  if (job.x < 0) return;
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  __shared__ float4 acc_lds[kGroups][kLanes];
-  __shared__ float4 stat_lds[kGroups];
+  const int row = SPREAD ? (int)blockIdx.x : (int)blockIdx.x * kGroups + group;
+  const int head = row / plan.tile_rows, in_tile = row - head * plan.tile_rows;
+  const Sequence seq = sequence(a, job.x);
+  const int i = tile * 16 * plan.nr + in_tile;
+  const bool there = head < a.c.H && i < seq.tokens * a.G;
   float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
   float4 acc = {0, 0, 0, 0};
   auto join = [&](const float4& s, const float4& o) {
@@ -628,23 +697,31 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
     sum16 = sum16 * mine + s.z * its;
     acc = float4{acc.x * mine + o.x * its, acc.y * mine + o.y * its, acc.z * mine + o.z * its, acc.w * mine + o.w * its};
   };
+  if (there) {
 #pragma unroll 4
-  for (int k = group; k < chunks.y; k += kGroups) {
-    const int64_t at = first + k * step;
-    join(w.stat[at], reinterpret_cast<const float4*>(w.acc + at * D)[lane]);
+    for (int k = SPREAD ? group : 0; k < job.y; k += SPREAD ? kGroups : 1) {
+      const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? job.z : 0, head, tile) + in_tile;
+      join(part.stat[at], reinterpret_cast<const float4*>(part.acc + at * D)[lane]);
+    }
   }
-  acc_lds[group][lane] = acc;
-  if (lane == 0) stat_lds[group] = float4{ref, sum, sum16, 0.0f};
-  __syncthreads();
-  if (group != 0) return;
-  const int used = chunks.y < kGroups ? chunks.y : kGroups;
-  for (int k = 1; k < used; ++k) join(stat_lds[k], acc_lds[k][lane]);
-  const int at = (seq.first + t) * a.Hq + hq;
+  if constexpr (SPREAD) {
+    __shared__ float4 acc_lds[kGroups][kLanes];
+    __shared__ float4 stat_lds[kGroups];
+    acc_lds[group][lane] = acc;
+    if (lane == 0) stat_lds[group] = float4{ref, sum, sum16, 0.0f};
+    __syncthreads();
+    if (group != 0) return;
+    const int used = job.y < kGroups ? job.y : kGroups;
+    for (int k = 1; k < used; ++k) join(stat_lds[k], acc_lds[k][lane]);
+  }
+  if (!there) return;
+  const int t = i / a.G;
+  const int64_t at = (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
   const bool empty = is_zero(sum16);
   const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / sum16;
   const float o[4] = {empty ? 0.0f : acc.x * norm, empty ? 0.0f : acc.y * norm, empty ? 0.0f : acc.z * norm,
                       empty ? 0.0f : acc.w * norm};
-  const int64_t to = (int64_t)at * D + lane * 4;
+  const int64_t to = at * D + lane * 4;
   if (a.out_bf16) {
     const unsigned lo = __builtin_bit_cast(unsigned, v2bf{(__bf16)o[0], (__bf16)o[1]});
     const unsigned hi = __builtin_bit_cast(unsigned, v2bf{(__bf16)o[2], (__bf16)o[3]});
@@ -661,35 +738,41 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
   if (plan.nr == 1) cache_attention_kernel<D, FP8, 1><<<grid, kThreads, 0, stream>>>(a, plan);
   else if (plan.nr == 2) cache_attention_kernel<D, FP8, 2><<<grid, kThreads, 0, stream>>>(a, plan);
   else cache_attention_kernel<D, FP8, 4><<<grid, kThreads, 0, stream>>>(a, plan);
-  if (plan.split)
-    cache_join_kernel<D, FP8><<<dim3((unsigned)(a.max_q * a.Hq), (unsigned)a.B), kJoinThreads, 0, stream>>>(a, plan);
+  if (!plan.split || plan.ranges == 1) return;
+  const unsigned rows = (unsigned)(plan.tile_rows * a.c.H), per = kJoinThreads / (D / 4);
+  // many pieces a sequence: a workgroup for each row
+  if (plan.ranges >= 4 * a.B)
+    cache_join_kernel<D, FP8, true><<<dim3(rows, plan.ranges - 1, plan.row_tiles), kJoinThreads, 0, stream>>>(a, plan);
+  else
+    cache_join_kernel<D, FP8, false><<<dim3((rows + per - 1) / per, plan.ranges - 1, plan.row_tiles), kJoinThreads, 0,
+                                       stream>>>(a, plan);
 }
 
 }  // namespace
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys) {
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int fp8, int64_t max_q, int64_t max_keys) {
   CachePlan p{};
   const int64_t rows = max_q * G;
   p.nr = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
-  p.row_tiles = (int)((rows + 16 * p.nr - 1) / (16 * p.nr));
+  const int64_t row_tiles = (rows + 16 * p.nr - 1) / (16 * p.nr);
+  p.row_tiles = (int)row_tiles;
   p.tile_rows = (int)(rows < 16 * p.nr ? rows : 16 * p.nr);
-  p.min_chunk = 1024;
-  const int64_t wanted = 1024;  // workgroups
-  const int64_t per_chunk = H * p.row_tiles;
-  p.split = max_keys > p.min_chunk && B * per_chunk < 2 * wanted;
-  p.target = (int)(wanted / per_chunk < 1 ? 1 : wanted / per_chunk);
-  const int64_t most = B * ((max_keys + p.min_chunk - 1) / p.min_chunk);
-  p.chunks = p.split ? p.target + B : B;
-  if (p.split && most < p.chunks) p.chunks = most;
-  const int64_t items = p.row_tiles > 1 ? (p.chunks * H + 7) / 8 * 8 : p.chunks * H;
-  p.workgroups = items * p.row_tiles;
-  p.workspace = 0;
-  if (p.split) p.workspace = (B * 8 + 255) / 256 * 256 + p.chunks * per_chunk * p.tile_rows * (d * 4 + 16);
+  p.min_units = 4;
+  // Ranges: as many workgroups as the chip holds at once, so that all end together.
+  const int64_t slots = 256 * waves_per_simd((int)d, fp8, p.nr), per_range = H * row_tiles;
+  p.split = max_keys > 1024;
+  p.ranges = p.split ? (int)(slots / per_range < 1 ? 1 : slots / per_range) : (int)B;
+  const int64_t most = B * ((max_keys + kUnit - 1) / kUnit);  // units there can be
+  if (p.split && p.ranges > (most + p.min_units - 1) / p.min_units) p.ranges = (int)((most + p.min_units - 1) / p.min_units);
+  const int64_t items = row_tiles > 1 ? (p.ranges * H + 7) / 8 * 8 : p.ranges * H;
+  p.workgroups = items * row_tiles;
+  if (p.split && p.ranges > 1)
+    p.workspace = p.ranges * row_tiles * 16 + p.ranges * 2 * per_range * p.tile_rows * (d * 4 + 16);
   return p;
 }
 
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream) {
-  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
+  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.c.fp8, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
   if (a.c.d == 64 && a.c.fp8) launch_format<64, true>(a, plan, stream);
   else if (a.c.d == 64) launch_format<64, false>(a, plan, stream);
   else if (a.c.fp8) launch_format<128, true>(a, plan, stream);

@@ -58,23 +58,22 @@ hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
 
 // How one attention call is cut up.  Rows (token, head of the group) of a sequence and
-// key head go to waves in tiles of 16 * nr; its keys are cut into chunks of one length
-// for the whole batch, found on the device from the sequences' lengths: at least
-// min_chunk keys, and so that the batch makes about `target` chunks.
+// key head go to waves in tiles of 16 * nr.  With split, the keys of all sequences lie end
+// to end in units of 128, and each of `ranges` workgroups per key head and row tile takes an
+// equal part of that line (fewer ranges if that leaves less than min_units each); lengths are
+// known on the device only.  Without, range b is sequence b.
 struct CachePlan {
   int nr;         // 16-row tiles of a wave: 1, 2 or 4
   int row_tiles;  // row tiles of the longest sequence and one key head
   int tile_rows;  // rows of a tile that can be in use
-  int split;      // 0: no sequence is cut (one chunk each)
-  int target, min_chunk;
-  int64_t chunks;       // upper bound of chunks over the batch
-  int64_t workgroups;   // of the first launch
-  int64_t workspace;    // bytes
+  int split, ranges, min_units;
+  int64_t workgroups;  // of the first launch
+  int64_t workspace;   // bytes
 };
 
 constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys);
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int fp8, int64_t max_q, int64_t max_keys);
 
 struct CacheAttentionArgs {
   CacheView c;
