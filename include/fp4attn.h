@@ -390,7 +390,8 @@ fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slo
  * q_heads no multiple of heads, a q_stride that is negative or no multiple of 8,
  * n not B * max_q without q_starts, tree_words * 64 < max_q with a tree, softmax_scale not
  * finite or <= 0, a bad out_dtype, a workspace that is too small; UNSUPPORTED for n * q_heads
- * or max_q * q_heads of 2^31 or more, max_pages * page_size above 2^30, B above 65535, or more than 2^24 workgroups.
+ * or max_q * q_heads of 2^31 or more, max_pages * page_size above 2^30 or B times that above
+ * 2^36, B above 65535, or more than 2^24 workgroups.
  */
 fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
                                        int64_t q_stride, int64_t B, const int32_t* page_table, int64_t max_pages,

@@ -264,8 +264,9 @@ fp4attn_status check_cache_attention(const fp4attn::CacheView& c, int64_t q_head
   if (q_heads % c.H != 0)
     return fail(FP4ATTN_ERR_INVALID_ARG, "q_heads=%lld is no multiple of the cache's %d heads", (long long)q_heads, c.H);
   if (B > 65535) return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld is above 65535", (long long)B);
-  if (max_pages > fp4attn::kMaxCacheKeys >> c.page_shift)
-    return fail(FP4ATTN_ERR_UNSUPPORTED, "max_pages=%lld: more than 2^30 keys a sequence", (long long)max_pages);
+  if (max_pages > fp4attn::kMaxCacheKeys >> c.page_shift || B > (int64_t(1) << 36) / (max_pages << c.page_shift))
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_pages=%lld: more than 2^30 keys a sequence or 2^36 in all",
+                (long long)B, (long long)max_pages);
   if (q_heads > 0x7fffffff || max_q > 0x7fffffff / q_heads)
     return fail(FP4ATTN_ERR_UNSUPPORTED, "max_q=%lld tokens of %lld heads are too many", (long long)max_q,
                 (long long)q_heads);

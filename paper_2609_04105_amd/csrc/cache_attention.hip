@@ -59,7 +59,14 @@ __device__ __forceinline__ float groups_sum(float x) {
   return as_float(r[0]) + as_float(r[1]);
 }
 
-// New tokens, keys and chunks of the sequences.
+__device__ __forceinline__ unsigned groups_or(unsigned x) {
+  auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  x = r[0] | r[1];
+  r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return r[0] | r[1];
+}
+
+// New tokens and keys of a sequence.
 struct Sequence {
   int first, tokens;  // rows of q
   int keys;           // lengths[b], within [0, the table's capacity]
@@ -77,7 +84,7 @@ __device__ __forceinline__ Sequence sequence(const CacheAttentionArgs& a, int b)
     s.prefix = (len < 0 ? 0 : len) - (int)(to - from);
     s.keys = len;
   } else {
-    s.tokens = (int)(a.n / a.B);
+    s.tokens = a.max_q;  // n = B * max_q
     s.first = b * s.tokens;
     s.keys = a.lengths[b];
     s.prefix = (s.keys < 0 ? 0 : s.keys) - s.tokens;
@@ -94,62 +101,78 @@ __device__ __forceinline__ int units_of(const CacheAttentionArgs& a, const Cache
   return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit;
 }
 
-// The units that range `w` of a row tile takes, of all sequences laid end to end in one
-// line of `total` units: equal parts for every workgroup, whatever the lengths.
+// All sequences laid end to end in one line, each as kSetup places for what starting one costs
+// and then its units; range w takes places [w per, (w + 1) per): equal parts for every
+// workgroup, whatever the lengths.
+constexpr int kSetup = 4;
 struct Range {
-  int64_t total, begin, end;
-  int64_t at;  // of unit 0 of sequence b
-  int ranges, b, units;
+  int begin, end;
+  int b, at, units;  // a sequence of the range: units at places [at, at + units)
+  Sequence seq;
+  int per;
 };
-__device__ __forceinline__ int64_t range_begin(int64_t w, int64_t total, int ranges) { return w * total / ranges; }
+
+// Inclusive prefix sum over the wave's lanes: within rows of 16, then across them.
+__device__ __forceinline__ int prefix_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr 1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15: rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast 31: rows 2 and 3
+  return x;
+}
 
 // Every wave finds its range by itself, 64 sequences at a time.
 __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const CachePlan& plan, int w, int tile) {
   const int lane = threadIdx.x & 63;
   Range r{};
-  auto scan = [&](int b0, int* own) {  // inclusive prefix over the lanes' sequences
-    int n = b0 + lane < a.B ? units_of(a, plan, sequence(a, b0 + lane), tile) : 0;
-    *own = n;
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const int up = __shfl_up(n, i);
-      n += lane >= i ? up : 0;
+  Sequence seq{};  // the lane's
+  int own = 0, sum = 0, total = 0;
+  auto scan = [&](int b0) {  // own: the sequence's places; sum: inclusive prefix over the lanes
+    own = 0;
+    if (b0 + lane < a.B) {
+      seq = sequence(a, b0 + lane);
+      own = units_of(a, plan, seq, tile);
+      own += own > 0 ? kSetup : 0;
     }
-    return n;
+    sum = prefix_sum(own);
   };
-  int own = 0, sum = scan(0, &own);
-  r.total = uniform(__shfl(sum, 63));
-  for (int b0 = 64; b0 < a.B; b0 += 64) r.total += uniform(__shfl(scan(b0, &own), 63));
-  const int64_t wanted = (r.total + plan.min_units - 1) / plan.min_units;
-  r.ranges = uniform((int)(wanted < 1 ? 1 : (wanted > plan.ranges ? plan.ranges : wanted)));
-  if (w >= r.ranges || r.total == 0) return r;  // empty: begin = end
-  r.begin = range_begin(w, r.total, r.ranges);
-  r.end = range_begin(w + 1, r.total, r.ranges);
-  int64_t before = 0;
-  if (a.B > 64) sum = scan(0, &own);
-  for (int b0 = 0;; b0 += 64) {
-    const int64_t from = before + sum - own;
-    const uint64_t found = __ballot(own > 0 && r.begin >= from && r.begin < from + own);
-    if (found) {
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    scan(b0);
+    total += __builtin_amdgcn_readlane(sum, 63);
+  }
+  r.per = (total + plan.ranges - 1) / plan.ranges;
+  r.per = r.per < plan.min_units ? plan.min_units : r.per;
+  r.begin = w * r.per;
+  r.end = r.begin + r.per < total ? r.begin + r.per : total;
+  if (r.begin >= total) return r;  // empty: begin >= end
+  for (int b0 = 0, before = 0;; b0 += 64) {
+    if (a.B > 64) scan(b0);
+    const int from = before + sum - own;
+    const uint64_t found = __ballot(r.begin >= from && r.begin < from + own);
+    if (found) {  // once, as begin < total
       const int src = __ffsll((unsigned long long)found) - 1;
-      r.b = uniform(b0 + src);
-      r.units = uniform(__shfl(own, src));
-      r.at = before + uniform(__shfl(sum - own, src));
+      r.b = b0 + src;
+      r.units = __builtin_amdgcn_readlane(own, src) - kSetup;
+      r.at = __builtin_amdgcn_readlane(from, src) + kSetup;
+      r.seq.first = __builtin_amdgcn_readlane(seq.first, src);
+      r.seq.tokens = __builtin_amdgcn_readlane(seq.tokens, src);
+      r.seq.keys = __builtin_amdgcn_readlane(seq.keys, src);
+      r.seq.prefix = __builtin_amdgcn_readlane(seq.prefix, src);
       return r;
     }
-    before += uniform(__shfl(sum, 63));
-    if (b0 + 64 >= a.B) break;  // not reached: begin < total
-    sum = scan(b0 + 64, &own);
+    before += __builtin_amdgcn_readlane(sum, 63);
+    if (b0 + 64 >= a.B) return r;
   }
-  r.end = r.begin;
-  return r;
 }
 
 // Partial results in the workspace.  A sequence that crosses from range to range leaves a
-// piece in each: a range's first sequence in slot 0, its last in slot 1 (if it has more than one).
-// joins[tile][w]: the sequence whose first crossing is into range w, its pieces and the slot of
-// the first; or b = -1.  Then per row of a slot (range, side, key head, row tile): {reference, sum, sum
-// of the rounded values}, and the accumulators.
+// piece in each: its first in slot 1 of its range, the others in slot 0 of theirs.
+// joins[tile][w], of the sequence whose first crossing is into range w: its pieces (0: there is
+// none), first token and rows.
+// Then per row of a slot (range, side, key head, row tile): {reference, sum, sum of the rounded
+// values}, and the accumulators.
 struct Partials {
   int4* joins;
   float4* stat;
@@ -170,7 +193,7 @@ __device__ __forceinline__ int64_t partial_row(const CacheAttentionArgs& a, cons
   return ((((int64_t)w * 2 + side) * a.c.H + head) * p.row_tiles + tile) * p.tile_rows;
 }
 
-// N consecutive values, 16 bytes at a time.
+// N consecutive values.
 template <int N>
 __device__ __forceinline__ void store_row(float* p, const float (&v)[N]) {
 #pragma unroll
@@ -179,14 +202,12 @@ __device__ __forceinline__ void store_row(float* p, const float (&v)[N]) {
 }
 template <int N>
 __device__ __forceinline__ void store_row(uint16_t* p, const float (&v)[N]) {
+  static_assert(N == 4 || N == 8, "8 or 16 bytes");
+  unsigned w[N / 2];
 #pragma unroll
-  for (int i = 0; i < N / 8; ++i) {
-    unsigned w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = __builtin_bit_cast(unsigned, v2bf{(__bf16)v[8 * i + 2 * j], (__bf16)v[8 * i + 2 * j + 1]});
-    reinterpret_cast<uint4*>(p)[i] = uint4{w[0], w[1], w[2], w[3]};
-  }
+  for (int j = 0; j < N / 2; ++j) w[j] = __builtin_bit_cast(unsigned, v2bf{(__bf16)v[2 * j], (__bf16)v[2 * j + 1]});
+  if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = uint4{w[0], w[1], w[2], w[3]};
+  else *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
 }
 
 __device__ __forceinline__ bool is_zero(float x) { return (as_uint(x) << 1) == 0u; }
@@ -264,33 +285,26 @@ struct Tile {
     if (c.page_shift != 4) return row;
     return upper ? row_of(c, pages.p1, head, 0) - 16 : row;
   }
-  // The lane's byte offsets in a tile.
-  struct Lane {
-    unsigned k, ks, v, vs;
-    bool k_upper, v_upper;
-    __device__ __forceinline__ Lane(int lane) {
-      const unsigned m = lane & 15, g = lane >> 4, key = (m >> 2) * 8 + (m & 3);
-      k = key * (4 * kKBytes) + g * kKBytes;
-      ks = key * F::kBlocks + g * F::kBlocks / 4;
-      v = (g * 16 + m) * kVBytes;
-      vs = (g * F::kBlocks + m * F::kBlocks / 16) * 8;
-      k_upper = m >= 8;
-      v_upper = g >= 2;
-    }
-  };
-  __device__ __forceinline__ void load_k(const CacheView& c, const Pages& pages, int key0, int head, const Lane& l) {
-    const int64_t row = base_row(c, pages, key0, head, l.k_upper);
-    const uint8_t *kp = c.k_codes + row * (4 * kKBytes) + l.k, *ksp = c.k_scales + row * F::kBlocks + l.ks;
+  // The lane's byte offsets in a tile are formed from its number at every load (the empty asm
+  // keeps them from being held in registers through the loop).
+  __device__ __forceinline__ void load_k(const CacheView& c, const Pages& pages, int key0, int head, int lane) {
+    asm volatile("" : "+v"(lane));
+    const unsigned m = lane & 15, g = (unsigned)lane >> 4, key = (m >> 2) * 8 + (m & 3);
+    const int64_t row = base_row(c, pages, key0, head, m >= 8);
+    const uint8_t* kp = c.k_codes + row * (4 * kKBytes) + (key * (4 * kKBytes) + g * kKBytes);
+    const uint8_t* ksp = c.k_scales + row * F::kBlocks + (key * F::kBlocks + g * F::kBlocks / 4);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       load_words<F::kKWords>(kp + h * 4 * (4 * kKBytes), k[h]);
       ks[h] = ksp[h * 4 * F::kBlocks];
     }
   }
-  __device__ __forceinline__ void load_v(const CacheView& c, const Pages& pages, int key0, int head, const Lane& l) {
-    const int64_t row = base_row(c, pages, key0, head, l.v_upper);
-    load_words<F::kVWords>(c.v_codes + row * (2 * kVBytes) + l.v, v);
-    const uint2 s = *reinterpret_cast<const uint2*>(c.v_scales + row * F::kBlocks + l.vs);
+  __device__ __forceinline__ void load_v(const CacheView& c, const Pages& pages, int key0, int head, int lane) {
+    asm volatile("" : "+v"(lane));
+    const unsigned m = lane & 15, g = (unsigned)lane >> 4;
+    const int64_t row = base_row(c, pages, key0, head, g >= 2);
+    load_words<F::kVWords>(c.v_codes + row * (2 * kVBytes) + (unsigned)lane * kVBytes, v);
+    const uint2 s = *reinterpret_cast<const uint2*>(c.v_scales + row * F::kBlocks + (g * F::kBlocks + m * F::kBlocks / 16) * 8);
     vs[0] = s.x;
     vs[1] = s.y;
   }
@@ -337,20 +351,66 @@ __device__ __forceinline__ unsigned seen8(int limit, const int64_t* bits, int ke
 }
 
 // Waves per SIMD that the registers are kept to.
-constexpr int waves_per_simd(int d, bool fp8, int nr) { return nr == 1 ? (d == 64 && !fp8 ? 4 : 3) : (nr == 4 && d == 128 ? 1 : 2); }
+constexpr int waves_per_simd(int d, bool fp8, int nr) {
+  if (nr == 1) return 3;
+  if (nr == 2) return d == 64 ? 3 : 2;
+  return d == 64 ? 2 : 1;
+}
+
+// Joins the waves' results of one row and D / 16 columns, and stores them: as outputs if the
+// sequence is whole here, else as a piece.  lds: [wave][product][row, 4 g + i]; stat: the row's
+// {reference, sum, sum of the rounded values} of the first wave, 16 rows apart; poison: its mark,
+// 64 words apart.
+template <int D, bool FP8>
+__device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& seq,
+                                           const float* lds, const float* stat, const unsigned* poison, int i, int c,
+                                           int head, bool whole, int64_t piece) {
+  constexpr int kCols = D / 16;
+  if (i >= seq.tokens * a.G) return;
+  float top = -__builtin_inff(), sum = 0.0f, rounded = 0.0f, o[kCols];
+  unsigned bad = 0;
+#pragma unroll
+  for (int j = 0; j < kCols; ++j) o[j] = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, stat[w * 64]);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float ref = stat[w * 64], part = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
+    sum += stat[w * 64 + 1] * part;
+    rounded += stat[w * 64 + 2] * part;
+    bad |= poison[w * 64];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) o[j] += lds[(w * kCols + j) * 256 + threadIdx.x] * part;
+  }
+  const bool empty = is_zero(rounded);
+  const float norm = whole ? (empty ? 0.0f : (FP8 ? 1.0f : 1.0f / 6.0f) / rounded) : 1.0f;
+#pragma unroll
+  for (int j = 0; j < kCols; ++j) o[j] = bad ? as_float(0x7fc00000u) : o[j] * norm;
+  if (whole) {
+    const int t = i / a.G;
+    const int64_t at = (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
+    if (a.out_bf16) store_row<kCols>(static_cast<uint16_t*>(a.out) + at * D + c * kCols, o);
+    else store_row<kCols>(static_cast<float*>(a.out) + at * D + c * kCols, o);
+    if (a.lse && c == 0) a.lse[at] = log_norm(top, sum);
+  } else {
+    const Partials p = partials(a, plan);
+    store_row<kCols>(p.acc + piece * D + c * kCols, o);
+    if (c == 0) p.stat[piece] = float4{top, sum, rounded, 0.0f};
+  }
+}
 
 // blockIdx.x: (range, key head, row tile)
 template <int D, bool FP8, int NR>
 __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_attention_kernel(const CacheAttentionArgs a,
                                                                                               const CachePlan plan) {
   using F = Format<D, FP8>;
-  constexpr int kV = D / 4;          // output values of a lane and row
   constexpr bool kSharedQ = NR > 1;  // Q operands in LDS: NR * D / 8 registers less
-  // the joining waves' results, or Q before them
-  __shared__ float4 lds_acc[kWaves / 2][NR * F::kDTiles][64];
-  __shared__ float lds_stat[kWaves / 2][NR][3][64];
-  static_assert(!kSharedQ || sizeof(lds_acc) >= NR * F::kSteps * 64 * 16, "Q fits in the accumulators' place");
-  v4i(*lds_q)[64] = reinterpret_cast<v4i(*)[64]>(&lds_acc[0][0][0]);
+  // the waves' results of one 16-row tile, or Q before them
+  constexpr int kAccWords = kWaves * F::kDTiles * 64, kQWords = kSharedQ ? NR * F::kSteps * 64 : 0;
+  __shared__ float4 lds[kAccWords > kQWords ? kAccWords : kQWords];
+  __shared__ float4 lds_stat[kWaves][16];
+  __shared__ unsigned lds_poison[kWaves][64];
+  v4i* lds_q = reinterpret_cast<v4i*>(lds);
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   // Row tiles of one (range, key head) go to one XCD (workgroups are dealt round-robin to
@@ -368,33 +428,29 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_at
   if (plan.split) {
     range = find_range(a, plan, w, tile);
     if (head == 0 && threadIdx.x == 0) {  // the sequence that crosses into this range for the first time
-      int4 join = {-1, 0, 0, 0};
-      if (range.begin < range.end && range.begin > range.at) {
-        const int64_t before = range_begin(w - 1, range.total, range.ranges), last = range.at + range.units;
-        if (range.at >= before)
-          join = int4{range.b, (int)((last * range.ranges + range.total - 1) / range.total - 1) - w + 2,
-                      range.at > before ? 1 : 0, 0};
-      }
+      int4 join = {0, 0, 0, 0};
+      if (range.begin < range.end && range.begin > range.at && range.at >= range.begin - range.per)
+        join = int4{(range.at + range.units - 1) / range.per - w + 2, range.seq.first, range.seq.tokens * a.G, 0};
       partials(a, plan).joins[tile * plan.ranges + w] = join;
     }
     if (range.begin >= range.end) return;
   } else {
     range.b = w;
-    range.units = units_of(a, plan, sequence(a, w), tile);
+    range.seq = sequence(a, w);
+    range.units = units_of(a, plan, range.seq, tile);
     range.end = range.units;
     if (range.units == 0) return;
   }
   const float factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
-  const int64_t first_at = range.begin;
 
   while (true) {
-    // Units [range.begin, range.end) of the line, of which sequence range.b has [at, at + units).
-    const Sequence seq = sequence(a, range.b);
-    const int64_t seq_end = range.at + range.units;
-    const int64_t stop = seq_end < range.end ? seq_end : range.end;
-    const int begin = (int)(range.begin - range.at) * kUnit;
-    const int end = stop < seq_end ? (int)(stop - range.at) * kUnit : seq.keys;
-    const bool whole = range.begin == range.at && stop == seq_end;
+    // The range's part of sequence range.b: keys [begin, end).
+    const int from = range.begin > range.at ? range.begin : range.at, seq_end = range.at + range.units;
+    const int stop = seq_end < range.end ? seq_end : range.end;
+    if (from >= stop) break;  // only places of its setup are left of the range
+    const Sequence seq = range.seq;
+    const int begin = (from - range.at) * kUnit, end = stop < seq_end ? (stop - range.at) * kUnit : seq.keys;
+    const bool whole = from == range.at && stop == seq_end;
     const int rows = seq.tokens * a.G, row0 = tile * 16 * NR;
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
@@ -409,7 +465,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_at
       if constexpr (kSharedQ) {
         if (r % kWaves == wave || NR < kWaves)
 #pragma unroll
-          for (int s = 0; s < F::kSteps; ++s) lds_q[r * F::kSteps + s][lane] = reinterpret_cast<const v4i*>(p)[s];
+          for (int s = 0; s < F::kSteps; ++s) lds_q[(r * F::kSteps + s) * 64 + lane] = reinterpret_cast<const v4i*>(p)[s];
       } else {
 #pragma unroll
         for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
@@ -446,10 +502,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_at
     int key0 = begin + kTile * wave;
     if (key0 < end) {
       Tile<D, FP8> t;
-      const typename Tile<D, FP8>::Lane part(lane);
       Pages pages = find_pages(a, table, key0), next = pages;
-      t.load_k(a.c, pages, key0, head, part);
-      t.load_v(a.c, pages, key0, head, part);
+      t.load_k(a.c, pages, key0, head, lane);
+      t.load_v(a.c, pages, key0, head, lane);
       if (key0 + kStride < end) next = find_pages(a, table, key0 + kStride);
       while (true) {
         const int ahead = key0 + kStride;
@@ -470,18 +525,50 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_at
               kk[i] = (int)code_pair<4 * st + i, FP8>(t.k[h], scale);
             });
 #pragma unroll
-            for (int r = 0; r < NR; ++r) s[r][h] = mfma_16x16x32(kk, kSharedQ ? lds_q[r * F::kSteps + st][lane] : q[kSharedQ ? 0 : r][st], s[r][h]);
+            for (int r = 0; r < NR; ++r)
+              s[r][h] = mfma_16x16x32(kk, kSharedQ ? lds_q[(r * F::kSteps + st) * 64 + lane] : q[kSharedQ ? 0 : r][st], s[r][h]);
           });
         }
-        if (ahead < end) t.load_k(a.c, next, ahead, head, part);
+        if (ahead < end) t.load_k(a.c, next, ahead, head, lane);
         if (masked) {
+          // Hidden scores become -inf.  Keys that no row sees hold anything: their V codes and
+          // scales become zero.  A non-finite V block that some row sees becomes zero too, and
+          // marks the rows that see it, whose outputs become NaN after the loop.
           const int base = key0 + 8 * g;
           const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - base) : 0u;
+          unsigned see[NR];
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
-            const unsigned see = there & seen(r, base);
+            see[r] = there & seen(r, base);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = see >> j & 1 ? s[r][j / 4][j % 4] : -__builtin_inff();
+            for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = see[r] >> j & 1 ? s[r][j / 4][j % 4] : -__builtin_inff();
+          }
+          unsigned huge = 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool in = there >> j & 1, big = (t.vs[j / 4] >> (8 * (j % 4)) & 255u) >= kHugeScale<FP8>;
+            huge |= in && big ? 1u : 0u;
+            const unsigned keep = in && !big ? ~0u : 0u;
+            t.vs[j / 4] &= keep | ~(255u << (8 * (j % 4)));
+            if constexpr (F::kVWords >= 8) {
+#pragma unroll
+              for (int i = 0; i < F::kVWords / 8; ++i) t.v[j * (F::kVWords / 8) + i] &= keep;
+            } else {
+              t.v[j / 2] &= keep | (j % 2 ? 0x0000ffffu : 0xffff0000u);
+            }
+          }
+          if (__any(huge)) {  // lane group g holds outputs of d block g (d = 64: g / 2)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) see[r] = groups_or(see[r] << (8 * g));
+            const int blk = g * F::kBlocks / 4;
+            for (int k = 0; k < kTile; ++k) {
+              const int page = k >= 16 ? pages.p1 : pages.p0, key = key0 + k;
+              if (!is_page(a.c, page) || key >= seq.keys) continue;
+              const int64_t group = Tile<D, FP8>::row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
+              const bool big = a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] >= kHugeScale<FP8>;
+#pragma unroll
+              for (int r = 0; r < NR; ++r) poisoned |= big ? (see[r] >> k & 1) << r : 0u;
+            }
           }
         }
         float top[NR];
@@ -521,39 +608,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_at
           const int one = (lane & 3) == r ? 0x3f803f80 : 0;
           sum16 = mfma_16x16x32(v4i{one, one, one, one}, p[r], sum16);
         }
-        if (masked) {
-          // Keys that no row sees hold anything: their V codes and scales become zero.  A
-          // non-finite V block that some row sees becomes zero too, and marks the rows that
-          // see it, whose outputs become NaN after the loop.
-          bool huge = false;
-          const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - (key0 + 8 * g)) : 0u;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const bool in = there >> j & 1;
-            const unsigned byte = t.vs[j / 4] >> (8 * (j % 4)) & 255u;
-            huge |= in && byte >= kHugeScale<FP8>;
-            if (!in || byte >= kHugeScale<FP8>) {
-              t.vs[j / 4] &= ~(255u << (8 * (j % 4)));
-              if constexpr (F::kVWords >= 8) {
-#pragma unroll
-                for (int i = 0; i < F::kVWords / 8; ++i) t.v[j * (F::kVWords / 8) + i] = 0u;
-              } else {
-                t.v[j / 2] &= j % 2 ? 0x0000ffffu : 0xffff0000u;
-              }
-            }
-          }
-          if (__any(huge)) {  // lane group g holds outputs of d block g (d = 64: g / 2)
-            const int blk = g * F::kBlocks / 4;
-            for (int k = 0; k < kTile; ++k) {
-              const int page = k >= 16 ? pages.p1 : pages.p0, key = key0 + k;
-              if (!is_page(a.c, page) || key >= seq.keys) continue;
-              const int64_t group = Tile<D, FP8>::row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
-              if (a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] < kHugeScale<FP8>) continue;
-#pragma unroll
-              for (int r = 0; r < NR; ++r) poisoned |= (seen(r, key & ~7) >> (key & 7) & 1) << r;
-            }
-          }
-        }
         // O^T: product t takes value t of every lane's part, rows d = D / 16 * m + t
         float vscale[8];
         static_for<8>([&](auto J_) { vscale[decltype(J_)::value] = scale_of_key<decltype(J_)::value>(t.vs); });
@@ -578,92 +632,38 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, FP8, NR)) void cache_at
           if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
         });
         if (ahead >= end) break;
-        t.load_v(a.c, next, ahead, head, part);
+        t.load_v(a.c, next, ahead, head, lane);
         key0 = ahead;
         pages = next;
         if (ahead + kStride < end) next = find_pages(a, table, ahead + kStride);
       }
     }
 
-    float rounded[NR];
+    // Join the waves, one 16-row tile at a time: thread (row, c) takes columns D / 16 * c .., which
+    // lane (row, g) of each wave holds in register i of its products, c = 4 g + i.
+    const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-      sum[r] = groups_sum(sum[r]);
-      rounded[r] = sum16[r];
+      __syncthreads();  // Q, or the tile before, is read
+      const float total = groups_sum(sum[r]);
 #pragma unroll
       for (int t = 0; t < F::kDTiles; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[r][t][i] = poisoned >> r & 1 ? as_float(0x7fc00000u) : acc[r][t][i];
-    }
-    // Join the waves, half of them at a time: same lanes, same rows and columns.
-#pragma unroll
-    for (int n = kWaves / 2; n >= 1; n /= 2) {
+        lds[(wave * F::kDTiles + t) * 64 + m * 4 + g] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
+      if (g == 0) lds_stat[wave][m] = float4{ref[r], total, sum16[r], 0.0f};
+      lds_poison[wave][m * 4 + g] = poisoned >> r & 1;
       __syncthreads();
-      if (wave >= n && wave < 2 * n) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          lds_stat[wave - n][r][0][lane] = ref[r];
-          lds_stat[wave - n][r][1][lane] = sum[r];
-          lds_stat[wave - n][r][2][lane] = rounded[r];
-#pragma unroll
-          for (int t = 0; t < F::kDTiles; ++t)
-            lds_acc[wave - n][r * F::kDTiles + t][lane] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
-        }
-      }
-      __syncthreads();
-      if (wave < n) {
-#pragma unroll
-        for (int r = 0; r < NR; ++r) {
-          const float other = lds_stat[wave][r][0][lane], top = fmaxf(ref[r], other);
-          const float mine = ref[r] == top ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - top);
-          const float its = other == top ? 1.0f : __builtin_amdgcn_exp2f(other - top);
-          ref[r] = top;
-          sum[r] = sum[r] * mine + lds_stat[wave][r][1][lane] * its;
-          rounded[r] = rounded[r] * mine + lds_stat[wave][r][2][lane] * its;
-#pragma unroll
-          for (int t = 0; t < F::kDTiles; ++t) {
-            const float4 o = lds_acc[wave][r * F::kDTiles + t][lane];
-            acc[r][t] = v4f{acc[r][t][0] * mine + o.x * its, acc[r][t][1] * mine + o.y * its,
-                            acc[r][t][2] * mine + o.z * its, acc[r][t][3] * mine + o.w * its};
-          }
-        }
-      }
+      join_waves<D, FP8>(a, plan, seq, reinterpret_cast<const float*>(lds), &lds_stat[0][row].x,
+                         &lds_poison[0][row * 4 + (c >> 2)], row0 + 16 * r + row, c, head, whole,
+                         partial_row(a, plan, w, from == range.at ? 1 : 0, head, tile) + 16 * r + row);
     }
-    if (wave == 0) {
-#pragma unroll
-      for (int r = 0; r < NR; ++r) {
-        const int i = row0 + 16 * r + m;
-        if (i >= rows) continue;
-        float o[kV];  // columns D / 4 * g ..: register i of product t is column D / 16 * (4 g + i) + t
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int t = 0; t < F::kDTiles; ++t) o[j * F::kDTiles + t] = acc[r][t][j];
-        if (whole) {
-          const int64_t at = (int64_t)(seq.first + token[r]) * a.Hq + head * a.G + (i - token[r] * a.G);
-          const bool empty = is_zero(rounded[r]);
-          const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / rounded[r];
-#pragma unroll
-          for (int j = 0; j < kV; ++j) o[j] = empty ? 0.0f : o[j] * norm;
-          if (a.out_bf16) store_row<kV>(static_cast<uint16_t*>(a.out) + at * D + g * kV, o);
-          else store_row<kV>(static_cast<float*>(a.out) + at * D + g * kV, o);
-          if (a.lse && g == 0) a.lse[at] = log_norm(ref[r], sum[r]);
-        } else {
-          const Partials part = partials(a, plan);
-          const int64_t at = partial_row(a, plan, w, range.begin == first_at ? 0 : 1, head, tile) + 16 * r + m;
-          store_row<kV>(part.acc + at * D + g * kV, o);
-          if (g == 0) part.stat[at] = float4{ref[r], sum[r], rounded[r], 0.0f};
-        }
-      }
-    }
+    // the next sequence that has rows here; there is one if the range goes on
     if (stop >= range.end) break;
-    // the next sequence that has rows here; there is one, since the line goes on
-    range.begin = range.at = stop;
     do {
-      ++range.b;
-      range.units = range.b < a.B ? units_of(a, plan, sequence(a, range.b), tile) : 1;
+      if (++range.b >= a.B) return;
+      range.seq = sequence(a, range.b);
+      range.units = units_of(a, plan, range.seq, tile);
     } while (range.units == 0);
-    if (range.b >= a.B) break;
+    range.at = stop + kSetup;
     __syncthreads();
   }
 }
@@ -678,14 +678,14 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
   const Partials part = partials(a, plan);
   const int w = blockIdx.y + 1, tile = blockIdx.z;
-  const int4 job = part.joins[tile * plan.ranges + w];  // sequence, pieces, slot of the first
-  if (job.x < 0) return;
+  const int4 job = part.joins[tile * plan.ranges + w];
+  const int pieces = job.x, first = job.y, rows = job.z;
+  if (pieces == 0) return;
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const int row = SPREAD ? (int)blockIdx.x : (int)blockIdx.x * kGroups + group;
   const int head = row / plan.tile_rows, in_tile = row - head * plan.tile_rows;
-  const Sequence seq = sequence(a, job.x);
   const int i = tile * 16 * plan.nr + in_tile;
-  const bool there = head < a.c.H && i < seq.tokens * a.G;
+  const bool there = head < a.c.H && i < rows;
   float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
   float4 acc = {0, 0, 0, 0};
   auto join = [&](const float4& s, const float4& o) {
@@ -699,8 +699,8 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
   };
   if (there) {
 #pragma unroll 4
-    for (int k = SPREAD ? group : 0; k < job.y; k += SPREAD ? kGroups : 1) {
-      const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? job.z : 0, head, tile) + in_tile;
+    for (int k = SPREAD ? group : 0; k < pieces; k += SPREAD ? kGroups : 1) {
+      const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? 1 : 0, head, tile) + in_tile;
       join(part.stat[at], reinterpret_cast<const float4*>(part.acc + at * D)[lane]);
     }
   }
@@ -711,24 +711,19 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
     if (lane == 0) stat_lds[group] = float4{ref, sum, sum16, 0.0f};
     __syncthreads();
     if (group != 0) return;
-    const int used = job.y < kGroups ? job.y : kGroups;
+    const int used = pieces < kGroups ? pieces : kGroups;
     for (int k = 1; k < used; ++k) join(stat_lds[k], acc_lds[k][lane]);
   }
   if (!there) return;
   const int t = i / a.G;
-  const int64_t at = (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
+  const int64_t at = (int64_t)(first + t) * a.Hq + head * a.G + (i - t * a.G);
   const bool empty = is_zero(sum16);
   const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / sum16;
   const float o[4] = {empty ? 0.0f : acc.x * norm, empty ? 0.0f : acc.y * norm, empty ? 0.0f : acc.z * norm,
                       empty ? 0.0f : acc.w * norm};
   const int64_t to = at * D + lane * 4;
-  if (a.out_bf16) {
-    const unsigned lo = __builtin_bit_cast(unsigned, v2bf{(__bf16)o[0], (__bf16)o[1]});
-    const unsigned hi = __builtin_bit_cast(unsigned, v2bf{(__bf16)o[2], (__bf16)o[3]});
-    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) = uint2{lo, hi};
-  } else {
-    store_row<4>(static_cast<float*>(a.out) + to, o);
-  }
+  if (a.out_bf16) store_row<4>(static_cast<uint16_t*>(a.out) + to, o);
+  else store_row<4>(static_cast<float*>(a.out) + to, o);
   if (a.lse && lane == 0) a.lse[at] = log_norm(ref, sum);
 }
 

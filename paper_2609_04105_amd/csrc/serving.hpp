@@ -59,9 +59,10 @@ hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
 
 // How one attention call is cut up.  Rows (token, head of the group) of a sequence and
 // key head go to waves in tiles of 16 * nr.  With split, the keys of all sequences lie end
-// to end in units of 128, and each of `ranges` workgroups per key head and row tile takes an
-// equal part of that line (fewer ranges if that leaves less than min_units each); lengths are
-// known on the device only.  Without, range b is sequence b.
+// to end in units of 128 (with a few places between sequences), and each of `ranges`
+// workgroups per key head and row tile takes an equal part of that line (fewer ranges if that
+// leaves less than min_units each); lengths are known on the device only.  Without, range b
+// is sequence b.
 struct CachePlan {
   int nr;         // 16-row tiles of a wave: 1, 2 or 4
   int row_tiles;  // row tiles of the longest sequence and one key head
