@@ -19,13 +19,13 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libfp4attn.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["fwd_mxfp4_guard.hip", "fwd_mxfp4_causal.hip", "fwd_mxfp4_ex2.hip", "fwd_mxfp4.hip",
-           "fwd_mxfp4_ex2_dense.hip", "fwd_mxfp4_fp8pv.hip", "fwd_bf16.hip", "cache_attention.hip", "api.hip", "quantize.hip",
-           "cache.hip", "rotary.hip", "mfma_stream.hip"]
+           "fwd_mxfp4_ex2_dense.hip", "fwd_mxfp4_fp8pv.hip", "fwd_bf16.hip", "cache_attention.hip", "cache_attention_rows.hip",
+           "api.hip", "quantize.hip", "cache.hip", "rotary.hip", "mfma_stream.hip"]
 # The attention kernels never rely on NaN ordering in fmax; without this flag the
 # compiler canonicalizes every fmax operand with an extra v_max_f32.
 EXTRA = {f: ["-fno-honor-nans"] for f in ("fwd_mxfp4.hip", "fwd_mxfp4_ex2.hip", "fwd_mxfp4_ex2_dense.hip",
                                           "fwd_mxfp4_guard.hip", "fwd_mxfp4_causal.hip", "fwd_mxfp4_fp8pv.hip",
-                                          "fwd_bf16.hip", "cache_attention.hip")}
+                                          "fwd_bf16.hip", "cache_attention.hip", "cache_attention_rows.hip")}
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")

@@ -58,23 +58,24 @@ hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
 
 // How one attention call is cut up.  Rows (token, head of the group) of a sequence and
-// key head go to waves in tiles of 16 * nr.  With split, the keys of all sequences lie end
-// to end in units of 128 (with a few places between sequences), and each of `ranges`
-// workgroups per key head and row tile takes an equal part of that line (fewer ranges if that
-// leaves less than min_units each); lengths are known on the device only.  Without, range b
-// is sequence b.
+// key head go to workgroups in tiles of 16, 32 (their waves split the keys) or 128 rows (their
+// waves split the rows).  With split, the keys of all sequences lie end to end in units of 128
+// (with a few places between sequences), and each of `ranges` workgroups per key head and row
+// tile takes an equal part of that line (fewer ranges if that leaves less than min_units
+// each); lengths are known on the device only.  Without, range b is sequence b.
 struct CachePlan {
-  int nr;         // 16-row tiles of a wave: 1, 2 or 4
-  int row_tiles;  // row tiles of the longest sequence and one key head
+  int tile;       // rows of a row tile
+  int row_tiles;  // of the longest sequence and one key head
   int tile_rows;  // rows of a tile that can be in use
   int split, ranges, min_units;
   int64_t workgroups;  // of the first launch
   int64_t workspace;   // bytes
 };
+constexpr int kRowsTile = 128, kRowsPerCu = 3;  // cache_attention_rows.hip: rows of a workgroup, workgroups of a CU
 
 constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int fp8, int64_t max_q, int64_t max_keys);
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys);
 
 struct CacheAttentionArgs {
   CacheView c;
@@ -94,6 +95,7 @@ struct CacheAttentionArgs {
   void* workspace;
 };
 
+void launch_cache_rows(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream);
 
 }  // namespace fp4attn
