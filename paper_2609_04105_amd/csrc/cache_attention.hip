@@ -385,7 +385,7 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
 
 }  // namespace
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys) {
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t max_keys) {
   CachePlan p{};
   const int64_t rows = max_q * G;
   p.tile = rows <= 16 ? 16 : (rows <= 32 ? 32 : kRowsTile);
@@ -394,7 +394,7 @@ CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, 
   p.tile_rows = (int)(rows < p.tile ? rows : p.tile);
   p.min_units = 4;
   // Ranges: as many workgroups as the chip holds at once, so that all end together.
-  const int64_t slots = 256 * (p.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, p.tile / 16));
+  const int64_t slots = 256 * (p.tile == kRowsTile ? rows_per_cu((int)d, fp8) : waves_per_simd((int)d, p.tile / 16));
   const int64_t per_range = H * row_tiles;
   p.split = max_keys > 1024;
   p.ranges = p.split ? (int)(slots / per_range < 1 ? 1 : slots / per_range) : (int)B;
@@ -408,7 +408,7 @@ CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, 
 }
 
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream) {
-  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
+  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.c.fp8 != 0, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
   if (a.c.d == 64 && a.c.fp8) launch_format<64, true>(a, plan, stream);
   else if (a.c.d == 64) launch_format<64, false>(a, plan, stream);
   else if (a.c.fp8) launch_format<128, true>(a, plan, stream);

@@ -15,39 +15,89 @@ namespace fp4attn {
 
 namespace {
 
-constexpr int kNr = 2;  // 16-row tiles of a wave
+constexpr int kNr = 2;    // 16-row tiles of a wave
+constexpr int kRing = 4;  // tiles whose codes are in LDS or on the way
 static_assert(kRowsTile == 16 * kNr * kWaves, "rows of a workgroup");
 
-// What a lane holds of a tile's codes: of K (waves 0, 1: halves 0, 1) a key's D / 4 values,
-// of V (waves 2, 3) four keys' D / 16 values.
+// Copies of 16 and 4 bytes a lane from memory to LDS bytes lds + 16 lane, lds + 4 lane.  Assembly, so
+// that the compiler counts neither the copies nor the LDS they write (it would wait for all of
+// them before every LDS read); the wave waits for its own with wait_copies.
+__device__ __forceinline__ void copy16(unsigned lds, const uint8_t* p) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(uniform((int)lds)) : "memory");
+}
+__device__ __forceinline__ void copy4(unsigned lds, const uint8_t* p) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(uniform((int)lds)) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_copies() {  // until at most N vector memory operations are in flight
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// A wave's share of a tile's codes, as it lies in LDS: of K (waves 0, 1: halves 0, 1) every lane a key's
+// D / 4 values, of V (waves 2, 3) four keys' D / 16 values; then the tile's K or V scales.
 template <int D, bool FP8>
-struct Raw {
+struct Share {
   using F = Format<D, FP8>;
-  static constexpr int kWords = F::kKWords, kBytes = 4 * kWords;
+  static constexpr int kWords = F::kKWords, kBytes = 4 * kWords;  // of a lane
+  static constexpr int kScaleBytes = kTile * F::kBlocks;
+  static constexpr int kSize = 64 * kBytes + kScaleBytes;
+  static constexpr int kCopies = (kWords == 2 ? 2 : kWords / 4) + 1;
   static_assert(F::kVWords == 2 * F::kKWords, "half a V run is a K run");
+
+  static __device__ __forceinline__ void copy(unsigned lds, const CacheView& c, const Pages& pages, int key0, int head,
+                                              int wave, int lane) {
+    asm volatile("" : "+v"(lane));  // offsets are formed here and not held through the loop
+    const unsigned m = lane & 15, g = (unsigned)lane >> 4;
+    const bool is_k = wave < 2;
+    const int64_t row = base_row(c, pages, key0, head, is_k ? m >= 8 : g >= 2);
+    const unsigned key = (m >> 2) * 8 + (m & 3) + 4 * wave;
+    const uint8_t* p = (is_k ? c.k_codes : c.v_codes) + row * (4 * kBytes) +
+                       (is_k ? key * (4 * kBytes) + g * kBytes : (unsigned)(lane * 2 + (wave - 2)) * kBytes);
+    if constexpr (kWords == 2) {
+      copy4(lds, p);
+      copy4(lds + 256, p + 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) copy16(lds + 1024 * i, p + 16 * i);
+    }
+    // the scales of 32 keys lie together, 16 keys in a half (K by key, V by eight keys)
+    if (lane < kScaleBytes / 4) {
+      const int64_t half = base_row(c, pages, key0, head, lane >= kScaleBytes / 8);
+      copy4(lds + 64 * kBytes, (is_k ? c.k_scales : c.v_scales) + half * F::kBlocks + 4 * lane);
+    }
+  }
+
   unsigned w[kWords];
   unsigned scale;  // K: an E8M0 byte; V: four
-
-  __device__ __forceinline__ void load(const CacheView& c, const Pages& pages, int key0, int head, int wave, int lane) {
-    const unsigned m = lane & 15, g = (unsigned)lane >> 4;
-    const int64_t row = base_row(c, pages, key0, head, wave < 2 ? m >= 8 : g >= 2);
-    if (wave < 2) {
-      const unsigned key = (m >> 2) * 8 + (m & 3) + 4 * wave;
-      load_words<kWords>(c.k_codes + row * (4 * kBytes) + (key * (4 * kBytes) + g * kBytes), w);
-      scale = c.k_scales[row * F::kBlocks + (key * F::kBlocks + g * F::kBlocks / 4)];
+  __device__ __forceinline__ void read(const uint8_t* lds, int wave, int lane) {
+    if constexpr (kWords == 2) {
+      w[0] = reinterpret_cast<const unsigned*>(lds)[lane];
+      w[1] = reinterpret_cast<const unsigned*>(lds + 256)[lane];
     } else {
-      load_words<kWords>(c.v_codes + row * (4 * kBytes) + (lane * 2 + (wave - 2)) * kBytes, w);
-      scale = *reinterpret_cast<const unsigned*>(c.v_scales + row * F::kBlocks +
-                                                 ((g * F::kBlocks + m * F::kBlocks / 16) * 8 + 4 * (wave - 2)));
+#pragma unroll
+      for (int i = 0; i < kWords / 4; ++i) {
+        const uint4 x = reinterpret_cast<const uint4*>(lds + 1024 * i)[lane];
+        w[4 * i] = x.x;
+        w[4 * i + 1] = x.y;
+        w[4 * i + 2] = x.z;
+        w[4 * i + 3] = x.w;
+      }
     }
+    const unsigned m = lane & 15, g = (unsigned)lane >> 4;
+    const uint8_t* sc = lds + 64 * kBytes;
+    if (wave < 2) scale = sc[((m >> 2) * 8 + (m & 3) + 4 * wave) * F::kBlocks + g * F::kBlocks / 4];
+    else scale = *reinterpret_cast<const unsigned*>(sc + (g * F::kBlocks + m * F::kBlocks / 16) * 8 + 4 * (wave - 2));
   }
 };
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const CacheAttentionArgs a, const CachePlan plan) {
+__global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kernel(const CacheAttentionArgs a, const CachePlan plan) {
   using F = Format<D, FP8>;
   __shared__ v4i k_lds[2][2][F::kSteps][64];  // [buffer][half][step][lane]
   __shared__ v4i v_lds[2][F::kDTiles][64];    // [buffer][product][lane]
+  using Codes = Share<D, FP8>;
+  __shared__ __attribute__((aligned(16))) uint8_t code_lds[kRing][kWaves][Codes::kSize];
   __shared__ unsigned huge_lds[2][2];         // [buffer][keys 0-3, 4-7 of eight]: a non-finite V block that some row sees
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -87,10 +137,10 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       sum[r] = 0.0f;
     }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
-    Raw<D, FP8> raw;
-
-    // Codes of the tile at key0 into buffer `buf`.
-    auto convert = [&](const Pages& pages, int key0, int buf) {
+    // The wave's codes of the tile at key0, in place `slot` of the ring, into buffer `buf`.
+    auto convert = [&](const Pages& pages, int key0, int slot, int buf) {
+      Codes raw;
+      raw.read(code_lds[slot][wave], wave, lane);
       if (wave < 2) {
         const float scale = scale_of(raw.scale);
         static_for<F::kSteps>([&](auto S_) {
@@ -218,32 +268,42 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       }
     };
 
-    // pages[i]: of the tile i ahead
-    int key0 = part.begin, buf = 0;
+    // Tile i of the part: its codes are copied into place i % kRing of the ring from kRing tiles
+    // before, when the place's last tile has been converted by every wave, and converted one
+    // tile before.  pages[j]: of the tile j ahead.
+    int key0 = part.begin, buf = 0, slot = 0;
     if (key0 < part.end) {
-      Pages pages[3];
+      Pages pages[kRing + 1];
       auto pages_at = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
+      auto copy = [&](const Pages& p, int key, int to) {
+        if (key < part.end) Codes::copy((unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)code_lds[to][wave], a.c, p, key, head, wave, lane);
+      };
 #pragma unroll
-      for (int i = 0; i < 3; ++i) pages[i] = pages_at(key0 + i * kTile);
-      raw.load(a.c, pages[0], key0, head, wave, lane);
-      convert(pages[0], key0, 0);
-      if (key0 + kTile < part.end) raw.load(a.c, pages[1], key0 + kTile, head, wave, lane);
+      for (int j = 0; j <= kRing; ++j) pages[j] = pages_at(key0 + j * kTile);
+#pragma unroll
+      for (int j = 0; j < kRing; ++j) copy(pages[j], key0 + j * kTile, j);
+      if (key0 + (kRing - 1) * kTile < part.end) wait_copies<(kRing - 1) * Codes::kCopies>();
+      else wait_copies<0>();
+      convert(pages[0], key0, 0, 0);
       __syncthreads();
       while (true) {
         const int ahead = key0 + kTile;
-        const Pages after = pages_at(key0 + 3 * kTile);
+        const Pages after = pages_at(key0 + (kRing + 1) * kTile);
         if (ahead < part.end) {
-          convert(pages[1], ahead, buf ^ 1);
-          if (ahead + kTile < part.end) raw.load(a.c, pages[2], ahead + kTile, head, wave, lane);
+          if (key0 + (kRing - 1) * kTile < part.end) wait_copies<(kRing - 2) * Codes::kCopies>();
+          else wait_copies<0>();
+          convert(pages[1], ahead, slot + 1 == kRing ? 0 : slot + 1, buf ^ 1);
+          copy(pages[kRing], key0 + kRing * kTile, slot);
         }
         if (row0 < rows) attend(pages[0], key0, buf);
         if (ahead >= part.end) break;
         __syncthreads();
         buf ^= 1;
+        slot = slot + 1 == kRing ? 0 : slot + 1;
         key0 = ahead;
-        pages[0] = pages[1];
-        pages[1] = pages[2];
-        pages[2] = after;
+#pragma unroll
+        for (int j = 0; j < kRing; ++j) pages[j] = pages[j + 1];
+        pages[kRing] = after;
       }
     }
 

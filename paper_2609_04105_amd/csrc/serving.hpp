@@ -71,11 +71,13 @@ struct CachePlan {
   int64_t workgroups;  // of the first launch
   int64_t workspace;   // bytes
 };
-constexpr int kRowsTile = 128, kRowsPerCu = 3;  // cache_attention_rows.hip: rows of a workgroup, workgroups of a CU
+// cache_attention_rows.hip: rows of a workgroup, and workgroups of a CU (registers; LDS for MXFP8 and d = 128)
+constexpr int kRowsTile = 128;
+constexpr int rows_per_cu(int d, bool fp8) { return d == 128 && fp8 ? 2 : 3; }
 
 constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys);
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t max_keys);
 
 struct CacheAttentionArgs {
   CacheView c;
