@@ -95,7 +95,6 @@ __device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const Ca
   store_columns<D, FP8>(a, plan, seq, i, head, c, whole, piece, top, sum, rounded, bad != 0, o);
 }
 
-// blockIdx.x: (range, key head, row tile)
 template <int D, bool FP8, int NR>
 __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attention_kernel(const CacheAttentionArgs a,
                                                                                          const CachePlan plan) {
@@ -109,17 +108,17 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
   v4i* lds_q = reinterpret_cast<v4i*>(lds);
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  const Place place = place_of(a, plan);
+  const Place place = place_of(plan);
   const int head = place.head;
-  if (place.w >= plan.ranges) return;
+  if (head >= a.c.H) return;
   Range range = open_range(a, plan, place);
   if (range.begin >= range.end) return;
   const float factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
 
   Part part;
-  while (open_part(a, plan, range, place.tile, &part)) {
+  while (open_part(a, plan, range, &part)) {
     const Sequence seq = range.seq;
-    const int rows = seq.tokens * a.G, row0 = place.tile * plan.tile;
+    const int rows = seq.tokens * a.G, row0 = range.tile * plan.tile;
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
     int token[NR];  // of the sequence
@@ -139,7 +138,12 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
         for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
       }
     }
-    if constexpr (kSharedQ) __syncthreads();
+    if constexpr (kSharedQ) {
+      __syncthreads();
+    } else {  // (waits for the queries here; in the loop the compiler would wait for tiles with them)
+#pragma unroll
+      for (int s = 0; s < F::kSteps; ++s) asm volatile("" : "+v"(q[0][s]));
+    }
     v4f acc[NR][F::kDTiles];
     v4f sum16 = {0, 0, 0, 0};  // register r: the rounded probabilities of row tile r
     unsigned poisoned = 0;     // bit r: this lane's columns of row r see a non-finite V block
@@ -301,30 +305,30 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       __syncthreads();
       join_waves<D, FP8>(a, plan, seq, reinterpret_cast<const float*>(lds), &lds_stat[0][row].x,
                          &lds_poison[0][row * 4 + (c >> 2)], row0 + 16 * r + row, c, head, part.whole,
-                         partial_row(a, plan, place.w, part.first ? 1 : 0, head, place.tile) + 16 * r + row);
+                         partial_row(a, plan, place.w, part.first ? 1 : 0, head) + 16 * r + row);
     }
-    if (!next_sequence(a, plan, place.tile, part.stop, range)) break;
+    if (!next_tile(a, plan, part.stop, range)) break;
     __syncthreads();
   }
 }
 
-// Joins the pieces of the sequences that cross ranges.  A row takes D / 4 lanes of 4
-// columns; kSpread = 1: every group of lanes has its own row and walks the pieces;
-// else one row a workgroup, the pieces dealt to the groups.
-// grid: (rows of a row tile and all key heads / rows of a workgroup, ranges - 1, row tiles)
+// Joins the pieces of the row tiles that cross ranges.  A row takes D / 4 lanes of 4 columns; with
+// SPREAD a workgroup has one row and deals the pieces to its groups of lanes, else every group
+// has its own row and walks the pieces.
+// grid: (rows of a row tile and all key heads / rows of a workgroup, ranges - 1)
 constexpr int kJoinThreads = 256;
 template <int D, bool FP8, bool SPREAD>
 __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttentionArgs a, const CachePlan plan) {
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
   const Partials part = partials(a, plan);
-  const int w = blockIdx.y + 1, tile = blockIdx.z;
-  const int4 job = part.joins[tile * plan.ranges + w];
+  const int w = blockIdx.y + 1;
+  const int4 job = part.joins[w];
   const int pieces = job.x, first = job.y, rows = job.z;
   if (pieces == 0) return;
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const int row = SPREAD ? (int)blockIdx.x : (int)blockIdx.x * kGroups + group;
   const int head = row / plan.tile_rows, in_tile = row - head * plan.tile_rows;
-  const int i = tile * plan.tile + in_tile;
+  const int i = job.w * plan.tile + in_tile;
   const bool there = head < a.c.H && i < rows;
   float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
   float4 acc = {0, 0, 0, 0};
@@ -340,7 +344,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
   if (there) {
 #pragma unroll 4
     for (int k = SPREAD ? group : 0; k < pieces; k += SPREAD ? kGroups : 1) {
-      const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? 1 : 0, head, tile) + in_tile;
+      const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? 1 : 0, head) + in_tile;
       join(part.stat[at], reinterpret_cast<const float4*>(part.acc + at * D)[lane]);
     }
   }
@@ -375,40 +379,39 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
   else launch_cache_rows(a, plan, stream);
   if (!plan.split || plan.ranges == 1) return;
   const unsigned rows = (unsigned)(plan.tile_rows * a.c.H), per = kJoinThreads / (D / 4);
-  // many pieces a sequence: a workgroup for each row
-  if (plan.ranges >= 16 * a.B)
-    cache_join_kernel<D, FP8, true><<<dim3(rows, plan.ranges - 1, plan.row_tiles), kJoinThreads, 0, stream>>>(a, plan);
+  // many pieces a row tile: a workgroup for each row
+  if (plan.ranges >= 16 * a.B * plan.row_tiles)
+    cache_join_kernel<D, FP8, true><<<dim3(rows, plan.ranges - 1), kJoinThreads, 0, stream>>>(a, plan);
   else
-    cache_join_kernel<D, FP8, false><<<dim3((rows + per - 1) / per, plan.ranges - 1, plan.row_tiles), kJoinThreads, 0,
-                                       stream>>>(a, plan);
+    cache_join_kernel<D, FP8, false><<<dim3((rows + per - 1) / per, plan.ranges - 1), kJoinThreads, 0, stream>>>(a, plan);
 }
 
 }  // namespace
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t max_keys) {
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys) {
   CachePlan p{};
   const int64_t rows = max_q * G;
   p.tile = rows <= 16 ? 16 : (rows <= 32 ? 32 : kRowsTile);
-  const int64_t row_tiles = (rows + p.tile - 1) / p.tile;
+  const int64_t row_tiles = (rows + p.tile - 1) / p.tile, units = (max_keys + kUnit - 1) / kUnit;
   p.row_tiles = (int)row_tiles;
   p.tile_rows = (int)(rows < p.tile ? rows : p.tile);
   p.min_units = 4;
-  // Ranges: as many workgroups as the chip holds at once, so that all end together.
-  const int64_t slots = 256 * (p.tile == kRowsTile ? rows_per_cu((int)d, fp8) : waves_per_simd((int)d, p.tile / 16));
-  const int64_t per_range = H * row_tiles;
   p.split = max_keys > 1024;
-  p.ranges = p.split ? (int)(slots / per_range < 1 ? 1 : slots / per_range) : (int)B;
-  const int64_t most = B * ((max_keys + kUnit - 1) / kUnit);  // units there can be
-  if (p.split && p.ranges > (most + p.min_units - 1) / p.min_units) p.ranges = (int)((most + p.min_units - 1) / p.min_units);
-  const int64_t items = row_tiles > 1 ? (p.ranges * H + 7) / 8 * 8 : p.ranges * H;
-  p.workgroups = items * row_tiles;
-  if (p.split && p.ranges > 1)
-    p.workspace = p.ranges * row_tiles * 16 + p.ranges * 2 * per_range * p.tile_rows * (d * 4 + 16);
+  // Ranges: as many workgroups as the chip holds at once, so that all end together.
+  const int64_t slots = 256 * (p.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, p.tile / 16));
+  const int64_t places = B * row_tiles * (units + kSetup);  // there can be
+  int64_t ranges = slots / H < 1 ? 1 : slots / H;
+  if (ranges > (places + p.min_units - 1) / p.min_units) ranges = (places + p.min_units - 1) / p.min_units;
+  if (!p.split) ranges = B * row_tiles;
+  p.fits = places < (int64_t(1) << 31) && ranges * H < (1 << 24);
+  p.ranges = (int)ranges;
+  p.workgroups = (ranges * H + 7) / 8 * 8;
+  if (p.split && ranges > 1) p.workspace = ranges * 16 + ranges * 2 * H * p.tile_rows * (d * 4 + 16);
   return p;
 }
 
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream) {
-  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.c.fp8 != 0, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
+  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
   if (a.c.d == 64 && a.c.fp8) launch_format<64, true>(a, plan, stream);
   else if (a.c.d == 64) launch_format<64, false>(a, plan, stream);
   else if (a.c.fp8) launch_format<128, true>(a, plan, stream);

@@ -92,20 +92,20 @@ __device__ __forceinline__ Sequence sequence(const CacheAttentionArgs& a, int b)
   return s;
 }
 
-// Units of kUnit keys of sequence s in row tile `tile` (rows tile * plan.tile ..): none without rows there, else at
-// least one, so that rows without keys are written.
-__device__ __forceinline__ int units_of(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& s, int tile) {
-  if (s.tokens * a.G <= tile * plan.tile) return 0;
-  return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit;
+// Units of kUnit keys; at least one, so that rows without keys are written.
+__device__ __forceinline__ int units_of(const Sequence& s) { return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int row_tiles_of(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& s) {
+  return (s.tokens * a.G + plan.tile - 1) / plan.tile;
 }
 
-// All sequences laid end to end in one line, each as kSetup places for what starting one costs
-// and then its units; range w takes places [w per, (w + 1) per): equal parts for every
-// workgroup, whatever the lengths.
+// The row tiles of all sequences laid end to end in one line, each as kSetup places for what
+// starting one costs and then its keys' units; range w takes places [w per, (w + 1) per): equal parts
+// for every workgroup, whatever the lengths and the numbers of rows.
 constexpr int kSetup = 4;
 struct Range {
   int begin, end;
-  int b, at, units;  // a sequence of the range: units at places [at, at + units)
+  int b, tile, tiles;  // a row tile of the range, of the sequence's `tiles`
+  int at, units;       // its units are at places [at, at + units)
   Sequence seq;
   int per;
 };
@@ -122,7 +122,7 @@ __device__ __forceinline__ int prefix_sum(int x) {
 }
 
 // Every wave finds its range by itself, 64 sequences at a time.
-__device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const CachePlan& plan, int w, int tile) {
+__device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const CachePlan& plan, int w) {
   const int lane = threadIdx.x & 63;
   Range r{};
   Sequence seq{};  // the lane's
@@ -131,8 +131,7 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
     own = 0;
     if (b0 + lane < a.B) {
       seq = sequence(a, b0 + lane);
-      own = units_of(a, plan, seq, tile);
-      own += own > 0 ? kSetup : 0;
+      own = row_tiles_of(a, plan, seq) * (units_of(seq) + kSetup);
     }
     sum = prefix_sum(own);
   };
@@ -152,12 +151,15 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
     if (found) {  // once, as begin < total
       const int src = __ffsll((unsigned long long)found) - 1;
       r.b = b0 + src;
-      r.units = __builtin_amdgcn_readlane(own, src) - kSetup;
-      r.at = __builtin_amdgcn_readlane(from, src) + kSetup;
       r.seq.first = __builtin_amdgcn_readlane(seq.first, src);
       r.seq.tokens = __builtin_amdgcn_readlane(seq.tokens, src);
       r.seq.keys = __builtin_amdgcn_readlane(seq.keys, src);
       r.seq.prefix = __builtin_amdgcn_readlane(seq.prefix, src);
+      r.units = units_of(r.seq);
+      r.tiles = row_tiles_of(a, plan, r.seq);
+      const int start = __builtin_amdgcn_readlane(from, src), places = r.units + kSetup;
+      r.tile = (r.begin - start) / places;
+      r.at = start + r.tile * places + kSetup;
       return r;
     }
     before += __builtin_amdgcn_readlane(sum, 63);
@@ -165,12 +167,11 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
   }
 }
 
-// Partial results in the workspace.  A sequence that crosses from range to range leaves a
-// piece in each: its first in slot 1 of its range, the others in slot 0 of theirs.
-// joins[tile][w], of the sequence whose first crossing is into range w: its pieces (0: there is
-// none), first token and rows.
-// Then per row of a slot (range, side, key head, row tile): {reference, sum, sum of the rounded
-// values}, and the accumulators.
+// Partial results in the workspace.  A row tile that crosses from range to range leaves a
+// piece in each: its first in slot 1 of its range, the others in slot 0 of theirs.  joins[w], of
+// the row tile whose first crossing is into range w: its pieces (0: there is none), its sequence's first
+// token and rows, its number.  Then per row of a slot (range, side, key head): {reference, sum,
+// sum of the rounded values}, and the accumulators.
 struct Partials {
   int4* joins;
   float4* stat;
@@ -180,15 +181,14 @@ __device__ __forceinline__ Partials partials(const CacheAttentionArgs& a, const 
   char* w = static_cast<char*>(a.workspace);
   Partials r;
   r.joins = reinterpret_cast<int4*>(w);
-  w += (int64_t)p.ranges * p.row_tiles * 16;
+  w += (int64_t)p.ranges * 16;
   r.stat = reinterpret_cast<float4*>(w);
-  w += (int64_t)p.ranges * 2 * a.c.H * p.row_tiles * p.tile_rows * 16;
+  w += (int64_t)p.ranges * 2 * a.c.H * p.tile_rows * 16;
   r.acc = reinterpret_cast<float*>(w);
   return r;
 }
-__device__ __forceinline__ int64_t partial_row(const CacheAttentionArgs& a, const CachePlan& p, int w, int side, int head,
-                                               int tile) {
-  return ((((int64_t)w * 2 + side) * a.c.H + head) * p.row_tiles + tile) * p.tile_rows;
+__device__ __forceinline__ int64_t partial_row(const CacheAttentionArgs& a, const CachePlan& p, int w, int side, int head) {
+  return (((int64_t)w * 2 + side) * a.c.H + head) * p.tile_rows;
 }
 
 // N consecutive values.
@@ -340,65 +340,64 @@ __device__ __forceinline__ void store_columns(const CacheAttentionArgs& a, const
   }
 }
 
-// Which range, key head and row tile a workgroup takes.  Row tiles of one (range, key
-// head) go to one XCD (workgroups are dealt round-robin to eight), which then reads the keys
-// once for all of them.
+// Which range and key head a workgroup takes.  Workgroups are dealt round-robin to eight XCDs;
+// neighbouring ranges of a key head go to one of them, whose L2 then holds the keys of a
+// sequence while its row tiles are at work.
 struct Place {
-  int w, head, tile;
+  int w, head;
 };
-__device__ __forceinline__ Place place_of(const CacheAttentionArgs& a, const CachePlan& plan) {
-  int item = blockIdx.x, tile = 0;
-  if (plan.row_tiles > 1) {
-    const int q = item / 8;
-    tile = q % plan.row_tiles;
-    item = q / plan.row_tiles * 8 + item % 8;
-  }
-  const int w = item / a.c.H;
-  return {w, item - w * a.c.H, tile};
+__device__ __forceinline__ Place place_of(const CachePlan& plan) {
+  const int item = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, head = item / plan.ranges;
+  return {item - head * plan.ranges, head};
 }
 
-// The workgroup's range, and (from one of its threads) the record for the sequence that
-// crosses into it for the first time.
+// The workgroup's range, and (from one of its threads) the record for the row tile that crosses
+// into it for the first time.
 __device__ __forceinline__ Range open_range(const CacheAttentionArgs& a, const CachePlan& plan, const Place& p) {
   Range range{};
   if (plan.split) {
-    range = find_range(a, plan, p.w, p.tile);
+    range = find_range(a, plan, p.w);
     if (p.head == 0 && threadIdx.x == 0) {
       int4 join = {0, 0, 0, 0};
       if (range.begin < range.end && range.begin > range.at && range.at >= range.begin - range.per)
-        join = int4{(range.at + range.units - 1) / range.per - p.w + 2, range.seq.first, range.seq.tokens * a.G, 0};
-      partials(a, plan).joins[p.tile * plan.ranges + p.w] = join;
+        join = int4{(range.at + range.units - 1) / range.per - p.w + 2, range.seq.first, range.seq.tokens * a.G, range.tile};
+      partials(a, plan).joins[p.w] = join;
     }
-  } else {
-    range.b = p.w;
-    range.seq = sequence(a, p.w);
-    range.units = range.end = units_of(a, plan, range.seq, p.tile);
+  } else {  // range w: row tile w % row_tiles of sequence w / row_tiles
+    range.b = p.w / plan.row_tiles;
+    range.tile = p.w - range.b * plan.row_tiles;
+    range.seq = sequence(a, range.b);
+    range.tiles = row_tiles_of(a, plan, range.seq);
+    range.units = units_of(range.seq);
+    range.end = range.tile < range.tiles ? range.units : 0;
   }
   return range;
 }
 
-// Goes on to the next sequence that has rows here, which begins at place `stop`; false at
-// the end of the range.
-__device__ __forceinline__ bool next_sequence(const CacheAttentionArgs& a, const CachePlan& plan, int tile, int stop,
-                                              Range& range) {
+// Goes on to the next row tile, which begins at place `stop`; false at the end of the range.
+__device__ __forceinline__ bool next_tile(const CacheAttentionArgs& a, const CachePlan& plan, int stop, Range& range) {
   if (stop >= range.end) return false;
-  do {
-    if (++range.b >= a.B) return false;
-    range.seq = sequence(a, range.b);
-    range.units = units_of(a, plan, range.seq, tile);
-  } while (range.units == 0);
+  if (++range.tile >= range.tiles) {
+    range.tile = 0;
+    do {
+      if (++range.b >= a.B) return false;
+      range.seq = sequence(a, range.b);
+      range.tiles = row_tiles_of(a, plan, range.seq);
+    } while (range.tiles == 0);
+    range.units = units_of(range.seq);
+  }
   range.at = stop + kSetup;
   return true;
 }
 
-// The range's part of its sequence: keys [begin, end) as rows row0 .. row0 + tile see them.
+// The range's part of its row tile: keys [begin, end).
 struct Part {
   int begin, end, stop;  // stop: place of the line where it ends
-  bool whole, first;     // the whole sequence; its first piece
+  bool whole, first;     // all keys of the row tile; its first piece
   int common;            // keys below are seen by every row of the tile
   int tree_tokens;       // new tokens that have a bit in the tree
 };
-__device__ __forceinline__ bool open_part(const CacheAttentionArgs& a, const CachePlan& plan, const Range& range, int tile,
+__device__ __forceinline__ bool open_part(const CacheAttentionArgs& a, const CachePlan& plan, const Range& range,
                                           Part* part) {
   const Sequence& seq = range.seq;
   const int from = range.begin > range.at ? range.begin : range.at, seq_end = range.at + range.units;
@@ -408,7 +407,7 @@ __device__ __forceinline__ bool open_part(const CacheAttentionArgs& a, const Cac
   part->whole = part->first && part->stop == seq_end;
   part->begin = (from - range.at) * kUnit;
   part->end = part->stop < seq_end ? (part->stop - range.at) * kUnit : seq.keys;
-  const int rows = seq.tokens * a.G, row0 = tile * plan.tile, row1 = row0 + plan.tile < rows ? row0 + plan.tile : rows;
+  const int rows = seq.tokens * a.G, row0 = range.tile * plan.tile, row1 = row0 + plan.tile < rows ? row0 + plan.tile : rows;
   if (a.tree) {
     part->common = seq.prefix;
   } else {  // causal: the first and the last row's token

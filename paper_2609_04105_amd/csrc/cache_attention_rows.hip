@@ -4,29 +4,42 @@
 // The same mathematics and operand orders as cache_attention.hip; what bounds it is another:
 // with 128 rows a key costs 128 * 4 D flop and 136 bytes (MXFP4, D 128), so the matrix unit and the
 // softmax's vector work do, and turning codes into bf16 must not be repeated by every wave.
-// The four waves of a workgroup take 32 rows each and walk the same keys; each 32-key tile is
-// turned into bf16 operands once, K by two waves and V by the other two, into LDS, in the order
-// in which every lane reads its own 16 bytes of a product's A operand (no bank conflicts, no
-// transposing).  Two buffers: a tile is converted while the one before is used, and loaded
-// while the one before that is; one barrier a tile.
+// The four waves of a workgroup take 32 rows each and walk the same keys; the codes of a step of 64
+// keys are turned into bf16 operands once, K by two waves and V by the other two, into LDS, in the
+// order in which every lane reads its own 16 bytes of a product's A operand (no bank conflicts,
+// no transposing).  The codes come by copies to LDS that hold no registers, sent one or two steps
+// ahead.  Two barriers a step; the second workgroup of a CU fills them.
 #include "cache_attention.hpp"
 
 namespace fp4attn {
 
 namespace {
 
-constexpr int kNr = 2;    // 16-row tiles of a wave
-constexpr int kRing = 4;  // tiles whose codes are in LDS or on the way
+constexpr int kNr = 2;                    // 16-row tiles of a wave
+constexpr int kTiles = 2;                 // 32-key tiles of a step
+constexpr int kKeys = kTiles * kTile;
+static_assert(kUnit % kKeys == 0, "a step that is cut short is the last of its sequence");
 static_assert(kRowsTile == 16 * kNr * kWaves, "rows of a workgroup");
 
-// Copies of 16 and 4 bytes a lane from memory to LDS bytes lds + 16 lane, lds + 4 lane.  Assembly, so
-// that the compiler counts neither the copies nor the LDS they write (it would wait for all of
-// them before every LDS read); the wave waits for its own with wait_copies.
-__device__ __forceinline__ void copy16(unsigned lds, const uint8_t* p) {
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(uniform((int)lds)) : "memory");
-}
-__device__ __forceinline__ void copy4(unsigned lds, const uint8_t* p) {
-  asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(uniform((int)lds)) : "memory");
+// Copies of 16 and 4 bytes a lane from memory to LDS bytes lds + 16 lane, lds + 4 lane, from base + off; all
+// lanes have one base, or (other != nullptr) the upper lanes another.  Assembly, so that the compiler
+// counts neither the copies nor the LDS they write (it would wait for all of them before every LDS
+// read); the wave waits for its own with wait_copies.  Nor does it look for hazards in there: a scalar
+// register that a vector instruction wrote must be five wait states old.
+template <int BYTES>
+__device__ __forceinline__ void copy(unsigned lds, const uint8_t* base, const uint8_t* other, bool upper, unsigned off) {
+  static_assert(BYTES == 16 || BYTES == 4, "sizes of the copy instructions");
+  const int to = uniform((int)lds);
+  if (other == nullptr) {  // uniform
+    const uint64_t u = (uint64_t)base;
+    const uint64_t s = ((uint64_t)(unsigned)uniform((int)(u >> 32)) << 32) | (unsigned)uniform((int)u);
+    if constexpr (BYTES == 16) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(s), "{m0}"(to) : "memory");
+    else asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(s), "{m0}"(to) : "memory");
+  } else {
+    const uint8_t* p = (upper ? other : base) + off;
+    if constexpr (BYTES == 16) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(to) : "memory");
+    else asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(to) : "memory");
+  }
 }
 template <int N>
 __device__ __forceinline__ void wait_copies() {  // until at most N vector memory operations are in flight
@@ -45,27 +58,24 @@ struct Share {
   static constexpr int kCopies = (kWords == 2 ? 2 : kWords / 4) + 1;
   static_assert(F::kVWords == 2 * F::kKWords, "half a V run is a K run");
 
-  static __device__ __forceinline__ void copy(unsigned lds, const CacheView& c, const Pages& pages, int key0, int head,
-                                              int wave, int lane) {
+  static __device__ __forceinline__ void fetch(unsigned lds, const CacheView& c, const Pages& pages, int key0, int head,
+                                               int wave, int lane) {
     asm volatile("" : "+v"(lane));  // offsets are formed here and not held through the loop
     const unsigned m = lane & 15, g = (unsigned)lane >> 4;
-    const bool is_k = wave < 2;
-    const int64_t row = base_row(c, pages, key0, head, is_k ? m >= 8 : g >= 2);
+    const bool is_k = wave < 2, two = c.page_shift == 4;
+    const uint8_t *codes = is_k ? c.k_codes : c.v_codes, *scales = is_k ? c.k_scales : c.v_scales;
+    const int64_t row = base_row(c, pages, key0, head, false), other = two ? base_row(c, pages, key0, head, true) : 0;
+    const uint8_t *b0 = codes + row * (4 * kBytes), *b1 = two ? codes + other * (4 * kBytes) : nullptr;
     const unsigned key = (m >> 2) * 8 + (m & 3) + 4 * wave;
-    const uint8_t* p = (is_k ? c.k_codes : c.v_codes) + row * (4 * kBytes) +
-                       (is_k ? key * (4 * kBytes) + g * kBytes : (unsigned)(lane * 2 + (wave - 2)) * kBytes);
-    if constexpr (kWords == 2) {
-      copy4(lds, p);
-      copy4(lds + 256, p + 4);
-    } else {
+    const unsigned off = is_k ? key * (4 * kBytes) + g * kBytes : (unsigned)(lane * 2 + (wave - 2)) * kBytes;
+    const bool upper = is_k ? m >= 8 : g >= 2;
+    constexpr int kStep = kWords == 2 ? 4 : 16;
 #pragma unroll
-      for (int i = 0; i < kWords / 4; ++i) copy16(lds + 1024 * i, p + 16 * i);
-    }
+    for (int i = 0; i < kBytes / kStep; ++i) copy<kStep>(lds + 64 * kStep * i, b0, b1, upper, off + kStep * i);
     // the scales of 32 keys lie together, 16 keys in a half (K by key, V by eight keys)
-    if (lane < kScaleBytes / 4) {
-      const int64_t half = base_row(c, pages, key0, head, lane >= kScaleBytes / 8);
-      copy4(lds + 64 * kBytes, (is_k ? c.k_scales : c.v_scales) + half * F::kBlocks + 4 * lane);
-    }
+    if (lane < kScaleBytes / 4)
+      copy<4>(lds + 64 * kBytes, scales + row * F::kBlocks, two ? scales + other * F::kBlocks : nullptr, lane >= kScaleBytes / 8,
+              4 * lane);
   }
 
   unsigned w[kWords];
@@ -92,26 +102,27 @@ struct Share {
 };
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kernel(const CacheAttentionArgs a, const CachePlan plan) {
+__global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const CacheAttentionArgs a, const CachePlan plan) {
   using F = Format<D, FP8>;
-  __shared__ v4i k_lds[2][2][F::kSteps][64];  // [buffer][half][step][lane]
-  __shared__ v4i v_lds[2][F::kDTiles][64];    // [buffer][product][lane]
   using Codes = Share<D, FP8>;
-  __shared__ __attribute__((aligned(16))) uint8_t code_lds[kRing][kWaves][Codes::kSize];
-  __shared__ unsigned huge_lds[2][2];         // [buffer][keys 0-3, 4-7 of eight]: a non-finite V block that some row sees
+  constexpr int kRing = FP8 && D == 128 ? 2 : 3;  // steps whose codes are in LDS or on the way (LDS for two workgroups)
+  __shared__ v4i k_lds[kTiles][2][F::kSteps][64];  // [tile][half][step of d][lane]
+  __shared__ v4i v_lds[kTiles][F::kDTiles][64];    // [tile][product][lane]
+  __shared__ __attribute__((aligned(16))) uint8_t code_lds[kRing][kTiles][kWaves][Codes::kSize];
+  __shared__ unsigned huge_lds[kTiles][2];  // [tile][keys 0-3, 4-7 of eight]: a non-finite V block that some row sees
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-  const Place place = place_of(a, plan);
+  const Place place = place_of(plan);
   const int head = place.head;
-  if (place.w >= plan.ranges) return;
+  if (head >= a.c.H) return;
   Range range = open_range(a, plan, place);
   if (range.begin >= range.end) return;
   const float factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
 
   Part part;
-  while (open_part(a, plan, range, place.tile, &part)) {
+  while (open_part(a, plan, range, &part)) {
     const Sequence seq = range.seq;
-    const int rows = seq.tokens * a.G, row0 = place.tile * kRowsTile + 16 * kNr * wave;
+    const int rows = seq.tokens * a.G, row0 = range.tile * kRowsTile + 16 * kNr * wave;
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
     int token[kNr];  // of the sequence
@@ -125,6 +136,11 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
 #pragma unroll
       for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
     }
+    // (waits for the queries here: the compiler would wait in the loop, and then for the copies too)
+#pragma unroll
+    for (int r = 0; r < kNr; ++r)
+#pragma unroll
+      for (int s = 0; s < F::kSteps; ++s) asm volatile("" : "+v"(q[r][s]));
     v4f acc[kNr][F::kDTiles];
     v4f sum16 = {0, 0, 0, 0};
     unsigned poisoned = 0;
@@ -137,10 +153,18 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
       sum[r] = 0.0f;
     }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
-    // The wave's codes of the tile at key0, in place `slot` of the ring, into buffer `buf`.
-    auto convert = [&](const Pages& pages, int key0, int slot, int buf) {
+    auto pages_of = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
+    auto fetch = [&](const Pages& p, int key, int slot, int tile) {
+      if (key < part.end)
+        Codes::fetch((unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)code_lds[slot][tile][wave], a.c, p,
+                     key, head, wave, lane);
+    };
+
+    // The wave's codes of tile `tile` of a step (keys from key0), in place `slot` of the ring, into
+    // operands.  Keys from part.end on are seen by no row.
+    auto convert = [&](const Pages& pages, int key0, int slot, int tile) {
       Codes raw;
-      raw.read(code_lds[slot][wave], wave, lane);
+      raw.read(code_lds[slot][tile][wave], wave, lane);
       if (wave < 2) {
         const float scale = scale_of(raw.scale);
         static_for<F::kSteps>([&](auto S_) {
@@ -150,7 +174,7 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
             constexpr int i = decltype(I_)::value;
             kk[i] = (int)code_pair<4 * st + i, FP8>(raw.w, scale);
           });
-          k_lds[buf][wave][st][lane] = kk;
+          k_lds[tile][wave][st][lane] = kk;
         });
         return;
       }
@@ -159,7 +183,7 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
       if (key0 + kTile > part.common || !page0 || !page1) {
         // Keys that no row sees hold anything: their V codes and scales become zero.  A
         // non-finite block of the others becomes zero too, and is looked for by the rows.
-        const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - (key0 + 8 * g)) >> (4 * half) : 0u;
+        const unsigned there = (g >= 2 ? page1 : page0) ? below(part.end - (key0 + 8 * g)) >> (4 * half) : 0u;
         bool huge = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -175,7 +199,7 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
           }
         }
         const bool any = __any(huge);
-        if (lane == 0) huge_lds[buf][half] = any;
+        if (lane == 0) huge_lds[tile][half] = any;
       }
       const unsigned sc[2] = {raw.scale, 0};
       float scale[4];
@@ -187,49 +211,64 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
           constexpr int j = decltype(J_)::value;
           x[j] = code_pair<j * (F::kDTiles / 2) + e, FP8>(raw.w, scale[j]);
         });
-        uint2* lo = reinterpret_cast<uint2*>(&v_lds[buf][2 * e][lane]) + half;
-        uint2* hi = reinterpret_cast<uint2*>(&v_lds[buf][2 * e + 1][lane]) + half;
+        uint2* lo = reinterpret_cast<uint2*>(&v_lds[tile][2 * e][lane]) + half;
+        uint2* hi = reinterpret_cast<uint2*>(&v_lds[tile][2 * e + 1][lane]) + half;
         *lo = uint2{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u)};
         *hi = uint2{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
       });
     };
 
-    auto attend = [&](const Pages& pages, int key0, int buf) {
-      const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
-      // S^T: register i of half h is key 8 g + 4 h + i
-      v4f s[kNr][2];
+    auto attend = [&](const Pages (&pages)[kTiles], int key0) {
+      // S^T: register i of half h of a tile is its key 8 g + 4 h + i
+      // (operands are read one half ahead of their products, and kept there)
+      v4f s[kNr][kTiles][2];
+      v4i kk[2 * kTiles][F::kSteps];
+      auto read_k = [&](int i) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+        for (int st = 0; st < F::kSteps; ++st) kk[i][st] = k_lds[i / 2][i % 2][st][lane];
+      };
+      read_k(0);
 #pragma unroll
-        for (int r = 0; r < kNr; ++r) s[r][h] = v4f{0, 0, 0, 0};
+      for (int i = 0; i < 2 * kTiles; ++i) {
+        if (i + 1 < 2 * kTiles) read_k(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int st = 0; st < F::kSteps; ++st) {
-          const v4i kk = k_lds[buf][h][st][lane];
+        for (int r = 0; r < kNr; ++r) s[r][i / 2][i % 2] = v4f{0, 0, 0, 0};
 #pragma unroll
-          for (int r = 0; r < kNr; ++r) s[r][h] = mfma_16x16x32(kk, q[r][st], s[r][h]);
-        }
+        for (int st = 0; st < F::kSteps; ++st)
+#pragma unroll
+          for (int r = 0; r < kNr; ++r) s[r][i / 2][i % 2] = mfma_16x16x32(kk[i][st], q[r][st], s[r][i / 2][i % 2]);
       }
-      if (key0 + kTile > part.common || !page0 || !page1) {
-        const int base = key0 + 8 * g;
-        const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - base) : 0u;
-        unsigned see[kNr];
+      bool all = key0 + kKeys <= part.common;
 #pragma unroll
-        for (int r = 0; r < kNr; ++r) {
-          see[r] = there & row_sees(a, seq, part, token[r], base);
+      for (int tile = 0; tile < kTiles; ++tile) all = all && is_page(a.c, pages[tile].p0) && is_page(a.c, pages[tile].p1);
+      if (!all) {  // uniform
 #pragma unroll
-          for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = see[r] >> j & 1 ? s[r][j / 4][j % 4] : -__builtin_inff();
-        }
-        if (huge_lds[buf][0] | huge_lds[buf][1]) {  // lane group g holds outputs of d block g (d = 64: g / 2)
+        for (int tile = 0; tile < kTiles; ++tile) {
+          const int first = key0 + kTile * tile, base = first + 8 * g;
+          const bool page0 = is_page(a.c, pages[tile].p0), page1 = is_page(a.c, pages[tile].p1);
+          const unsigned there = (g >= 2 ? page1 : page0) ? below(part.end - base) : 0u;
+          unsigned see[kNr];
 #pragma unroll
-          for (int r = 0; r < kNr; ++r) see[r] = groups_or(see[r] << (8 * g));
-          const int blk = g * F::kBlocks / 4;
-          for (int k = 0; k < kTile; ++k) {
-            const int page = k >= 16 ? pages.p1 : pages.p0, key = key0 + k;
-            if (!is_page(a.c, page) || key >= seq.keys) continue;
-            const int64_t group = row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
-            const bool big = a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] >= kHugeScale<FP8>;
+          for (int r = 0; r < kNr; ++r) {
+            see[r] = there & row_sees(a, seq, part, token[r], base);
 #pragma unroll
-            for (int r = 0; r < kNr; ++r) poisoned |= big ? (see[r] >> k & 1) << r : 0u;
+            for (int j = 0; j < 8; ++j)
+              s[r][tile][j / 4][j % 4] = see[r] >> j & 1 ? s[r][tile][j / 4][j % 4] : -__builtin_inff();
+          }
+          const bool looked = first + kTile > part.common || !page0 || !page1;  // as convert did
+          if (looked && (huge_lds[tile][0] | huge_lds[tile][1])) {  // lane group g holds outputs of d block g (d = 64: g / 2)
+#pragma unroll
+            for (int r = 0; r < kNr; ++r) see[r] = groups_or(see[r] << (8 * g));
+            const int blk = g * F::kBlocks / 4;
+            for (int k = 0; k < kTile; ++k) {
+              const int page = k >= 16 ? pages[tile].p1 : pages[tile].p0, key = first + k;
+              if (!is_page(a.c, page) || key >= part.end) continue;
+              const int64_t group = row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
+              const bool big = a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] >= kHugeScale<FP8>;
+#pragma unroll
+              for (int r = 0; r < kNr; ++r) poisoned |= big ? (see[r] >> k & 1) << r : 0u;
+            }
           }
         }
       }
@@ -237,7 +276,7 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
       bool rise = false;
 #pragma unroll
       for (int r = 0; r < kNr; ++r) {
-        top[r] = groups_max(max8(s[r])) * factor;
+        top[r] = groups_max(fmaxf(max8(s[r][0]), max8(s[r][1]))) * factor;
         rise |= top[r] > ref[r] + kLag;
       }
       if (__any(rise)) {
@@ -252,58 +291,68 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
           for (int t = 0; t < F::kDTiles; ++t) acc[r][t] *= down;
         }
       }
-      v4i p[kNr];
+      constexpr int kVAhead = 4;
+      v4i vv[kTiles * F::kDTiles];
 #pragma unroll
-      for (int r = 0; r < kNr; ++r) {
-        p[r] = probabilities(s[r], factor, ref[r], &sum[r]);
-        const int one = (lane & 3) == r ? 0x3f803f80 : 0;
-        sum16 = mfma_16x16x32(v4i{one, one, one, one}, p[r], sum16);
-      }
+      for (int i = 0; i < kVAhead; ++i) vv[i] = v_lds[0][i][lane];
+      v4i p[kNr][kTiles];
+#pragma unroll
+      for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+        for (int r = 0; r < kNr; ++r) {
+          p[r][tile] = probabilities(s[r][tile], factor, ref[r], &sum[r]);
+          const int one = (lane & 3) == r ? 0x3f803f80 : 0;
+          sum16 = mfma_16x16x32(v4i{one, one, one, one}, p[r][tile], sum16);
+        }
       // O^T: product t has rows d = D / 16 * m + t
 #pragma unroll
-      for (int t = 0; t < F::kDTiles; ++t) {
-        const v4i vv = v_lds[buf][t][lane];
+      for (int i = 0; i < kTiles * F::kDTiles; ++i) {
+        constexpr int n = kTiles * F::kDTiles;
+        if (i + kVAhead < n) vv[i + kVAhead] = v_lds[(i + kVAhead) / F::kDTiles][(i + kVAhead) % F::kDTiles][lane];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int r = 0; r < kNr; ++r) acc[r][t] = mfma_16x16x32(vv, p[r], acc[r][t]);
+        for (int r = 0; r < kNr; ++r)
+          acc[r][i % F::kDTiles] = mfma_16x16x32(vv[i], p[r][i / F::kDTiles], acc[r][i % F::kDTiles]);
       }
     };
 
-    // Tile i of the part: its codes are copied into place i % kRing of the ring from kRing tiles
-    // before, when the place's last tile has been converted by every wave, and converted one
-    // tile before.  pages[j]: of the tile j ahead.
-    int key0 = part.begin, buf = 0, slot = 0;
-    if (key0 < part.end) {
-      Pages pages[kRing + 1];
-      auto pages_at = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
-      auto copy = [&](const Pages& p, int key, int to) {
-        if (key < part.end) Codes::copy((unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)code_lds[to][wave], a.c, p, key, head, wave, lane);
-      };
+    // Step i: the codes of step i + kRing - 1 are sent for (their place in the ring was last read before the
+    // barrier), the step's own become operands, and after a barrier every wave uses them.
+    // pages[j][t]: of tile t of the step j ahead.
+    if (part.begin < part.end) {
+      Pages pages[kRing][kTiles];
 #pragma unroll
-      for (int j = 0; j <= kRing; ++j) pages[j] = pages_at(key0 + j * kTile);
+      for (int j = 0; j < kRing; ++j)
 #pragma unroll
-      for (int j = 0; j < kRing; ++j) copy(pages[j], key0 + j * kTile, j);
-      if (key0 + (kRing - 1) * kTile < part.end) wait_copies<(kRing - 1) * Codes::kCopies>();
-      else wait_copies<0>();
-      convert(pages[0], key0, 0, 0);
-      __syncthreads();
-      while (true) {
-        const int ahead = key0 + kTile;
-        const Pages after = pages_at(key0 + (kRing + 1) * kTile);
-        if (ahead < part.end) {
-          if (key0 + (kRing - 1) * kTile < part.end) wait_copies<(kRing - 2) * Codes::kCopies>();
-          else wait_copies<0>();
-          convert(pages[1], ahead, slot + 1 == kRing ? 0 : slot + 1, buf ^ 1);
-          copy(pages[kRing], key0 + kRing * kTile, slot);
-        }
-        if (row0 < rows) attend(pages[0], key0, buf);
-        if (ahead >= part.end) break;
+        for (int t = 0; t < kTiles; ++t) pages[j][t] = pages_of(part.begin + j * kKeys + t * kTile);
+#pragma unroll
+      for (int j = 0; j + 1 < kRing; ++j)
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) fetch(pages[j][t], part.begin + j * kKeys + t * kTile, j, t);
+      for (int key0 = part.begin, slot = 0;;) {
+        constexpr int kAhead = kRing - 1;
+        const int send = key0 + kAhead * kKeys, to = slot == 0 ? kRing - 1 : slot - 1;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) fetch(pages[kAhead][t], send + t * kTile, to, t);
+        if (send + kKeys <= part.end) wait_copies<kAhead * kTiles * Codes::kCopies>();
+        else wait_copies<0>();
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) convert(pages[0][t], key0 + t * kTile, slot, t);
+        Pages after[kTiles];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) after[t] = pages_of(key0 + kRing * kKeys + t * kTile);
         __syncthreads();
-        buf ^= 1;
+        if (row0 < rows) attend(pages[0], key0);
+        key0 += kKeys;
+        if (key0 >= part.end) break;
+        __syncthreads();
         slot = slot + 1 == kRing ? 0 : slot + 1;
-        key0 = ahead;
 #pragma unroll
-        for (int j = 0; j < kRing; ++j) pages[j] = pages[j + 1];
-        pages[kRing] = after;
+        for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+          for (int j = 0; j + 1 < kRing; ++j) pages[j][t] = pages[j + 1][t];
+          pages[kRing - 1][t] = after[t];
+        }
       }
     }
 
@@ -313,7 +362,7 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
       const int i = row0 + 16 * r + m;
       const float total = groups_sum(sum[r]);
       if (i >= rows) continue;
-      const int64_t piece = partial_row(a, plan, place.w, part.first ? 1 : 0, head, place.tile) + (16 * kNr * wave + 16 * r + m);
+      const int64_t piece = partial_row(a, plan, place.w, part.first ? 1 : 0, head) + (16 * kNr * wave + 16 * r + m);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float o[F::kDTiles];
@@ -323,7 +372,7 @@ __global__ __launch_bounds__(kThreads, rows_per_cu(D, FP8)) void cache_rows_kern
                               (poisoned >> r & 1) != 0, o);
       }
     }
-    if (!next_sequence(a, plan, place.tile, part.stop, range)) break;
+    if (!next_tile(a, plan, part.stop, range)) break;
     __syncthreads();
   }
 }

@@ -59,25 +59,24 @@ hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
 
 // How one attention call is cut up.  Rows (token, head of the group) of a sequence and
 // key head go to workgroups in tiles of 16, 32 (their waves split the keys) or 128 rows (their
-// waves split the rows).  With split, the keys of all sequences lie end to end in units of 128
-// (with a few places between sequences), and each of `ranges` workgroups per key head and row
-// tile takes an equal part of that line (fewer ranges if that leaves less than min_units
-// each); lengths are known on the device only.  Without, range b is sequence b.
+// waves split the rows).  With split, the row tiles of all sequences, each with its keys in
+// units of 128, lie end to end (with a few places between them), and each of `ranges` workgroups
+// per key head takes an equal part of that line (fewer ranges if that leaves less than
+// min_units each); lengths are known on the device only.  Without, a range is a row tile.
 struct CachePlan {
   int tile;       // rows of a row tile
   int row_tiles;  // of the longest sequence and one key head
   int tile_rows;  // rows of a tile that can be in use
   int split, ranges, min_units;
+  bool fits;           // the line's places and the workgroups are in range
   int64_t workgroups;  // of the first launch
   int64_t workspace;   // bytes
 };
-// cache_attention_rows.hip: rows of a workgroup, and workgroups of a CU (registers; LDS for MXFP8 and d = 128)
-constexpr int kRowsTile = 128;
-constexpr int rows_per_cu(int d, bool fp8) { return d == 128 && fp8 ? 2 : 3; }
+constexpr int kRowsTile = 128, kRowsPerCu = 2;  // cache_attention_rows.hip: rows of a workgroup, workgroups of a CU
 
 constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t max_keys);
+CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys);
 
 struct CacheAttentionArgs {
   CacheView c;
