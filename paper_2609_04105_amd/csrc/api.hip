@@ -232,6 +232,7 @@ fp4attn_status check_cache_sizes(const fp4attn_cache* c, fp4attn::CacheView* vie
   view->v_codes = c->v_codes;
   view->v_scales = c->v_scales;
   view->pages = c->pages;
+  view->page_limit = (int)(c->pages < 0x7fffffff ? c->pages : 0x7fffffff);
   view->H = (int)c->heads;
   view->d = (int)c->head_dim;
   view->fp8 = c->fp8;

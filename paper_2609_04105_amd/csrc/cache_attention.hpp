@@ -259,7 +259,7 @@ __device__ __forceinline__ Pages find_pages(const CacheAttentionArgs& a, ScalarI
   }
   return r;
 }
-__device__ __forceinline__ bool is_page(const CacheView& c, int p) { return (unsigned)p < (uint64_t)c.pages; }
+__device__ __forceinline__ bool is_page(const CacheView& c, int p) { return (unsigned)p < (unsigned)c.page_limit; }
 
 // Row (page, head, place); a missing page reads page 0.
 __device__ __forceinline__ int64_t row_of(const CacheView& c, int page, int head, int place) {

@@ -5,9 +5,8 @@
 // with 128 rows a key costs 128 * 4 D flop and 136 bytes (MXFP4, D 128), so the matrix unit and the
 // softmax's vector work do, and turning codes into bf16 must not be repeated by every wave.
 // The four waves of a workgroup take 32 rows each and walk the same keys; the codes of a step of 64
-// keys are turned into bf16 operands once, K by two waves and V by the other two, into LDS, in the
-// order in which every lane reads its own 16 bytes of a product's A operand (no bank conflicts,
-// no transposing).  The codes come by copies to LDS that hold no registers, sent one or two steps
+// keys are turned into bf16 operands once, a quarter by each wave, into LDS, in the order in which
+// every lane reads its own 16 bytes of a product's A operand (no bank conflicts, no transposing).  The codes come by copies to LDS that hold no registers, sent one or two steps
 // ahead.  Two barriers a step; the second workgroup of a CU fills them.
 #include "cache_attention.hpp"
 
@@ -18,28 +17,24 @@ namespace {
 constexpr int kNr = 2;                    // 16-row tiles of a wave
 constexpr int kTiles = 2;                 // 32-key tiles of a step
 constexpr int kKeys = kTiles * kTile;
-static_assert(kUnit % kKeys == 0, "a step that is cut short is the last of its sequence");
+static_assert(kTiles == kWaves / 2 && kUnit % kKeys == 0, "a step that is cut short is the last of its sequence");
 static_assert(kRowsTile == 16 * kNr * kWaves, "rows of a workgroup");
 
-// Copies of 16 and 4 bytes a lane from memory to LDS bytes lds + 16 lane, lds + 4 lane, from base + off; all
-// lanes have one base, or (other != nullptr) the upper lanes another.  Assembly, so that the compiler
-// counts neither the copies nor the LDS they write (it would wait for all of them before every LDS
-// read); the wave waits for its own with wait_copies.  Nor does it look for hazards in there: a scalar
-// register that a vector instruction wrote must be five wait states old.
+// Copies of 16 and 4 bytes a lane from memory to LDS bytes lds + 16 lane, lds + 4 lane: from base + off with
+// one base for the wave, or from the lane's p.  Assembly, so that the compiler counts neither the
+// copies nor the LDS they write (it would wait for all of them before every LDS read); the wave
+// waits for its own with wait_copies.  Nor does it look for hazards in there: a scalar register that
+// a vector instruction wrote must be five wait states old.
 template <int BYTES>
-__device__ __forceinline__ void copy(unsigned lds, const uint8_t* base, const uint8_t* other, bool upper, unsigned off) {
+__device__ __forceinline__ void copy(unsigned lds, const uint8_t* base, unsigned off) {
   static_assert(BYTES == 16 || BYTES == 4, "sizes of the copy instructions");
-  const int to = uniform((int)lds);
-  if (other == nullptr) {  // uniform
-    const uint64_t u = (uint64_t)base;
-    const uint64_t s = ((uint64_t)(unsigned)uniform((int)(u >> 32)) << 32) | (unsigned)uniform((int)u);
-    if constexpr (BYTES == 16) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(s), "{m0}"(to) : "memory");
-    else asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(s), "{m0}"(to) : "memory");
-  } else {
-    const uint8_t* p = (upper ? other : base) + off;
-    if constexpr (BYTES == 16) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(to) : "memory");
-    else asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(to) : "memory");
-  }
+  if constexpr (BYTES == 16) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+  else asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+template <int BYTES>
+__device__ __forceinline__ void copy(unsigned lds, const uint8_t* p) {
+  if constexpr (BYTES == 16) asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "{m0}"(lds) : "memory");
+  else asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, off" ::"v"(p), "{m0}"(lds) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_copies() {  // until at most N vector memory operations are in flight
@@ -47,40 +42,54 @@ __device__ __forceinline__ void wait_copies() {  // until at most N vector memor
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// A wave's share of a tile's codes, as it lies in LDS: of K (waves 0, 1: halves 0, 1) every lane a key's
-// D / 4 values, of V (waves 2, 3) four keys' D / 16 values; then the tile's K or V scales.
+// A wave's share of a step's codes, as it lies in LDS: of tile wave / 2, half h = wave % 2 of K (every lane a
+// key's D / 4 values) and keys 4 h .. 4 h + 3 of every eight of V (every lane D / 16 values of
+// each); then the tile's scales.
 template <int D, bool FP8>
 struct Share {
   using F = Format<D, FP8>;
-  static constexpr int kWords = F::kKWords, kBytes = 4 * kWords;  // of a lane
-  static constexpr int kScaleBytes = kTile * F::kBlocks;
-  static constexpr int kSize = 64 * kBytes + kScaleBytes;
-  static constexpr int kCopies = (kWords == 2 ? 2 : kWords / 4) + 1;
+  static constexpr int kWords = F::kKWords, kBytes = 4 * kWords;  // of a lane, for K and for V
+  static constexpr int kScaleBytes = kTile * F::kBlocks;          // of a tile's K; V as much
+  static constexpr int kV = 64 * kBytes, kScales = 2 * kV, kSize = kScales + 2 * kScaleBytes;
+  static constexpr int kStep = kWords == 2 ? 4 : 16;
+  static constexpr int kCopies = 2 * kBytes / kStep + 1;
   static_assert(F::kVWords == 2 * F::kKWords, "half a V run is a K run");
 
   static __device__ __forceinline__ void fetch(unsigned lds, const CacheView& c, const Pages& pages, int key0, int head,
-                                               int wave, int lane) {
+                                               int half, int lane) {
     asm volatile("" : "+v"(lane));  // offsets are formed here and not held through the loop
-    const unsigned m = lane & 15, g = (unsigned)lane >> 4;
-    const bool is_k = wave < 2, two = c.page_shift == 4;
-    const uint8_t *codes = is_k ? c.k_codes : c.v_codes, *scales = is_k ? c.k_scales : c.v_scales;
-    const int64_t row = base_row(c, pages, key0, head, false), other = two ? base_row(c, pages, key0, head, true) : 0;
-    const uint8_t *b0 = codes + row * (4 * kBytes), *b1 = two ? codes + other * (4 * kBytes) : nullptr;
-    const unsigned key = (m >> 2) * 8 + (m & 3) + 4 * wave;
-    const unsigned off = is_k ? key * (4 * kBytes) + g * kBytes : (unsigned)(lane * 2 + (wave - 2)) * kBytes;
-    const bool upper = is_k ? m >= 8 : g >= 2;
-    constexpr int kStep = kWords == 2 ? 4 : 16;
-#pragma unroll
-    for (int i = 0; i < kBytes / kStep; ++i) copy<kStep>(lds + 64 * kStep * i, b0, b1, upper, off + kStep * i);
+    const unsigned m = lane & 15, g = (unsigned)lane >> 4, key = (m >> 2) * 8 + (m & 3) + 4 * half;
+    const unsigned k_off = key * (4 * kBytes) + g * kBytes, v_off = (unsigned)(lane * 2 + half) * kBytes;
     // the scales of 32 keys lie together, 16 keys in a half (K by key, V by eight keys)
-    if (lane < kScaleBytes / 4)
-      copy<4>(lds + 64 * kBytes, scales + row * F::kBlocks, two ? scales + other * F::kBlocks : nullptr, lane >= kScaleBytes / 8,
-              4 * lane);
+    constexpr unsigned n = kScaleBytes / 4;
+    const bool of_v = (unsigned)lane >= n;
+    const unsigned word = of_v ? lane - n : lane;
+    const uint8_t* scales = of_v ? c.v_scales : c.k_scales;
+    const int64_t row = base_row(c, pages, key0, head, false);
+    if (c.page_shift != 4) {
+      const uint8_t *kb = c.k_codes + row * (4 * kBytes), *vb = c.v_codes + row * (4 * kBytes);
+#pragma unroll
+      for (int i = 0; i < kBytes / kStep; ++i) {
+        copy<kStep>(lds + 64 * kStep * i, kb, k_off + kStep * i);
+        copy<kStep>(lds + kV + 64 * kStep * i, vb, v_off + kStep * i);
+      }
+      if ((unsigned)lane < 2 * n) copy<4>(lds + kScales, scales + (row * F::kBlocks + 4 * word));
+    } else {
+      const int64_t other = base_row(c, pages, key0, head, true);
+      const uint8_t *kp = c.k_codes + ((m >= 8 ? other : row) * (4 * kBytes) + k_off);
+      const uint8_t *vp = c.v_codes + ((g >= 2 ? other : row) * (4 * kBytes) + v_off);
+#pragma unroll
+      for (int i = 0; i < kBytes / kStep; ++i) {
+        copy<kStep>(lds + 64 * kStep * i, kp + kStep * i);
+        copy<kStep>(lds + kV + 64 * kStep * i, vp + kStep * i);
+      }
+      if ((unsigned)lane < 2 * n) copy<4>(lds + kScales, scales + ((word >= n / 2 ? other : row) * F::kBlocks + 4 * word));
+    }
   }
 
-  unsigned w[kWords];
-  unsigned scale;  // K: an E8M0 byte; V: four
-  __device__ __forceinline__ void read(const uint8_t* lds, int wave, int lane) {
+  unsigned k[kWords], v[kWords];
+  unsigned k_scale, v_scales;  // an E8M0 byte; four
+  static __device__ __forceinline__ void read_words(const uint8_t* lds, int lane, unsigned (&w)[kWords]) {
     if constexpr (kWords == 2) {
       w[0] = reinterpret_cast<const unsigned*>(lds)[lane];
       w[1] = reinterpret_cast<const unsigned*>(lds + 256)[lane];
@@ -94,10 +103,13 @@ struct Share {
         w[4 * i + 3] = x.w;
       }
     }
+  }
+  __device__ __forceinline__ void read(const uint8_t* lds, int half, int lane) {
+    read_words(lds, lane, k);
+    read_words(lds + kV, lane, v);
     const unsigned m = lane & 15, g = (unsigned)lane >> 4;
-    const uint8_t* sc = lds + 64 * kBytes;
-    if (wave < 2) scale = sc[((m >> 2) * 8 + (m & 3) + 4 * wave) * F::kBlocks + g * F::kBlocks / 4];
-    else scale = *reinterpret_cast<const unsigned*>(sc + (g * F::kBlocks + m * F::kBlocks / 16) * 8 + 4 * (wave - 2));
+    k_scale = lds[kScales + ((m >> 2) * 8 + (m & 3) + 4 * half) * F::kBlocks + g * F::kBlocks / 4];
+    v_scales = *reinterpret_cast<const unsigned*>(lds + kScales + kScaleBytes + (g * F::kBlocks + m * F::kBlocks / 16) * 8 + 4 * half);
   }
 };
 
@@ -107,8 +119,8 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
   using Codes = Share<D, FP8>;
   constexpr int kRing = FP8 && D == 128 ? 2 : 3;  // steps whose codes are in LDS or on the way (LDS for two workgroups)
   __shared__ v4i k_lds[kTiles][2][F::kSteps][64];  // [tile][half][step of d][lane]
-  __shared__ v4i v_lds[kTiles][F::kDTiles][64];    // [tile][product][lane]
-  __shared__ __attribute__((aligned(16))) uint8_t code_lds[kRing][kTiles][kWaves][Codes::kSize];
+  __shared__ uint2 v_lds[kTiles][F::kDTiles][2][64];  // [tile][product][keys 0-3, 4-7 of eight][lane]
+  __shared__ __attribute__((aligned(16))) uint8_t code_lds[kRing][kWaves][Codes::kSize];
   __shared__ unsigned huge_lds[kTiles][2];  // [tile][keys 0-3, 4-7 of eight]: a non-finite V block that some row sees
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -154,31 +166,29 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
     }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
     auto pages_of = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
-    auto fetch = [&](const Pages& p, int key, int slot, int tile) {
+    // the wave's tile of every step and its halves there
+    const int my_tile = wave / 2, half = wave % 2;
+    auto fetch = [&](const Pages& p, int key, int slot) {
       if (key < part.end)
-        Codes::fetch((unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)code_lds[slot][tile][wave], a.c, p,
-                     key, head, wave, lane);
+        Codes::fetch((unsigned)(uintptr_t)(const __attribute__((address_space(3))) uint8_t*)code_lds[slot][wave], a.c, p, key, head,
+                     half, lane);
     };
 
-    // The wave's codes of tile `tile` of a step (keys from key0), in place `slot` of the ring, into
-    // operands.  Keys from part.end on are seen by no row.
-    auto convert = [&](const Pages& pages, int key0, int slot, int tile) {
+    // The wave's codes of its tile (keys from key0), in place `slot` of the ring, into operands.  Keys from
+    // part.end on are seen by no row.
+    auto convert = [&](const Pages& pages, int key0, int slot) {
       Codes raw;
-      raw.read(code_lds[slot][tile][wave], wave, lane);
-      if (wave < 2) {
-        const float scale = scale_of(raw.scale);
-        static_for<F::kSteps>([&](auto S_) {
-          constexpr int st = decltype(S_)::value;
-          v4i kk;
-          static_for<4>([&](auto I_) {
-            constexpr int i = decltype(I_)::value;
-            kk[i] = (int)code_pair<4 * st + i, FP8>(raw.w, scale);
-          });
-          k_lds[tile][wave][st][lane] = kk;
+      raw.read(code_lds[slot][wave], half, lane);
+      const float k_scale = scale_of(raw.k_scale);
+      static_for<F::kSteps>([&](auto S_) {
+        constexpr int st = decltype(S_)::value;
+        v4i kk;
+        static_for<4>([&](auto I_) {
+          constexpr int i = decltype(I_)::value;
+          kk[i] = (int)code_pair<4 * st + i, FP8>(raw.k, k_scale);
         });
-        return;
-      }
-      const int half = wave - 2;
+        k_lds[my_tile][half][st][lane] = kk;
+      });
       const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
       if (key0 + kTile > part.common || !page0 || !page1) {
         // Keys that no row sees hold anything: their V codes and scales become zero.  A
@@ -187,21 +197,21 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         bool huge = false;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const bool in = there >> j & 1, big = (raw.scale >> (8 * j) & 255u) >= kHugeScale<FP8>;
+          const bool in = there >> j & 1, big = (raw.v_scales >> (8 * j) & 255u) >= kHugeScale<FP8>;
           huge |= in && big;
           const unsigned keep = in && !big ? ~0u : 0u;
-          raw.scale &= keep | ~(255u << (8 * j));
+          raw.v_scales &= keep | ~(255u << (8 * j));
           if constexpr (raw.kWords >= 4) {
 #pragma unroll
-            for (int i = 0; i < raw.kWords / 4; ++i) raw.w[j * (raw.kWords / 4) + i] &= keep;
+            for (int i = 0; i < raw.kWords / 4; ++i) raw.v[j * (raw.kWords / 4) + i] &= keep;
           } else {
-            raw.w[j / 2] &= keep | (j % 2 ? 0x0000ffffu : 0xffff0000u);
+            raw.v[j / 2] &= keep | (j % 2 ? 0x0000ffffu : 0xffff0000u);
           }
         }
         const bool any = __any(huge);
-        if (lane == 0) huge_lds[tile][half] = any;
+        if (lane == 0) huge_lds[my_tile][half] = any;
       }
-      const unsigned sc[2] = {raw.scale, 0};
+      const unsigned sc[2] = {raw.v_scales, 0};
       float scale[4];
       static_for<4>([&](auto J_) { scale[decltype(J_)::value] = scale_of_key<decltype(J_)::value>(sc); });
       static_for<F::kDTiles / 2>([&](auto E_) {
@@ -209,13 +219,17 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         unsigned x[4];
         static_for<4>([&](auto J_) {
           constexpr int j = decltype(J_)::value;
-          x[j] = code_pair<j * (F::kDTiles / 2) + e, FP8>(raw.w, scale[j]);
+          x[j] = code_pair<j * (F::kDTiles / 2) + e, FP8>(raw.v, scale[j]);
         });
-        uint2* lo = reinterpret_cast<uint2*>(&v_lds[tile][2 * e][lane]) + half;
-        uint2* hi = reinterpret_cast<uint2*>(&v_lds[tile][2 * e + 1][lane]) + half;
-        *lo = uint2{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u)};
-        *hi = uint2{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
+        v_lds[my_tile][2 * e][half][lane] =
+            uint2{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u)};
+        v_lds[my_tile][2 * e + 1][half][lane] =
+            uint2{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
       });
+    };
+    auto read_v = [&](int i) {
+      const uint2 lo = v_lds[i / F::kDTiles][i % F::kDTiles][0][lane], hi = v_lds[i / F::kDTiles][i % F::kDTiles][1][lane];
+      return v4i{(int)lo.x, (int)lo.y, (int)hi.x, (int)hi.y};
     };
 
     auto attend = [&](const Pages (&pages)[kTiles], int key0) {
@@ -294,7 +308,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       constexpr int kVAhead = 4;
       v4i vv[kTiles * F::kDTiles];
 #pragma unroll
-      for (int i = 0; i < kVAhead; ++i) vv[i] = v_lds[0][i][lane];
+      for (int i = 0; i < kVAhead; ++i) vv[i] = read_v(i);
       v4i p[kNr][kTiles];
 #pragma unroll
       for (int tile = 0; tile < kTiles; ++tile)
@@ -308,7 +322,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
       for (int i = 0; i < kTiles * F::kDTiles; ++i) {
         constexpr int n = kTiles * F::kDTiles;
-        if (i + kVAhead < n) vv[i + kVAhead] = v_lds[(i + kVAhead) / F::kDTiles][(i + kVAhead) % F::kDTiles][lane];
+        if (i + kVAhead < n) vv[i + kVAhead] = read_v(i + kVAhead);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int r = 0; r < kNr; ++r)
@@ -318,41 +332,32 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 
     // Step i: the codes of step i + kRing - 1 are sent for (their place in the ring was last read before the
     // barrier), the step's own become operands, and after a barrier every wave uses them.
-    // pages[j][t]: of tile t of the step j ahead.
     if (part.begin < part.end) {
-      Pages pages[kRing][kTiles];
+      constexpr int kAhead = kRing - 1;
+      const int mine = my_tile * kTile;  // the wave's tile in a step
 #pragma unroll
-      for (int j = 0; j < kRing; ++j)
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) pages[j][t] = pages_of(part.begin + j * kKeys + t * kTile);
-#pragma unroll
-      for (int j = 0; j + 1 < kRing; ++j)
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) fetch(pages[j][t], part.begin + j * kKeys + t * kTile, j, t);
+      for (int j = 0; j < kAhead; ++j) {
+        const int key = part.begin + j * kKeys + mine;
+        fetch(pages_of(key), key, j);
+      }
+      Pages send = pages_of(part.begin + kAhead * kKeys + mine);  // of the step to send for
       for (int key0 = part.begin, slot = 0;;) {
-        constexpr int kAhead = kRing - 1;
-        const int send = key0 + kAhead * kKeys, to = slot == 0 ? kRing - 1 : slot - 1;
+        const int ahead = key0 + kAhead * kKeys;
+        Pages pages[kTiles];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) fetch(pages[kAhead][t], send + t * kTile, to, t);
-        if (send + kKeys <= part.end) wait_copies<kAhead * kTiles * Codes::kCopies>();
+        for (int t = 0; t < kTiles; ++t) pages[t] = pages_of(key0 + t * kTile);
+        const Pages next = pages_of(ahead + kKeys + mine);
+        fetch(send, ahead + mine, slot == 0 ? kRing - 1 : slot - 1);
+        send = next;
+        if (ahead + kKeys <= part.end) wait_copies<kAhead * Codes::kCopies>();
         else wait_copies<0>();
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) convert(pages[0][t], key0 + t * kTile, slot, t);
-        Pages after[kTiles];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) after[t] = pages_of(key0 + kRing * kKeys + t * kTile);
+        convert(my_tile == 0 ? pages[0] : pages[1], key0 + mine, slot);
         __syncthreads();
-        if (row0 < rows) attend(pages[0], key0);
+        if (row0 < rows) attend(pages, key0);
         key0 += kKeys;
         if (key0 >= part.end) break;
         __syncthreads();
         slot = slot + 1 == kRing ? 0 : slot + 1;
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-#pragma unroll
-          for (int j = 0; j + 1 < kRing; ++j) pages[j][t] = pages[j + 1][t];
-          pages[kRing - 1][t] = after[t];
-        }
       }
     }
 

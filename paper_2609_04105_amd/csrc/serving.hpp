@@ -33,6 +33,7 @@ struct CacheView {
   uint8_t* v_codes;
   uint8_t* v_scales;
   int64_t pages;
+  int page_limit;  // page numbers below it (they are 32-bit in a page table) are in the cache
   int H, d, page_shift, fp8;
 };
 
