@@ -277,10 +277,10 @@ __device__ __forceinline__ int64_t base_row(const CacheView& c, const Pages& pag
 // The E8M0 byte as the converter's scale operand: a float's exponent field.
 __device__ __forceinline__ float scale_of(unsigned byte) { return as_float(byte << 23); }
 template <int J>
-__device__ __forceinline__ float scale_of_key(const unsigned (&vs)[2]) {
+__device__ __forceinline__ float scale_of_key(const unsigned (&vs)[2]) {  // byte J of the two words
   const unsigned w = vs[J / 4];
-  constexpr int j = J % 4;
-  return as_float((j == 3 ? w >> 1 : w << (23 - 8 * j)) & 0x7f800000u);
+  if constexpr (J % 4 == 3) return as_float(w >> 1 & 0x7f800000u);
+  else return as_float(w << (23 - 8 * (J % 4)) & 0x7f800000u);
 }
 
 // Pair I (values 2 I, 2 I + 1) of packed codes as two bf16.

@@ -174,11 +174,8 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
                      half, lane);
     };
 
-    // The wave's codes of its tile (keys from key0), in place `slot` of the ring, into operands.  Keys from
-    // part.end on are seen by no row.
-    auto convert = [&](const Pages& pages, int key0, int slot) {
-      Codes raw;
-      raw.read(code_lds[slot][wave], half, lane);
+    // The codes of the wave's tile (keys from key0) into operands.  Keys from part.end on are seen by no row.
+    auto convert = [&](Codes& raw, const Pages& pages, int key0) {
       const float k_scale = scale_of(raw.k_scale);
       static_for<F::kSteps>([&](auto S_) {
         constexpr int st = decltype(S_)::value;
@@ -201,9 +198,9 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
           huge |= in && big;
           const unsigned keep = in && !big ? ~0u : 0u;
           raw.v_scales &= keep | ~(255u << (8 * j));
-          if constexpr (raw.kWords >= 4) {
+          if constexpr (Codes::kWords >= 4) {
 #pragma unroll
-            for (int i = 0; i < raw.kWords / 4; ++i) raw.v[j * (raw.kWords / 4) + i] &= keep;
+            for (int i = 0; i < Codes::kWords / 4; ++i) raw.v[j * (Codes::kWords / 4) + i] &= keep;
           } else {
             raw.v[j / 2] &= keep | (j % 2 ? 0x0000ffffu : 0xffff0000u);
           }
@@ -330,17 +327,26 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       }
     };
 
-    // Step i: the codes of step i + kRing - 1 are sent for (their place in the ring was last read before the
-    // barrier), the step's own become operands, and after a barrier every wave uses them.
+    // Step i: the codes of step i + kRing - 1 are sent for (their place in the ring was read before the last
+    // barrier), the step's own become operands, and after a barrier every wave uses them and reads
+    // its codes of the next step.
     if (part.begin < part.end) {
       constexpr int kAhead = kRing - 1;
       const int mine = my_tile * kTile;  // the wave's tile in a step
+      Codes raw;
+      // the codes of the step at `key`, the first of those on the way
+      auto take = [&](int key, int slot) {
+        if (key + kAhead * kKeys <= part.end) wait_copies<(kAhead - 1) * Codes::kCopies>();
+        else wait_copies<0>();
+        raw.read(code_lds[slot][wave], half, lane);
+      };
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         const int key = part.begin + j * kKeys + mine;
         fetch(pages_of(key), key, j);
       }
       Pages send = pages_of(part.begin + kAhead * kKeys + mine);  // of the step to send for
+      take(part.begin, 0);
       for (int key0 = part.begin, slot = 0;;) {
         const int ahead = key0 + kAhead * kKeys;
         Pages pages[kTiles];
@@ -349,15 +355,14 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         const Pages next = pages_of(ahead + kKeys + mine);
         fetch(send, ahead + mine, slot == 0 ? kRing - 1 : slot - 1);
         send = next;
-        if (ahead + kKeys <= part.end) wait_copies<kAhead * Codes::kCopies>();
-        else wait_copies<0>();
-        convert(my_tile == 0 ? pages[0] : pages[1], key0 + mine, slot);
+        convert(raw, my_tile == 0 ? pages[0] : pages[1], key0 + mine);
         __syncthreads();
         if (row0 < rows) attend(pages, key0);
         key0 += kKeys;
         if (key0 >= part.end) break;
-        __syncthreads();
         slot = slot + 1 == kRing ? 0 : slot + 1;
+        take(key0, slot);
+        __syncthreads();
       }
     }
 
