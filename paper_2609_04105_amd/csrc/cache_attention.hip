@@ -145,13 +145,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       for (int s = 0; s < F::kSteps; ++s) asm volatile("" : "+v"(q[0][s]));
     }
     v4f acc[NR][F::kDTiles];
-    v4f sum16 = {0, 0, 0, 0};  // register r: the rounded probabilities of row tile r
+    v4f sum16[NR];  // the rounded probabilities (the same in all four)
     unsigned poisoned = 0;     // bit r: this lane's columns of row r see a non-finite V block
     float ref[NR], sum[NR];    // base 2, lags the maximum by at most kLag; this lane's own keys
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
 #pragma unroll
       for (int t = 0; t < F::kDTiles; ++t) acc[r][t] = v4f{0, 0, 0, 0};
+      sum16[r] = v4f{0, 0, 0, 0};
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
     }
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
         if (__any(rise)) {
 #pragma unroll
           for (int r = 0; r < NR; ++r) {
-            const float now = fmaxf(ref[r], top[r]);
+            const float now = top[r] > ref[r] + kLag ? top[r] : ref[r];  // (a row moves by its own keys alone)
             const float down = now == ref[r] ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);
             ref[r] = now;
             sum[r] *= down;
@@ -255,9 +256,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
           p[r] = probabilities(s[r], factor, ref[r], &sum[r]);
-          // ones in the rows r, r + 4, r + 8, r + 12 of A: register r of every lane group
-          const int one = (lane & 3) == r ? 0x3f803f80 : 0;
-          sum16 = mfma_16x16x32(v4i{one, one, one, one}, p[r], sum16);
+          sum16[r] = mfma_16x16x32(v4i{kOnes, kOnes, kOnes, kOnes}, p[r], sum16[r]);
         }
         // O^T: product t takes value t of every lane's part, rows d = D / 16 * m + t
         float vscale[8];
@@ -300,7 +299,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 #pragma unroll
       for (int t = 0; t < F::kDTiles; ++t)
         lds[(wave * F::kDTiles + t) * 64 + m * 4 + g] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
-      if (g == 0) lds_stat[wave][m] = float4{ref[r], total, sum16[r], 0.0f};
+      if (g == 0) lds_stat[wave][m] = float4{ref[r], total, sum16[r][0], 0.0f};
       lds_poison[wave][m * 4 + g] = poisoned >> r & 1;
       __syncthreads();
       join_waves<D, FP8>(a, plan, seq, reinterpret_cast<const float*>(lds), &lds_stat[0][row].x,

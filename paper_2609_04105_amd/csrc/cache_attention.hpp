@@ -50,6 +50,8 @@ __device__ __forceinline__ float max8(const v4f (&s)[2]) {
   return fmaxf(x, s[1][3]);
 }
 
+constexpr int kOnes = 0x3f803f80;  // two bf16
+
 // The bf16 probabilities 2^(s factor - ref) of a lane's eight scores; *sum grows by the
 // unrounded ones.
 __device__ __forceinline__ v4i probabilities(const v4f (&s)[2], float factor, float ref, float* sum) {
@@ -208,7 +210,13 @@ __device__ __forceinline__ void store_row(uint16_t* p, const float (&v)[N]) {
   else *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
 }
 
-__device__ __forceinline__ bool is_zero(float x) { return (as_uint(x) << 1) == 0u; }
+// Of +0 and -0 only.  (The empty asm keeps it a test of bits: as a comparison of floats the compiler,
+// told that there are no NaNs, may choose one that holds for them.)
+__device__ __forceinline__ bool is_zero(float x) {
+  unsigned bits = as_uint(x);
+  asm("" : "+v"(bits));
+  return (bits << 1) == 0u;
+}
 
 // The log normaliser in nats from a base-2 reference and sum.
 __device__ __forceinline__ float log_norm(float ref, float sum) {

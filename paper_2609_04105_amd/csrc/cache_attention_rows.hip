@@ -154,13 +154,14 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
       for (int s = 0; s < F::kSteps; ++s) asm volatile("" : "+v"(q[r][s]));
     v4f acc[kNr][F::kDTiles];
-    v4f sum16 = {0, 0, 0, 0};
+    v4f sum16[kNr];
     unsigned poisoned = 0;
     float ref[kNr], sum[kNr];
 #pragma unroll
     for (int r = 0; r < kNr; ++r) {
 #pragma unroll
       for (int t = 0; t < F::kDTiles; ++t) acc[r][t] = v4f{0, 0, 0, 0};
+      sum16[r] = v4f{0, 0, 0, 0};
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
     }
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       if (__any(rise)) {
 #pragma unroll
         for (int r = 0; r < kNr; ++r) {
-          const float now = fmaxf(ref[r], top[r]);
+          const float now = top[r] > ref[r] + kLag ? top[r] : ref[r];  // (a row moves by its own keys alone)
           const float down = now == ref[r] ? 1.0f : __builtin_amdgcn_exp2f(ref[r] - now);
           ref[r] = now;
           sum[r] *= down;
@@ -312,8 +313,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
         for (int r = 0; r < kNr; ++r) {
           p[r][tile] = probabilities(s[r][tile], factor, ref[r], &sum[r]);
-          const int one = (lane & 3) == r ? 0x3f803f80 : 0;
-          sum16 = mfma_16x16x32(v4i{one, one, one, one}, p[r][tile], sum16);
+          sum16[r] = mfma_16x16x32(v4i{kOnes, kOnes, kOnes, kOnes}, p[r][tile], sum16[r]);
         }
       // O^T: product t has rows d = D / 16 * m + t
 #pragma unroll
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         float o[F::kDTiles];
 #pragma unroll
         for (int t = 0; t < F::kDTiles; ++t) o[t] = acc[r][t][j];
-        store_columns<D, FP8>(a, plan, seq, i, head, 4 * g + j, part.whole, piece, ref[r], total, sum16[r],
+        store_columns<D, FP8>(a, plan, seq, i, head, 4 * g + j, part.whole, piece, ref[r], total, sum16[r][0],
                               (poisoned >> r & 1) != 0, o);
       }
     }

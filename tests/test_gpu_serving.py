@@ -497,6 +497,84 @@ def test_rows_of_no_sequence_stay(fa):
     assert bool((out[:2] == 7).all()) and torch.equal(out[2:5], want[:3].to(dtype))
 
 
+def _beside_idle(b, tiles, width):
+    """The batch with enough idle sequences behind it that `tiles` row tiles are exceeded, and a page table
+    for `width` keys."""
+    idle = -(-tiles // b.H)
+    b.keys, b.new = list(b.keys) + [0] * idle, list(b.new) + [0] * idle
+    b.slots += [np.zeros(0, dtype=np.int64)] * idle
+    table = np.full((len(b.keys), max(-(-width // b.page), b.table.shape[1])), -7, dtype=np.int32)
+    table[:b.table.shape[0], :b.table.shape[1]] = b.table
+    b.table = table
+    b.starts = np.concatenate((b.starts, np.full(idle, b.starts[-1]))).astype(np.int32)
+    return b
+
+
+@pytest.mark.parametrize("width", [1, 6000])
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("new,keys,H,G,page", [([1, 1, 1], [77, 0, 1300], 2, 33, 16), ([70, 0, 65], [150, 90, 65], 1, 2, 64),
+                                               ([130, 3], [1000, 3], 1, 3, 32), ([16], [1990], 3, 8, 128)])
+def test_many_row_tiles(fa, d, fp8, new, keys, H, G, page, width):
+    """More than 32 rows in a batch that fills the chip with row tiles, causal and with trees, with
+    short page tables and with long ones."""
+    b = _beside_idle(Batch(keys, new, H, G, d, fp8, page, seed=sum(new)), 256, width)
+    lse = torch.empty((sum(new), H * G), device="cuda")
+    b.check(b.call(fa, lse=lse), lse)
+    b.check(b.call(fa, out_dtype=torch.bfloat16))
+    tree = _tree(b.new, 3, sum(new))
+    b.check(b.call(fa, tree=tree, lse=lse), lse, tree=tree)
+
+
+@pytest.mark.parametrize("width", [1, 6000])
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,idle", [(2, 0), (5, 0), (20, 0), (20, 256)])
+def test_hidden_and_missing_in_every_tiling(fa, d, fp8, G, idle, width):
+    """NaN keys, NaN and overflowing value blocks that some drafted tokens see, and a page outside the
+    cache, in row tiles of every size."""
+    b = Batch([190], [6], 2, G, d, fp8, 16, seed=9)
+    if idle or width > 1:
+        _beside_idle(b, idle, width)
+    prefix = 184
+    tree = np.array([0b1, 0b11, 0b101, 0b1000, 0b10001, 0b100000], dtype=np.int64)
+    clean = b.call(fa, tree=tree)
+    b.check(clean, tree=tree)
+
+    def at(token):
+        return divmod(int(b.slots[0][prefix + token]), 16)
+
+    p, off = at(1)
+    b.cache[3][p, 0, off // 8, 1, off % 8] = 255
+    p, off = at(3)
+    b.cache[1][p, 1, off, 0] = 255
+    p, off = at(4)
+    b.cache[3][p, 1, off // 8, 0, off % 8] = 254
+    lse = torch.empty((6, 2 * G), device="cuda")
+    out = b.call(fa, tree=tree, lse=lse)
+    bad = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    bad[1, :G, 32:64] = True
+    bad[3, G:] = True
+    bad[4, G:, :32] = True
+    assert torch.equal(~torch.isfinite(out), bad)
+    nan = torch.zeros(lse.shape, dtype=torch.bool, device="cuda")
+    nan[3, G:] = True   # (values are not in the normaliser)
+    assert torch.equal(torch.isnan(lse), nan) and bool(torch.isfinite(lse[~nan]).all())
+    assert torch.equal(out[~bad], clean[~bad])
+    # the page of keys 48 .. 63 is missing; the bad tokens are still seen
+    real = b.table[0, 3]
+    b.table[0, 3] = 10 ** 6
+    out = b.call(fa, tree=tree)
+    assert torch.equal(~torch.isfinite(out), bad)
+    k, v = serving.key_values(b.cache, b.slots[0], fp8)
+    see = serving.tree_mask(tree.reshape(6, 1).view(np.uint64), 6, 190, 190) & (np.arange(190) // 16 != 3)
+    rows = np.array([0, 2, 5])
+    o, _, spread, size, reach = serving.attention(_f64(b.q[rows]), k, np.nan_to_num(v, posinf=0.0, neginf=0.0), see[rows], b.scale)
+    e = 2 * ((d + 4) * U * reach + (190 + 64) * 2 * U + 4 * U)
+    tol = 2.0 ** -8 * (1 + 2.0 ** -7) * spread + e[..., None] * size + U * np.abs(o)
+    assert np.all(np.abs(_f64(out[rows]) - o) <= tol)
+    b.table[0, 3] = real
+    assert torch.equal(b.call(fa, tree=tree)[~bad], clean[~bad])
+
+
 @pytest.mark.parametrize("split", [False, True])
 def test_long_cache_offsets(fa, split):
     """Pages whose bytes lie past 2^32 of the cache."""
