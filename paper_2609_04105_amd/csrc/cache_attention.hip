@@ -65,8 +65,10 @@ struct Tile {
   }
 };
 
-// Waves per SIMD that the registers are kept to.
-constexpr int waves_per_simd(int d, int nr) { return nr == 1 || d == 64 ? 3 : 2; }
+// Waves per SIMD that the registers are kept to.  (Two tiles in flight instead of one, at 2 .. 3 waves:
+// within 3 % either way for d = 128, and four waves of d = 64 are faster, 126 us against 130 for 64
+// sequences of 16384 keys and 8 key heads; at three waves 140.)
+constexpr int waves_per_simd(int d, int nr) { return 6 - d / 64 - nr; }
 
 // Joins the waves' results of row i and columns D / 16 * c ..  lds: [wave][product][row, 4 g + i];
 // stat: the row's {reference, sum, sum of the rounded values} of the first wave, 16 rows apart; poison:
@@ -389,13 +391,23 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
 
 CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys) {
   CachePlan p{};
-  const int64_t rows = max_q * G;
-  p.tile = rows <= 16 ? 16 : (rows <= 32 ? 32 : kRowsTile);
-  const int64_t row_tiles = (rows + p.tile - 1) / p.tile, units = (max_keys + kUnit - 1) / kUnit;
+  const int64_t rows = max_q * G, units = (max_keys + kUnit - 1) / kUnit;
+  auto tiles_of = [&](int64_t tile) { return (rows + tile - 1) / tile; };
+  // Rows of a tile.  Up to 16 rows the matrix products have one column tile of them.  More: the 128-row
+  // kernel converts a key's codes once for 128 rows, the other once for 32, but it needs a workgroup
+  // of 128 rows for every CU.  d = 128, MXFP4, 8 key heads of 8 query heads, us at tile 32 / 128:
+  //   32 sequences, 64 tokens (512 workgroups of 128 rows), 2048 keys 188 / 162, 16 tokens (256), 8192 keys 214 / 175;
+  //   8 sequences, 32 tokens of 4 heads (64), 8192 keys 61 / 64, 1 sequence, 64 tokens of 4 heads (16), 8192 keys 32 / 44.
+  p.tile = rows <= 16 ? 16 : (B * H * tiles_of(kRowsTile) >= 256 ? kRowsTile : 32);
+  const int64_t row_tiles = tiles_of(p.tile);
   p.row_tiles = (int)row_tiles;
   p.tile_rows = (int)(rows < p.tile ? rows : p.tile);
   p.min_units = 4;
-  p.split = max_keys > 1024;
+  // Without the split there is no second launch and a range has no neighbours.  It pays while a
+  // workgroup alone walks its keys in the time of that launch, and longer where the row tiles fill the
+  // chip anyway.  Single tokens, d = 128, MXFP4, 8 key heads, us split / not:
+  //   1 sequence, 1024 keys 10.9 / 10.4, 2048 keys 10.9 / 16.4; 32 sequences, 2048 keys 23.9 / 20.6, 4096 keys 37.6 / 41.6.
+  p.split = max_keys > (B * H * row_tiles >= 256 ? 2048 : 1024);
   // Ranges: as many workgroups as the chip holds at once, so that all end together.
   const int64_t slots = 256 * (p.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, p.tile / 16));
   const int64_t places = B * row_tiles * (units + kSetup);  // there can be
