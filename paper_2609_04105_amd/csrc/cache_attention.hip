@@ -124,23 +124,33 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
     int token[NR];  // of the sequence
-    v4i q[kSharedQ ? 1 : NR][F::kSteps];
+    v4i q[kSharedQ ? 1 : NR][F::kSteps];  // in LDS later: wave r has row tile r
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
       token[r] = ic / a.G;
       const int h = head * a.G + (ic - token[r] * a.G);
       const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
-      if constexpr (kSharedQ) {
-        if (r % kWaves == wave || NR < kWaves)
+      if (!kSharedQ || r == wave)
 #pragma unroll
-          for (int s = 0; s < F::kSteps; ++s) lds_q[(r * F::kSteps + s) * 64 + lane] = reinterpret_cast<const v4i*>(p)[s];
-      } else {
-#pragma unroll
-        for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
-      }
+        for (int s = 0; s < F::kSteps; ++s) q[kSharedQ ? 0 : r][s] = reinterpret_cast<const v4i*>(p)[s];
+    }
+    // the wave's first tile, on its way together with the queries
+    const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
+    constexpr int kStride = kTile * kWaves;
+    int key0 = part.begin + kTile * wave;
+    Tile<D, FP8> t;
+    Pages pages{0, 0}, next{0, 0};
+    if (key0 < part.end) {
+      pages = find_pages(a, table, key0);
+      t.load_k(a.c, pages, key0, head, lane);
+      t.load_v(a.c, pages, key0, head, lane);
+      if (key0 + kStride < part.end) next = find_pages(a, table, key0 + kStride);
     }
     if constexpr (kSharedQ) {
+      if (wave < NR)
+#pragma unroll
+        for (int s = 0; s < F::kSteps; ++s) lds_q[(wave * F::kSteps + s) * 64 + lane] = q[0][s];
       __syncthreads();
     } else {  // (waits for the queries here; in the loop the compiler would wait for tiles with them)
 #pragma unroll
@@ -158,18 +168,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
     }
-    const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
 
     // The wave's tiles.  One set of registers: a tile's K is loaded when the one before has
     // become scores, its V when the one before is in the accumulators.
-    constexpr int kStride = kTile * kWaves;
-    int key0 = part.begin + kTile * wave;
     if (key0 < part.end) {
-      Tile<D, FP8> t;
-      Pages pages = find_pages(a, table, key0), next = pages;
-      t.load_k(a.c, pages, key0, head, lane);
-      t.load_v(a.c, pages, key0, head, lane);
-      if (key0 + kStride < part.end) next = find_pages(a, table, key0 + kStride);
       while (true) {
         const int ahead = key0 + kStride;
         const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
