@@ -110,6 +110,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
   v4i* lds_q = reinterpret_cast<v4i*>(lds);
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+  fetch_arguments(a, plan);
   const Place place = place_of(plan);
   const int head = place.head;
   if (head >= a.c.H) return;
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
-      token[r] = ic / a.G;
+      token[r] = divide(ic, a.G);
       const int h = head * a.G + (ic - token[r] * a.G);
       const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
       if (!kSharedQ || r == wave)
@@ -173,7 +174,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
     // become scores, its V when the one before is in the accumulators.
     if (key0 < part.end) {
       while (true) {
-        const int ahead = key0 + kStride;
+        // The last tile is loaded again instead of one behind it: where the loads of a tile depended on
+        // a branch, the compiler's waits for K waited for V too, the whole latency of a load in every tile.
+        const bool more = key0 + kStride < part.end;
+        const int ahead = more ? key0 + kStride : key0;
+        if (!more) next = pages;
         const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
         const bool masked = key0 + kTile > part.common || !page0 || !page1;  // uniform
         // S^T: register i of half h is key 8 g + 4 h + i
@@ -195,7 +200,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
               s[r][h] = mfma_16x16x32(kk, kSharedQ ? lds_q[(r * F::kSteps + st) * 64 + lane] : q[kSharedQ ? 0 : r][st], s[r][h]);
           });
         }
-        if (ahead < part.end) t.load_k(a.c, next, ahead, head, lane);
+        t.load_k(a.c, next, ahead, head, lane);
         if (masked) {
           // Hidden scores become -inf.  Keys that no row sees hold anything: their V codes and
           // scales become zero.  A non-finite V block that some row sees becomes zero too, and
@@ -285,8 +290,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
           }
           if constexpr (NR > 1) __builtin_amdgcn_sched_barrier(0);
         });
-        if (ahead >= part.end) break;
         t.load_v(a.c, next, ahead, head, lane);
+        if (!more) break;
         key0 = ahead;
         pages = next;
         if (ahead + kStride < part.end) next = find_pages(a, table, ahead + kStride);
@@ -323,6 +328,7 @@ constexpr int kJoinThreads = 256;
 template <int D, bool FP8, bool SPREAD>
 __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttentionArgs a, const CachePlan plan) {
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+  fetch_arguments(a, plan);
   const Partials part = partials(a, plan);
   const int w = blockIdx.y + 1;
   const int4 job = part.joins[w];
@@ -330,7 +336,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
   if (pieces == 0) return;
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const int row = SPREAD ? (int)blockIdx.x : (int)blockIdx.x * kGroups + group;
-  const int head = row / plan.tile_rows, in_tile = row - head * plan.tile_rows;
+  const int head = divide(row, plan.tile_rows), in_tile = row - head * plan.tile_rows;
   const int i = job.w * plan.tile + in_tile;
   const bool there = head < a.c.H && i < rows;
   float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
@@ -362,7 +368,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
     for (int k = 1; k < used; ++k) join(stat_lds[k], acc_lds[k][lane]);
   }
   if (!there) return;
-  const int t = i / a.G;
+  const int t = divide(i, a.G);
   const int64_t at = (int64_t)(first + t) * a.Hq + head * a.G + (i - t * a.G);
   const bool empty = is_zero(sum16);
   const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / sum16;

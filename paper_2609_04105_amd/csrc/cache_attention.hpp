@@ -66,6 +66,15 @@ __device__ __forceinline__ v4i probabilities(const v4f (&s)[2], float factor, fl
   return p;
 }
 
+// The arguments lie in four lines of the scalar cache, each a miss of 0.7 us when it is first used: one
+// value of each is read at the start, so that the misses overlap.
+__device__ __forceinline__ void fetch_arguments(const CacheAttentionArgs& a, const CachePlan& plan) {
+  asm volatile("" ::"s"(a.c.H), "s"(a.B), "s"(a.tree), "s"(plan.ranges));
+}
+
+// Of numbers that are not negative (half the instructions of a signed division).
+__device__ __forceinline__ int divide(int a, int b) { return (int)((unsigned)a / (unsigned)b); }
+
 // New tokens and keys of a sequence.
 struct Sequence {
   int first, tokens;  // rows of q
@@ -97,7 +106,7 @@ __device__ __forceinline__ Sequence sequence(const CacheAttentionArgs& a, int b)
 // Units of kUnit keys; at least one, so that rows without keys are written.
 __device__ __forceinline__ int units_of(const Sequence& s) { return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit; }
 __device__ __forceinline__ int row_tiles_of(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& s) {
-  return (s.tokens * a.G + plan.tile - 1) / plan.tile;
+  return (s.tokens * a.G + plan.tile - 1) >> __builtin_ctz(plan.tile);
 }
 
 // The row tiles of all sequences laid end to end in one line, each as kSetup places for what
@@ -141,7 +150,7 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
     scan(b0);
     total += __builtin_amdgcn_readlane(sum, 63);
   }
-  r.per = (total + plan.ranges - 1) / plan.ranges;
+  r.per = divide(total + plan.ranges - 1, plan.ranges);
   r.per = r.per < plan.min_units ? plan.min_units : r.per;
   r.begin = w * r.per;
   r.end = r.begin + r.per < total ? r.begin + r.per : total;
@@ -160,7 +169,7 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
       r.units = units_of(r.seq);
       r.tiles = row_tiles_of(a, plan, r.seq);
       const int start = __builtin_amdgcn_readlane(from, src), places = r.units + kSetup;
-      r.tile = (r.begin - start) / places;
+      r.tile = divide(r.begin - start, places);
       r.at = start + r.tile * places + kSetup;
       return r;
     }
@@ -336,7 +345,7 @@ __device__ __forceinline__ void store_columns(const CacheAttentionArgs& a, const
 #pragma unroll
   for (int j = 0; j < kCols; ++j) x[j] = bad ? as_float(0x7fc00000u) : o[j] * norm;
   if (whole) {
-    const int t = i / a.G;
+    const int t = divide(i, a.G);
     const int64_t at = (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
     if (a.out_bf16) store_row<kCols>(static_cast<uint16_t*>(a.out) + at * D + c * kCols, x);
     else store_row<kCols>(static_cast<float*>(a.out) + at * D + c * kCols, x);
@@ -355,7 +364,7 @@ struct Place {
   int w, head;
 };
 __device__ __forceinline__ Place place_of(const CachePlan& plan) {
-  const int item = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, head = item / plan.ranges;
+  const int item = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, head = divide(item, plan.ranges);
   return {item - head * plan.ranges, head};
 }
 
@@ -368,11 +377,11 @@ __device__ __forceinline__ Range open_range(const CacheAttentionArgs& a, const C
     if (p.head == 0 && threadIdx.x == 0) {
       int4 join = {0, 0, 0, 0};
       if (range.begin < range.end && range.begin > range.at && range.at >= range.begin - range.per)
-        join = int4{(range.at + range.units - 1) / range.per - p.w + 2, range.seq.first, range.seq.tokens * a.G, range.tile};
+        join = int4{divide(range.at + range.units - 1, range.per) - p.w + 2, range.seq.first, range.seq.tokens * a.G, range.tile};
       partials(a, plan).joins[p.w] = join;
     }
   } else {  // range w: row tile w % row_tiles of sequence w / row_tiles
-    range.b = p.w / plan.row_tiles;
+    range.b = divide(p.w, plan.row_tiles);
     range.tile = p.w - range.b * plan.row_tiles;
     range.seq = sequence(a, range.b);
     range.tiles = row_tiles_of(a, plan, range.seq);
@@ -419,8 +428,8 @@ __device__ __forceinline__ bool open_part(const CacheAttentionArgs& a, const Cac
   if (a.tree) {
     part->common = seq.prefix;
   } else {  // causal: the first and the last row's token
-    const int last = seq.prefix + (row1 - 1) / a.G + 1;
-    part->common = seq.prefix + row0 / a.G + 1;
+    const int last = seq.prefix + divide(row1 - 1, a.G) + 1;
+    part->common = seq.prefix + divide(row0, a.G) + 1;
     part->end = part->end > last ? last : part->end;
   }
   part->common = part->common > seq.keys ? seq.keys : part->common;

@@ -124,6 +124,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
   __shared__ unsigned huge_lds[kTiles][2];  // [tile][keys 0-3, 4-7 of eight]: a non-finite V block that some row sees
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
+  fetch_arguments(a, plan);
   const Place place = place_of(plan);
   const int head = place.head;
   if (head >= a.c.H) return;
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
     for (int r = 0; r < kNr; ++r) {
       const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
-      token[r] = ic / a.G;
+      token[r] = divide(ic, a.G);
       const int h = head * a.G + (ic - token[r] * a.G);
       const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
 #pragma unroll
