@@ -7,7 +7,7 @@
 //
 // Angles of far positions need more than 24 bits (position 10^6 at one radian a step is
 // off by 0.06 in fp32), so t and its reduction to a quarter turn are fp64; what is
-// left, |t| <= pi / 4, is exact to 2^-26 quarter turns in fp32.  A workgroup takes four tokens
+// left, |t| <= pi / 4, is exact to 2^-26 quarter turns in fp32.  A workgroup takes 4 or 16 tokens
 // and forms each token's angles once, in LDS, for all its heads.
 #include <cmath>
 
@@ -71,14 +71,14 @@ struct Unit<float> {
 };
 
 // grid: (token groups, head groups of `heads`, B)
-template <typename T, bool INTERLEAVED>
+template <typename T, bool INTERLEAVED, int TOKENS>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, int heads) {
   constexpr int kItems = sizeof(T) == 2 ? 4 : 2;  // units of a thread in flight
-  __shared__ __attribute__((aligned(16))) float table[2][kRotaryTokens][kRotaryMaxDim / 2];
+  __shared__ __attribute__((aligned(16))) float table[2][TOKENS][kRotaryMaxDim / 2];
   const int tid = threadIdx.x, half = a.r / 2;
-  const int64_t n0 = (int64_t)blockIdx.x * kRotaryTokens;
+  const int64_t n0 = (int64_t)blockIdx.x * TOKENS;
   const int64_t b = blockIdx.z;
-  const int tokens = a.N - n0 < kRotaryTokens ? (int)(a.N - n0) : kRotaryTokens;
+  const int tokens = a.N - n0 < TOKENS ? (int)(a.N - n0) : TOKENS;
   for (int i = tid; i < tokens * half; i += kThreads) {
     const int tok = i / half, j = i - tok * half;
     const double t = (double)a.positions[b * a.pos_stride + n0 + tok] * a.inv_freq[j];
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
   const int h0 = blockIdx.y * heads;
   const int nh = a.H - h0 < heads ? (int)(a.H - h0) : heads;
   const int units = a.d / kUnit, turned = a.r / kUnit;
-  const int count = units * nh * kRotaryTokens;
+  const int count = units * nh * TOKENS;
   const T* x = static_cast<const T*>(a.x) + b * a.xb + n0 * a.xn + h0 * a.xh;
   T* out = static_cast<T*>(a.out) + b * a.ob + n0 * a.on + h0 * a.oh;
   const bool in_place = a.x == a.out;
@@ -105,9 +105,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
     int tok[kItems], u[kItems], gap[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-      const int idx = first + i * kThreads, row = idx / units, h = row / kRotaryTokens;
+      const int idx = first + i * kThreads, row = idx / units, h = row / TOKENS;
       u[i] = idx - row * units;
-      tok[i] = row % kRotaryTokens;
+      tok[i] = row % TOKENS;
       const bool turn = u[i] < turned;
       if (idx >= count || tok[i] >= tokens || (in_place && !turn)) tok[i] = -1;
       const int c = turn && !INTERLEAVED ? 8 * u[i] : kUnit * u[i];
@@ -145,21 +145,32 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
 }  // namespace
 
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream) {
-  // Heads of a workgroup: enough units for four of each thread where the grid stays
-  // large, one of each where it is small.
   const int units = a.d / kUnit;
-  const int64_t groups = (a.N + kRotaryTokens - 1) / kRotaryTokens;
-  auto heads_for = [&](int per_thread) {
-    int64_t h = (int64_t)kThreads * per_thread / (units * kRotaryTokens);
-    h = h < 1 ? 1 : h;
-    return h > a.H ? a.H : h;
+  int tokens;
+  int64_t groups, heads;
+  auto plan = [&](int t, int per_thread) {  // heads of a workgroup: `per_thread` units for each thread
+    tokens = t;
+    groups = (a.N + t - 1) / t;
+    heads = (int64_t)kThreads * per_thread / (units * t);
+    heads = heads < 1 ? 1 : (heads > a.H ? a.H : heads);
+    return groups * a.B * ((a.H + heads - 1) / heads);
   };
-  int64_t heads = heads_for(4);
-  if (groups * a.B * ((a.H + heads - 1) / heads) < 512) heads = heads_for(1);
+  // Sixteen tokens make longer runs where tokens lie side by side, but fewer workgroups: bf16, d = 128,
+  // 32 heads, 16384 tokens 54.3 -> 49.4 us (4096 workgroups), 8 heads 15.3 -> 13.8 (1024), 32 heads of 2048
+  // tokens 8.9 -> 9.8 (512); with heads side by side 16384 tokens 50.7 -> 53.8.  One unit a thread where
+  // four leave few workgroups: one token of 32 heads 4.0 -> 3.1 us.
+  if (!(a.xn < a.xh && plan(16, 4) >= 1024) && plan(4, 4) < 512) plan(4, 1);
   const dim3 grid((unsigned)groups, (unsigned)((a.H + heads - 1) / heads), (unsigned)a.B);
-  auto* kernel = a.bf16 ? (a.interleaved ? rotary_kernel<uint16_t, true> : rotary_kernel<uint16_t, false>)
-                        : (a.interleaved ? rotary_kernel<float, true> : rotary_kernel<float, false>);
-  kernel<<<grid, kThreads, 0, stream>>>(a, (int)heads);
+  auto launch = [&](auto T_, auto INTERLEAVED_) {
+    using T = decltype(T_);
+    constexpr bool kInterleaved = decltype(INTERLEAVED_)::value;
+    if (tokens == 16) rotary_kernel<T, kInterleaved, 16><<<grid, kThreads, 0, stream>>>(a, (int)heads);
+    else rotary_kernel<T, kInterleaved, 4><<<grid, kThreads, 0, stream>>>(a, (int)heads);
+  };
+  if (a.bf16 && a.interleaved) launch(uint16_t{}, std::true_type{});
+  else if (a.bf16) launch(uint16_t{}, std::false_type{});
+  else if (a.interleaved) launch(float{}, std::true_type{});
+  else launch(float{}, std::false_type{});
   return hipGetLastError();
 }
 

@@ -21,7 +21,6 @@ struct RotaryArgs {
   int bf16, interleaved, inverse;
 };
 
-constexpr int kRotaryTokens = 4;     // tokens of one workgroup
 constexpr int kRotaryMaxDim = 512;
 
 hipError_t launch_rotary(const RotaryArgs& a, hipStream_t stream);

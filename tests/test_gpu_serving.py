@@ -78,6 +78,25 @@ def test_rotary(fa, B, H, N, d, r, interleaved, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,H,N,d,r", [(2, 64, 1033, 128, 96), (16, 16, 1030, 64, 32), (1, 40, 835, 512, 512)])
+def test_rotary_many_tokens(fa, B, H, N, d, r, dtype):
+    """Batches that fill the chip, with the last tokens of a sequence alone; in place, and token-major."""
+    g = torch.Generator(device="cuda").manual_seed(N + d)
+    x = torch.randn((B, H, N, d), device="cuda", generator=g).to(dtype)
+    positions = torch.randint(0, 1 << 20, (B, N), device="cuda", generator=g)
+    freq, _ = fa.rotary_frequencies(r)
+    for o in (dict(interleaved=False, magnitude=1.25), dict(interleaved=True, magnitude=0.75, inverse=True)):
+        got = fa.rotary(x, positions, freq, **o)
+        some = slice(0, 2)
+        for h in (0, H - 1):
+            _check_rotary(_f64(got[some, h:h + 1]), _f64(x[some, h:h + 1]), positions[some].cpu().numpy(), _f64(freq), dtype, **o)
+        y = x.clone()
+        assert fa.rotary(y, positions, freq, out=y, **o) is y and torch.equal(y, got)
+        z = x.transpose(1, 2).contiguous().transpose(1, 2)
+        assert torch.equal(fa.rotary(z, positions, freq, **o), got)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_rotary_strides(fa, dtype):
     """Heads of a fused projection, token-major sequences, a head shared by expansion; the
     rest of the output's buffer stays as it was."""
