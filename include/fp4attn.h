@@ -342,7 +342,7 @@ typedef struct fp4attn_cache {
  *
  * Errors: those of the cache (below), INVALID_ARG for null or misaligned pointers,
  * n < 0, strides negative or no multiple of 16 bytes, a bad src_dtype; UNSUPPORTED for more
- * than 2^30 blocks of 32.  Errors of the cache: INVALID_ARG for NULL, a wrong struct_size,
+ * than 2^29 blocks of 32.  Errors of the cache: INVALID_ARG for NULL, a wrong struct_size,
  * fp8 not 0 or 1, sizes < 1, a page_size that is no power of two or below 16, null or
  * misaligned pointers; UNSUPPORTED for head_dim not 64 or 128, heads above 65535, page_size
  * above 2^20, or more than 2^40 slots.
@@ -391,7 +391,8 @@ fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slo
  * n not B * max_q without q_starts, tree_words * 64 < max_q with a tree, softmax_scale not
  * finite or <= 0, a bad out_dtype, a workspace that is too small; UNSUPPORTED for n * q_heads
  * or max_q * q_heads of 2^31 or more, max_pages * page_size above 2^30 or B times that above
- * 2^36, B above 65535, or more than 2^24 workgroups.
+ * 2^36, B above 65535, 2^24 workgroups, or (row tiles of B max_q-token sequences times keys
+ * of max_pages) 2^31 units of 128 keys.
  */
 fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
                                        int64_t q_stride, int64_t B, const int32_t* page_table, int64_t max_pages,

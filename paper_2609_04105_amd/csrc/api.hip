@@ -252,7 +252,7 @@ fp4attn_status check_cache(const fp4attn_cache* c, fp4attn::CacheView* view) {
 
 fp4attn_status check_tokens(const fp4attn::CacheView& c, int64_t n) {
   if (n < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "n=%lld must not be negative", (long long)n);
-  if (n > (int64_t(1) << 30) / (c.H * (c.d / 32)) - 8)
+  if (n > (int64_t(1) << 29) / (c.H * (c.d / 32)) - 8)  // 16 threads a token and head read: below 2^32
     return fail(FP4ATTN_ERR_UNSUPPORTED, "n=%lld tokens of %d heads are too many for one launch", (long long)n, c.H);
   return FP4ATTN_OK;
 }

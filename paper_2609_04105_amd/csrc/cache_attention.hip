@@ -422,7 +422,7 @@ CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, 
   int64_t ranges = slots / H < 1 ? 1 : slots / H;
   if (ranges > (places + p.min_units - 1) / p.min_units) ranges = (places + p.min_units - 1) / p.min_units;
   if (!p.split) ranges = B * row_tiles;
-  p.fits = places < (int64_t(1) << 31) && ranges * H < (1 << 24);
+  p.fits = places + ranges < (int64_t(1) << 31) && ranges * H <= (1 << 24) - 8;  // int places; launches below 2^32 threads
   p.ranges = (int)ranges;
   p.workgroups = (ranges * H + 7) / 8 * 8;
   if (p.split && ranges > 1) p.workspace = ranges * 16 + ranges * 2 * H * p.tile_rows * (d * 4 + 16);

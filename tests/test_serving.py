@@ -76,6 +76,8 @@ def test_cache_refusals(fa):
               (PTR[0], PTR[1], 1, 3, 128, 128, ctypes.c_void_p(4100))):
         assert write(c, *o, None) == 1, o
     assert write(c, PTR[0], PTR[1], 1, 1 << 30, 128, 128, PTR[2], None) == 2
+    one = ctypes.byref(_cache(fa, heads=1, head_dim=64))
+    assert write(one, PTR[0], PTR[1], 1, 1 << 28, 64, 64, PTR[2], None) == 2
     assert write(c, None, None, 1, 0, 128, 128, None, None) == 0
     for o in ((None, 3, PTR[1], PTR[2], 0), (PTR[0], 3, None, PTR[2], 0), (PTR[0], 3, PTR[1], ODD, 0),
               (PTR[0], 3, PTR[1], PTR[2], 5), (PTR[0], -2, PTR[1], PTR[2], 0)):
