@@ -11,8 +11,10 @@
 // a step; the second workgroup of a CU fills them.
 //
 // Measured, d = 128, MXFP4, 32 sequences of 8192 keys and less, trees of 64 tokens, 8 key heads of 8 query heads:
-// 373 us, 717 TFLOP/s (a large bf16 matrix product: 1170).  A step takes some 1100 cycles of a wave in the matrix
-// unit, 1200 in the vector unit and 1000 reading LDS; two waves a SIMD overlap them in part.
+// 357 us, 748 TFLOP/s; 2048 new tokens over 8192 keys 556 us, 989 (a large bf16 matrix product: 1170).  Counters of
+// the first: the matrix unit is busy 33 % of the time, vector instructions take 42 %, LDS 33 %; two waves a SIMD
+// overlap them in part.  Work put between the products of the same wave (converting V and K, the second tile's
+// probabilities) made it 1 to 3 % slower, four sums side by side in the K products changed nothing.
 #include "cache_attention.hpp"
 
 namespace fp4attn {
