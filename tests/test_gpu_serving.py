@@ -536,7 +536,7 @@ def _beside_idle(b, tiles, width):
 def test_many_row_tiles(fa, d, fp8, new, keys, H, G, page, width):
     """More than 32 rows in a batch that fills the chip with row tiles, causal and with trees, with
     short page tables and with long ones."""
-    b = _beside_idle(Batch(keys, new, H, G, d, fp8, page, seed=sum(new)), 256, width)
+    b = _beside_idle(Batch(keys, new, H, G, d, fp8, page, seed=sum(new)), 512, width)
     lse = torch.empty((sum(new), H * G), device="cuda")
     b.check(b.call(fa, lse=lse), lse)
     b.check(b.call(fa, out_dtype=torch.bfloat16))
@@ -546,7 +546,7 @@ def test_many_row_tiles(fa, d, fp8, new, keys, H, G, page, width):
 
 @pytest.mark.parametrize("width", [1, 6000])
 @pytest.mark.parametrize("d,fp8", FORMATS)
-@pytest.mark.parametrize("G,idle", [(2, 0), (5, 0), (20, 0), (20, 256)])
+@pytest.mark.parametrize("G,idle", [(2, 0), (5, 0), (20, 0), (20, 512)])
 def test_hidden_and_missing_in_every_tiling(fa, d, fp8, G, idle, width):
     """NaN keys, NaN and overflowing value blocks that some drafted tokens see, and a page outside the
     cache, in row tiles of every size."""
