@@ -21,8 +21,8 @@
 //   second launch (no atomics: the order is fixed).
 //
 // Measured, single tokens, 8 key heads: MXFP4, d = 128, 64 sequences of 16384 keys and four query heads to
-// a key head 210 us, 5.4 TB/s of the cache (a large copy: 5.0 .. 5.3); MXFP8, 4 sequences of 131072 keys,
-// eight to a key head 160 us, 5.4 TB/s; d = 64, MXFP4, 64 of 16384 keys, eight to a key head 123 us, 4.6 TB/s
+// a key head 208 us, 5.5 TB/s of the cache (a large copy: 5.0 .. 5.3); MXFP8, 4 sequences of 131072 keys,
+// eight to a key head 160 us, 5.4 TB/s; d = 64, MXFP4, 64 of 16384 keys, eight to a key head 117 us, 4.9 TB/s
 // (half the bytes a key, more than half the instructions).  Short calls are latency: one sequence of 517 keys
 // 8.1 us, of which the arguments, the length, the page, the first tile one after the other 2.3 us, the tiles
 // 0.74 us each (330 instructions of a wave alone on its SIMD), the join of the waves and the stores 1.2 us.
@@ -126,6 +126,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
   if (range.begin >= range.end) return;
   const float factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
 
+  // A CU serves the workgroups that came first, of the first half of the grid, before the others, which then end
+  // later: those go first in every second tile.  64 sequences of 2768 keys 46.9 -> 45.7 us, of 16384
+  // keys 210.3 -> 208.0; d = 64 119.4 -> 117.2; trees of 16 tokens over 8 of 2047 keys 22.6 -> 21.8.
+  const bool late = plan.split && blockIdx.x >= gridDim.x / 2;
   Part part;
   while (open_part(a, plan, range, &part)) {
     const Sequence seq = range.seq;
@@ -182,6 +186,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
     // become scores, its V when the one before is in the accumulators.
     if (key0 < part.end) {
       while (true) {
+        if (late) {
+          if (key0 & kStride) __builtin_amdgcn_s_setprio(2);
+          else __builtin_amdgcn_s_setprio(0);
+        }
         // The last tile is loaded again instead of one behind it: where the loads of a tile depended on
         // a branch, the compiler's waits for K waited for V too, the whole latency of a load in every tile.
         const bool more = key0 + kStride < part.end;
