@@ -87,6 +87,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
   constexpr int kItems = 4;  // units of a thread in flight
   constexpr int kPairs = kUnit<T> / 2;
   __shared__ __attribute__((aligned(16))) float table[2][TOKENS][kRotaryMaxDim / 2];
+  asm volatile("" ::"s"(heads), "s"(a.N), "s"(a.x));  // of each line of the arguments: their misses overlap
   const int tid = threadIdx.x, half = a.r / 2;
   const int64_t n0 = (int64_t)blockIdx.x * TOKENS;
   const int64_t b = blockIdx.z;
