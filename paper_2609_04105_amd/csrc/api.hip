@@ -6,6 +6,7 @@
 #include <cstring>
 
 #include "../../include/fp4attn.h"
+#include "cache_plan.hpp"
 #include "launch.hpp"
 #include "serving.hpp"
 

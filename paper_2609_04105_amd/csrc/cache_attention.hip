@@ -73,11 +73,6 @@ struct Tile {
   }
 };
 
-// Waves per SIMD that the registers are kept to.  (Two tiles in flight instead of one, at 2 .. 3 waves:
-// within 3 % either way for d = 128, and four waves of d = 64 are faster, 126 us against 130 for 64
-// sequences of 16384 keys and 8 key heads; at three waves 140.)
-constexpr int waves_per_simd(int d, int nr) { return 6 - d / 64 - nr; }
-
 // Joins the waves' results of row i and columns D / 16 * c ..  lds: [wave][product][row, 4 g + i];
 // stat: the row's {reference, sum, sum of the rounded values} of the first wave, 16 rows apart; poison:
 // its mark, 64 words apart.
@@ -412,46 +407,6 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
 }
 
 }  // namespace
-
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys) {
-  CachePlan p{};
-  const int64_t rows = max_q * G, units = (max_keys + kUnit - 1) / kUnit;
-  auto tiles_of = [&](int64_t tile) { return (rows + tile - 1) / tile; };
-  // Rows of a tile.  Up to 16 rows the matrix products have one column tile of them.  More: the 128-row
-  // kernel converts a key's codes once for 128 rows, the other once for 32, but it needs more work to
-  // fill the chip: two workgroups of 128 rows for every CU with d = 64 (half the products to a conversion), one
-  // with d = 128, half of one if there are many keys to cut up.  MXFP4, 8 key heads of 8 query heads, us at tile 32 / 128:
-  //   d = 128, 32 sequences, 64 tokens (1024 workgroups of 128 rows), 2048 keys 184 / 154, 12 (384), 1024 keys 57 / 46;
-  //   24 sequences, 16 tokens (192), 4096 keys 89 / 84, 8192 keys 149 / 135, 2048 keys 53 / 54, 1024 keys 36 / 38;
-  //   16 sequences, 16 tokens (128), 8192 keys MXFP4 96 / 95, MXFP8 145 / 108, 4096 keys 60 / 63;
-  //   d = 64, 16 sequences, 64 tokens (512), 1024 keys 45 / 39, 4096 keys 121 / 125; 32, 16 tokens (256), 2048 keys 44 / 53.
-  const int64_t wide = B * H * tiles_of(kRowsTile);
-  const bool rows128 = wide >= 512 || (d == 128 && (wide >= 256 || (wide >= 128 && wide * max_keys >= 3 << 18)));
-  p.tile = rows <= 16 ? 16 : (rows128 ? kRowsTile : 32);
-  const int64_t row_tiles = tiles_of(p.tile);
-  p.row_tiles = (int)row_tiles;
-  p.tile_rows = (int)(rows < p.tile ? rows : p.tile);
-  p.min_units = 4;
-  // Without the split there is no second launch and a range has no neighbours.  It pays while a
-  // workgroup alone walks its keys in the time of that launch, and longer where the row tiles fill the
-  // chip anyway (of 128 rows: twice).  Single tokens, d = 128, MXFP4, 8 key heads, us split / not:
-  //   1 sequence, 1024 keys 10.9 / 10.4, 2048 keys 10.9 / 16.4; 32 sequences, 2048 keys 23.9 / 20.6, 4096 keys 37.6 / 41.6;
-  // of 128 rows: 16 sequences, 64 tokens (512 workgroups), 2048 keys 92 / 81, 8 (256) 60 / 68, 1024 keys 43 / 38;
-  // 32, 16 tokens (256), 1040 keys 49 / 39.
-  const bool full = B * H * row_tiles >= (p.tile == kRowsTile ? 512 : 256);
-  p.split = max_keys > (full ? 2048 : (p.tile == kRowsTile ? 1536 : 1024));
-  // Ranges: as many workgroups as the chip holds at once, so that all end together.
-  const int64_t slots = 256 * (p.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, p.tile / 16));
-  const int64_t places = B * row_tiles * (units + kSetup);  // there can be
-  int64_t ranges = slots / H < 1 ? 1 : slots / H;
-  if (ranges > (places + p.min_units - 1) / p.min_units) ranges = (places + p.min_units - 1) / p.min_units;
-  if (!p.split) ranges = B * row_tiles;
-  p.fits = places + ranges < (int64_t(1) << 31) && ranges * H <= (1 << 24) - 8;  // int places; launches below 2^32 threads
-  p.ranges = (int)ranges;
-  p.workgroups = (ranges * H + 7) / 8 * 8;
-  if (p.split && ranges > 1) p.workspace = ranges * 16 + ranges * 2 * H * p.tile_rows * (d * 4 + 16);
-  return p;
-}
 
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream) {
   const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.max_q, (int64_t)a.max_pages << a.c.page_shift);

@@ -2,6 +2,7 @@
 // keys are dealt to workgroups, the cache's codes as bf16, masks, partial results.
 #pragma once
 
+#include "cache_plan.hpp"
 #include "gfx950.hpp"
 #include "serving.hpp"
 
@@ -10,7 +11,6 @@ namespace fp4attn {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kTile = 32;   // keys of a wave's step
-constexpr int kUnit = 128;  // keys that ranges are counted in
 constexpr float kLag = 8.0f;    // binades that a row's reference may lag its maximum
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -113,7 +113,6 @@ __device__ __forceinline__ int row_tiles_of(const CacheAttentionArgs& a, const C
 // starting one costs and then its keys' units; range w takes places [w per, (w + 1) per): equal parts
 // for every workgroup, whatever the lengths and the numbers of rows.  (Places to a start, 64 sequences of 128 to
 // 16384 keys: 4 47.9 us, 3 47.3, 2 48.3, 1 50.5; trees of 16 tokens over 8 of 2047 keys: 22.6, 22.2, 24.2, 25.0.)
-constexpr int kSetup = 4;
 struct Range {
   int begin, end;
   int b, tile, tiles;  // a row tile of the range, of the sequence's `tiles`

@@ -1,4 +1,4 @@
-// Host-side launchers and launch plans of the operators around a key/value cache:
+// Host-side launchers of the operators around a key/value cache:
 // rotary positions, the cache's quantizer and reader, attention over it.  Arguments
 // are already validated by the C-ABI layer (api.hip).
 #pragma once
@@ -57,26 +57,7 @@ struct CacheReadArgs {
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
 
-// How one attention call is cut up.  Rows (token, head of the group) of a sequence and
-// key head go to workgroups in tiles of 16, 32 (their waves split the keys) or 128 rows (their
-// waves split the rows).  With split, the row tiles of all sequences, each with its keys in
-// units of 128, lie end to end (with a few places between them), and each of `ranges` workgroups
-// per key head takes an equal part of that line (fewer ranges if that leaves less than
-// min_units each); lengths are known on the device only.  Without, a range is a row tile.
-struct CachePlan {
-  int tile;       // rows of a row tile
-  int row_tiles;  // of the longest sequence and one key head
-  int tile_rows;  // rows of a tile that can be in use
-  int split, ranges, min_units;
-  bool fits;           // the line's places and the workgroups are in range
-  int64_t workgroups;  // of the first launch
-  int64_t workspace;   // bytes
-};
-constexpr int kRowsTile = 128, kRowsPerCu = 2;  // cache_attention_rows.hip: rows of a workgroup, workgroups of a CU
-
-constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
-
-CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys);
+struct CachePlan;  // cache_plan.hpp
 
 struct CacheAttentionArgs {
   CacheView c;
