@@ -397,7 +397,7 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
   if (plan.tile == 16) cache_attention_kernel<D, FP8, 1><<<grid, kThreads, 0, stream>>>(a, plan);
   else if (plan.tile == 32) cache_attention_kernel<D, FP8, 2><<<grid, kThreads, 0, stream>>>(a, plan);
   else launch_cache_rows(a, plan, stream);
-  if (!plan.split || plan.ranges == 1) return;
+  if (!plan.split) return;
   const unsigned rows = (unsigned)(plan.tile_rows * a.c.H), per = kJoinThreads / (D / 4);
   // many pieces a row tile: a workgroup for each row
   if (plan.ranges >= 16 * a.B * plan.row_tiles)

@@ -57,17 +57,18 @@ inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t 
   // of 128 rows: 16 sequences, 64 tokens (512 workgroups), 2048 keys 92 / 81, 8 (256) 60 / 68, 1024 keys 43 / 38;
   // 32, 16 tokens (256), 1040 keys 49 / 39.
   const bool full = B * H * row_tiles >= (p.tile == kRowsTile ? 512 : 256);
-  p.split = max_keys > (full ? 2048 : (p.tile == kRowsTile ? 1536 : 1024));
-  // Ranges: as many workgroups as the chip holds at once, so that all end together.
+  // Ranges: as many workgroups as the chip holds at once, so that all end together.  With so many key heads that
+  // this leaves each a single range, nothing can be cut.
   const int64_t slots = 256 * (p.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, p.tile / 16));
+  p.split = max_keys > (full ? 2048 : (p.tile == kRowsTile ? 1536 : 1024)) && slots / H >= 2;
   const int64_t places = B * row_tiles * (units + kSetup);  // there can be
-  int64_t ranges = slots / H < 1 ? 1 : slots / H;
+  int64_t ranges = slots / H;
   if (ranges > (places + p.min_units - 1) / p.min_units) ranges = (places + p.min_units - 1) / p.min_units;
   if (!p.split) ranges = B * row_tiles;
   p.fits = places + ranges < (int64_t(1) << 31) && ranges * H <= (1 << 24) - 8;  // int places; launches below 2^32 threads
   p.ranges = (int)ranges;
   p.workgroups = (ranges * H + 7) / 8 * 8;
-  if (p.split && ranges > 1) p.workspace = ranges * 16 + ranges * 2 * H * p.tile_rows * (d * 4 + 16);
+  if (p.split) p.workspace = ranges * 16 + ranges * 2 * H * p.tile_rows * (d * 4 + 16);
   return p;
 }
 

@@ -53,3 +53,17 @@ def test_tiles_cover_the_rows(plans):
         assert p.ranges >= 1 and p.workgroups % 8 == 0 and p.workgroups >= p.ranges * H, c
         if not p.split:
             assert p.ranges == B * p.row_tiles and p.workspace == 0, c
+
+
+def test_cut_calls_have_a_workspace(plans):
+    """A call is cut only into ranges that share a key head's row tiles, two at least, and then has room for the
+    records and for both ends of every range: the kernels write them whenever a call is cut."""
+    calls = list(_calls())
+    cut = 0
+    for c, p in zip(calls, plans(calls)):
+        B, H, G, d, max_q, keys = c
+        if p.split:
+            cut += 1
+            assert p.ranges >= 2, c
+            assert p.workspace >= 16 * p.ranges + 2 * p.ranges * H * p.tile_rows * (4 * d + 16), c
+    assert cut > len(calls) // 10

@@ -839,3 +839,17 @@ def test_native_calls_equal_the_python_path(fa, monkeypatch):
             if kind != "refused":
                 assert watched.took == (kind == "taken"), f"{kind} call {i}"
     monkeypatch.setattr(fa.api, "_binding", native)
+
+
+@pytest.mark.parametrize("d,fp8,H,G,new", [(128, False, 390, 2, [1, 1]), (64, False, 520, 1, [1, 1]), (64, True, 390, 1, [20, 3]),
+                                           (128, True, 260, 1, [70, 1])])
+def test_more_key_heads_than_ranges(fa, d, fp8, H, G, new):
+    """So many key heads that a key head's workgroups cannot be two: nothing is cut, and no workspace is asked for,
+    in a table of 4096 keys."""
+    keys = [200, 130]
+    b = Batch(keys, new, H, G, d, fp8, 64, seed=H, spare=60)
+    c = fa.api._cache(fa.KVCache(*(torch.from_numpy(t).cuda() for t in b.cache)))
+    size = fa.lib.fp4attn_cache_attention_workspace
+    assert size(c, H * G, 2, b.table.shape[1], max(new)) == 0 and size(c, H * G, 2, 16, max(new)) == 0
+    lse = torch.empty((sum(new), H * G), device="cuda")
+    b.check(b.call(fa, lse=lse), lse)
