@@ -75,7 +75,7 @@ struct Tile {
 
 // Joins the waves' results of row i and columns D / 16 * c ..  lds: [wave][product][row, 4 g + i];
 // stat: the row's {reference, sum, sum of the rounded values} of the first wave, 16 rows apart; poison:
-// its mark, 64 words apart.
+// its marks (four c's), 64 words apart.
 template <int D, bool FP8>
 __device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& seq,
                                            const float* lds, const float* stat, const unsigned* poison, int i, int c,
@@ -83,7 +83,7 @@ __device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const Ca
   constexpr int kCols = D / 16;
   if (i >= seq.tokens * a.G) return;
   float top = -__builtin_inff(), sum = 0.0f, rounded = 0.0f, o[kCols];
-  unsigned bad = 0;
+  unsigned odd = 0;
 #pragma unroll
   for (int j = 0; j < kCols; ++j) o[j] = 0.0f;
 #pragma unroll
@@ -93,11 +93,11 @@ __device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const Ca
     const float ref = stat[w * 64], part = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
     sum += stat[w * 64 + 1] * part;
     rounded += stat[w * 64 + 2] * part;
-    bad |= poison[w * 64];
+    odd |= poison[w * 64];
 #pragma unroll
     for (int j = 0; j < kCols; ++j) o[j] += lds[(w * kCols + j) * 256 + threadIdx.x] * part;
   }
-  store_columns<D, FP8>(a, plan, seq, i, head, c, whole, piece, top, sum, rounded, bad != 0, o);
+  store_columns<D, FP8>(a, plan, seq, i, head, c, whole, piece, top, sum, rounded, odd >> kCols * (c % 4), o);
 }
 
 template <int D, bool FP8, int NR>
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
     }
     v4f acc[NR][F::kDTiles];
     v4f sum16[NR];  // the rounded probabilities (the same in all four)
-    unsigned poisoned = 0;     // bit r: this lane's columns of row r see a non-finite V block
+    unsigned poisoned[NR];     // this lane's columns (odd_columns) in which the row sees a V that is no number
     float ref[NR], sum[NR];    // base 2, lags the maximum by at most kLag; this lane's own keys
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -175,6 +175,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       sum16[r] = v4f{0, 0, 0, 0};
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
+      poisoned[r] = 0;
     }
 
     // The wave's tiles.  One set of registers: a tile's K is loaded when the one before has
@@ -214,8 +215,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
         t.load_k(a.c, next, ahead, head, lane);
         if (masked) {
           // Hidden scores become -inf.  Keys that no row sees hold anything: their V codes and
-          // scales become zero.  A non-finite V block that some row sees becomes zero too, and
-          // marks the rows that see it, whose outputs become NaN after the loop.
+          // scales become zero.  A non-finite V block that some row may see becomes zero too, and a NaN
+          // code of MXFP8; they mark the rows that see them, whose outputs become NaN after the loop.
           const int base = key0 + 8 * g;
           const unsigned there = (g >= 2 ? page1 : page0) ? below(seq.keys - base) : 0u;
           unsigned see[NR];
@@ -225,11 +226,11 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = see[r] >> j & 1 ? s[r][j / 4][j % 4] : -__builtin_inff();
           }
-          unsigned huge = 0;
+          unsigned odd = 0;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const bool in = there >> j & 1, big = (t.vs[j / 4] >> (8 * (j % 4)) & 255u) >= kHugeScale<FP8>;
-            huge |= in && big ? 1u : 0u;
+            odd |= in && big ? 1u : 0u;
             const unsigned keep = in && !big ? ~0u : 0u;
             t.vs[j / 4] &= keep | ~(255u << (8 * (j % 4)));
             if constexpr (F::kVWords >= 8) {
@@ -239,17 +240,22 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
               t.v[j / 2] &= keep | (j % 2 ? 0x0000ffffu : 0xffff0000u);
             }
           }
-          if (__any(huge)) {  // lane group g holds outputs of d block g (d = 64: g / 2)
+          if constexpr (FP8)
+#pragma unroll
+            for (int i = 0; i < F::kVWords; ++i) odd |= nan_codes(t.v[i]);
+          if (__any(odd)) {
+            if constexpr (FP8)
+#pragma unroll
+              for (int i = 0; i < F::kVWords; ++i) t.v[i] = without_nan_codes(t.v[i]);
 #pragma unroll
             for (int r = 0; r < NR; ++r) see[r] = groups_or(see[r] << (8 * g));
-            const int blk = g * F::kBlocks / 4;
             for (int k = 0; k < kTile; ++k) {
               const int page = k >= 16 ? pages.p1 : pages.p0, key = key0 + k;
               if (!is_page(a.c, page) || key >= seq.keys) continue;
               const int64_t group = row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
-              const bool big = a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] >= kHugeScale<FP8>;
+              const unsigned columns = odd_columns<D, FP8>(a.c, group, k & 7, g);
 #pragma unroll
-              for (int r = 0; r < NR; ++r) poisoned |= big ? (see[r] >> k & 1) << r : 0u;
+              for (int r = 0; r < NR; ++r) poisoned[r] |= see[r] >> k & 1 ? columns : 0u;
             }
           }
         }
@@ -320,7 +326,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       for (int t = 0; t < F::kDTiles; ++t)
         lds[(wave * F::kDTiles + t) * 64 + m * 4 + g] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
       if (g == 0) lds_stat[wave][m] = float4{ref[r], total, sum16[r][0], 0.0f};
-      lds_poison[wave][m * 4 + g] = poisoned >> r & 1;
+      lds_poison[wave][m * 4 + g] = poisoned[r];
       __syncthreads();
       join_waves<D, FP8>(a, plan, seq, reinterpret_cast<const float*>(lds), &lds_stat[0][row].x,
                          &lds_poison[0][row * 4 + (c >> 2)], row0 + 16 * r + row, c, head, part.whole,

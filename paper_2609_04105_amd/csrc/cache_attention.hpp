@@ -314,6 +314,32 @@ __device__ __forceinline__ unsigned code_pair(const unsigned* w, float scale) {
 template <bool FP8>
 constexpr unsigned kHugeScale = FP8 ? 247u : 253u;
 
+// The top bits of those bytes of w that are E4M3's NaN codes, 0x7f and 0xff (carries stay in their bytes).
+__device__ __forceinline__ unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ unsigned without_nan_codes(unsigned w) {
+  const unsigned n = nan_codes(w);
+  return w & ~(n | (n - (n >> 7)));
+}
+
+// Of the D / 4 output columns that lane group g holds, D / 16 * (4 g + i) + t as bit D / 16 * i + t, those in which
+// key `key` of eight keys' V is no number: all under a huge scale (they lie in one block), else those of NaN codes.
+template <int D, bool FP8>
+__device__ __forceinline__ unsigned odd_columns(const CacheView& c, int64_t group, int key, int g) {
+  constexpr int kCols = D / 16, kBlocks = D / 32;
+  if (c.v_scales[(group * kBlocks + g * kBlocks / 4) * 8 + key] >= kHugeScale<FP8>) return ~0u;
+  unsigned odd = 0;
+  if constexpr (FP8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint8_t* p = c.v_codes + ((group * 16 + 4 * g + i) * 8 + key) * kCols;
+#pragma unroll
+      for (int j = 0; j < kCols / 4; ++j)  // (the product gathers the four bytes' bits at 24 .. 27, no two terms meet)
+        odd |= (nan_codes(reinterpret_cast<const unsigned*>(p)[j]) >> 7) * 0x01020408u >> 24 << (kCols * i + 4 * j);
+    }
+  }
+  return odd;
+}
+
 // Which of keys key .. key + 7 a row sees, as bits: those under `limit`, and of the new
 // tokens those in its words of the tree (none if words = 0).  Straight-line code: loads are
 // clamped to the row's words instead of branched around.
@@ -333,17 +359,18 @@ __device__ __forceinline__ unsigned seen8(int limit, const int64_t* bits, int ke
 
 // Joins and stores: D / 16 columns from D / 16 * c of row i of the sequence, as output if the
 // sequence is whole in this workgroup, else as a piece.  o are sums of probabilities times codes'
-// values, `rounded` the sum of the probabilities, ref their base-2 reference, sum the unrounded sum.
+// values, `rounded` the sum of the probabilities, ref their base-2 reference, sum the unrounded sum; columns
+// whose bit of `odd` is set are NaN.
 template <int D, bool FP8>
 __device__ __forceinline__ void store_columns(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& seq, int i,
                                               int head, int c, bool whole, int64_t piece, float ref, float sum,
-                                              float rounded, bool bad, const float (&o)[D / 16]) {
+                                              float rounded, unsigned odd, const float (&o)[D / 16]) {
   constexpr int kCols = D / 16;
   const bool empty = is_zero(rounded);
   const float norm = whole ? (empty ? 0.0f : (FP8 ? 1.0f : 1.0f / 6.0f) / rounded) : 1.0f;
   float x[kCols];
 #pragma unroll
-  for (int j = 0; j < kCols; ++j) x[j] = bad ? as_float(0x7fc00000u) : o[j] * norm;
+  for (int j = 0; j < kCols; ++j) x[j] = odd >> j & 1 ? as_float(0x7fc00000u) : o[j] * norm;
   if (whole) {
     const int t = divide(i, a.G);
     const int64_t at = (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
   __shared__ v4i k_lds[kTiles][2][F::kSteps][64];  // [tile][half][step of d][lane]
   __shared__ uint2 v_lds[kTiles][F::kDTiles][2][64];  // [tile][product][keys 0-3, 4-7 of eight][lane]
   __shared__ __attribute__((aligned(16))) uint8_t code_lds[kRing][kWaves][Codes::kSize];
-  __shared__ unsigned huge_lds[kTiles][2];  // [tile][keys 0-3, 4-7 of eight]: a non-finite V block that some row sees
+  __shared__ unsigned odd_lds[kTiles][2];  // [tile][keys 0-3, 4-7 of eight]: V that is no number, of a key that some row may see
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   fetch_arguments(a, plan);
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       for (int s = 0; s < F::kSteps; ++s) asm volatile("" : "+v"(q[r][s]));
     v4f acc[kNr][F::kDTiles];
     v4f sum16[kNr];
-    unsigned poisoned = 0;
+    unsigned poisoned[kNr];  // this lane's columns (odd_columns) in which the row sees a V that is no number
     float ref[kNr], sum[kNr];
 #pragma unroll
     for (int r = 0; r < kNr; ++r) {
@@ -176,6 +176,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       sum16[r] = v4f{0, 0, 0, 0};
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
+      poisoned[r] = 0;
     }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
     auto pages_of = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
@@ -202,13 +203,13 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
       if (key0 + kTile > part.common || !page0 || !page1) {
         // Keys that no row sees hold anything: their V codes and scales become zero.  A
-        // non-finite block of the others becomes zero too, and is looked for by the rows.
+        // non-finite block of the others becomes zero too, as a NaN code of MXFP8 does, and is looked for by the rows.
         const unsigned there = (g >= 2 ? page1 : page0) ? below(part.end - (key0 + 8 * g)) >> (4 * half) : 0u;
-        bool huge = false;
+        unsigned odd = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const bool in = there >> j & 1, big = (raw.v_scales >> (8 * j) & 255u) >= kHugeScale<FP8>;
-          huge |= in && big;
+          odd |= in && big ? 1u : 0u;
           const unsigned keep = in && !big ? ~0u : 0u;
           raw.v_scales &= keep | ~(255u << (8 * j));
           if constexpr (Codes::kWords >= 4) {
@@ -218,8 +219,15 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
             raw.v[j / 2] &= keep | (j % 2 ? 0x0000ffffu : 0xffff0000u);
           }
         }
-        const bool any = __any(huge);
-        if (lane == 0) huge_lds[my_tile][half] = any;
+        if constexpr (FP8)
+#pragma unroll
+          for (int i = 0; i < Codes::kWords; ++i) odd |= nan_codes(raw.v[i]);
+        const bool any = __any(odd);
+        if (lane == 0) odd_lds[my_tile][half] = any;
+        if constexpr (FP8)
+          if (any)
+#pragma unroll
+            for (int i = 0; i < Codes::kWords; ++i) raw.v[i] = without_nan_codes(raw.v[i]);
       }
       const unsigned sc[2] = {raw.v_scales, 0};
       float scale[4];
@@ -281,17 +289,16 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
               s[r][tile][j / 4][j % 4] = see[r] >> j & 1 ? s[r][tile][j / 4][j % 4] : -__builtin_inff();
           }
           const bool looked = first + kTile > part.common || !page0 || !page1;  // as convert did
-          if (looked && (huge_lds[tile][0] | huge_lds[tile][1])) {  // lane group g holds outputs of d block g (d = 64: g / 2)
+          if (looked && (odd_lds[tile][0] | odd_lds[tile][1])) {
 #pragma unroll
             for (int r = 0; r < kNr; ++r) see[r] = groups_or(see[r] << (8 * g));
-            const int blk = g * F::kBlocks / 4;
             for (int k = 0; k < kTile; ++k) {
               const int page = k >= 16 ? pages[tile].p1 : pages[tile].p0, key = first + k;
               if (!is_page(a.c, page) || key >= part.end) continue;
               const int64_t group = row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
-              const bool big = a.c.v_scales[(group * F::kBlocks + blk) * 8 + (k & 7)] >= kHugeScale<FP8>;
+              const unsigned columns = odd_columns<D, FP8>(a.c, group, k & 7, g);
 #pragma unroll
-              for (int r = 0; r < kNr; ++r) poisoned |= big ? (see[r] >> k & 1) << r : 0u;
+              for (int r = 0; r < kNr; ++r) poisoned[r] |= see[r] >> k & 1 ? columns : 0u;
             }
           }
         }
@@ -393,7 +400,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
         for (int t = 0; t < F::kDTiles; ++t) o[t] = acc[r][t][j];
         store_columns<D, FP8>(a, plan, seq, i, head, 4 * g + j, part.whole, piece, ref[r], total, sum16[r][0],
-                              (poisoned >> r & 1) != 0, o);
+                              poisoned[r] >> F::kDTiles * j, o);
       }
     }
     if (!next_tile(a, plan, part.stop, range)) break;

@@ -853,3 +853,38 @@ def test_more_key_heads_than_ranges(fa, d, fp8, H, G, new):
     assert size(c, H * G, 2, b.table.shape[1], max(new)) == 0 and size(c, H * G, 2, 16, max(new)) == 0
     lse = torch.empty((sum(new), H * G), device="cuda")
     b.check(b.call(fa, lse=lse), lse)
+
+
+@pytest.mark.parametrize("width", [1, 6000])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,idle", [(2, 0), (5, 0), (20, 0), (20, 512)])
+def test_hidden_nan_codes_in_every_tiling(fa, d, G, idle, width):
+    """NaN codes of MXFP8 values under ordinary scales: the rows that see them are NaN in their channels, and
+    no other row or channel changes; with a tree, causal, and before the new tokens."""
+    b = Batch([190], [6], 2, G, d, True, 16, seed=9)
+    if idle or width > 1:
+        _beside_idle(b, idle, width)
+    prefix = 184
+    tree = np.array([0b1, 0b11, 0b101, 0b1000, 0b10001, 0b100000], dtype=np.int64)
+    clean = {True: b.call(fa, tree=tree), False: b.call(fa)}
+    part = d // 16
+    codes = [(1, 0, 37, 0x7F), (4, 1, 3, 0xFF), (4, 1, d - 1, 0x7F), (4, 1, d - 2, 0xFF), (0, 1, 20, 0xFF)]
+    for token, head, channel, code in codes:
+        p, off = divmod(int(b.slots[0][prefix + token]), 16)
+        b.cache[2][p, head, off // 8, channel // part, off % 8, channel % part] = code
+    for with_tree in (True, False):
+        out = b.call(fa, tree=tree if with_tree else None)
+        bad = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+        for token, head, channel, _ in codes:
+            for row in range(6):
+                if (int(tree[row]) >> token & 1) if with_tree else token <= row:
+                    bad[row, head * G:(head + 1) * G, channel] = True
+        assert torch.equal(torch.isnan(out), bad), with_tree
+        assert torch.equal(out[~bad], clean[with_tree][~bad]), with_tree
+    for token in (0, 100, 183):   # of the prefix: every row sees it
+        p, off = divmod(int(b.slots[0][token]), 16)
+        b.cache[2][p, 1, off // 8, token % 16, off % 8, 1] = 0x7F
+        bad[:, G:, token % 16 * part + 1] = True
+    out = b.call(fa)
+    assert torch.equal(torch.isnan(out), bad)
+    assert torch.equal(out[~bad], clean[False][~bad])
