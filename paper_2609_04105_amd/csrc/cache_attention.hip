@@ -74,11 +74,11 @@ struct Tile {
 };
 
 // Joins the waves' results of row i and columns D / 16 * c ..  lds: [wave][product][row, 4 g + i];
-// stat: the row's {reference, sum, sum of the rounded values} of the first wave, 16 rows apart; poison:
-// its marks (four c's), 64 words apart.
+// stat: the row's {reference, sum, sum of the rounded values} of the first wave, 16 rows apart;
+// odd_marks: its marks, 64 words apart.
 template <int D, bool FP8>
 __device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& seq,
-                                           const float* lds, const float* stat, const unsigned* poison, int i, int c,
+                                           const float* lds, const float* stat, const unsigned* odd_marks, int i, int c,
                                            int head, bool whole, int64_t piece) {
   constexpr int kCols = D / 16;
   if (i >= seq.tokens * a.G) return;
@@ -93,11 +93,11 @@ __device__ __forceinline__ void join_waves(const CacheAttentionArgs& a, const Ca
     const float ref = stat[w * 64], part = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
     sum += stat[w * 64 + 1] * part;
     rounded += stat[w * 64 + 2] * part;
-    odd |= poison[w * 64];
+    odd |= odd_marks[w * 64];
 #pragma unroll
     for (int j = 0; j < kCols; ++j) o[j] += lds[(w * kCols + j) * 256 + threadIdx.x] * part;
   }
-  store_columns<D, FP8>(a, plan, seq, i, head, c, whole, piece, top, sum, rounded, odd >> kCols * (c % 4), o);
+  store_columns<D, FP8>(a, plan, seq, i, head, c, whole, piece, top, sum, rounded, FP8 ? odd >> kCols * (c % 4) : odd, o);
 }
 
 template <int D, bool FP8, int NR>
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
   constexpr int kAccWords = kWaves * F::kDTiles * 64, kQWords = kSharedQ ? NR * F::kSteps * 64 : 0;
   __shared__ float4 lds[kAccWords > kQWords ? kAccWords : kQWords];
   __shared__ float4 lds_stat[kWaves][16];
-  __shared__ unsigned lds_poison[kWaves][64];
+  __shared__ unsigned lds_odd[kWaves][64];
   v4i* lds_q = reinterpret_cast<v4i*>(lds);
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
     }
     v4f acc[NR][F::kDTiles];
     v4f sum16[NR];  // the rounded probabilities (the same in all four)
-    unsigned poisoned[NR];     // this lane's columns (odd_columns) in which the row sees a V that is no number
+    OddMarks<FP8, NR> odd_marks;
     float ref[NR], sum[NR];    // base 2, lags the maximum by at most kLag; this lane's own keys
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
@@ -175,7 +175,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       sum16[r] = v4f{0, 0, 0, 0};
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
-      poisoned[r] = 0;
     }
 
     // The wave's tiles.  One set of registers: a tile's K is loaded when the one before has
@@ -255,7 +254,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
               const int64_t group = row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
               const unsigned columns = odd_columns<D, FP8>(a.c, group, k & 7, g);
 #pragma unroll
-              for (int r = 0; r < NR; ++r) poisoned[r] |= see[r] >> k & 1 ? columns : 0u;
+              for (int r = 0; r < NR; ++r) odd_marks.add(r, see[r] >> k & 1, columns);
             }
           }
         }
@@ -326,10 +325,10 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       for (int t = 0; t < F::kDTiles; ++t)
         lds[(wave * F::kDTiles + t) * 64 + m * 4 + g] = float4{acc[r][t][0], acc[r][t][1], acc[r][t][2], acc[r][t][3]};
       if (g == 0) lds_stat[wave][m] = float4{ref[r], total, sum16[r][0], 0.0f};
-      lds_poison[wave][m * 4 + g] = poisoned[r];
+      lds_odd[wave][m * 4 + g] = odd_marks.template of<0>(r, 0);
       __syncthreads();
       join_waves<D, FP8>(a, plan, seq, reinterpret_cast<const float*>(lds), &lds_stat[0][row].x,
-                         &lds_poison[0][row * 4 + (c >> 2)], row0 + 16 * r + row, c, head, part.whole,
+                         &lds_odd[0][row * 4 + (c >> 2)], row0 + 16 * r + row, c, head, part.whole,
                          partial_row(a, plan, place.w, part.first ? 1 : 0, head) + 16 * r + row);
     }
     if (!next_tile(a, plan, part.stop, range)) break;

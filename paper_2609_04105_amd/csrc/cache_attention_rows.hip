@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       for (int s = 0; s < F::kSteps; ++s) asm volatile("" : "+v"(q[r][s]));
     v4f acc[kNr][F::kDTiles];
     v4f sum16[kNr];
-    unsigned poisoned[kNr];  // this lane's columns (odd_columns) in which the row sees a V that is no number
+    OddMarks<FP8, kNr> odd_marks;
     float ref[kNr], sum[kNr];
 #pragma unroll
     for (int r = 0; r < kNr; ++r) {
@@ -176,7 +176,6 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       sum16[r] = v4f{0, 0, 0, 0};
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
-      poisoned[r] = 0;
     }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
     auto pages_of = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
               const int64_t group = row_of(a.c, page, head, key & ((1 << a.c.page_shift) - 1)) >> 3;
               const unsigned columns = odd_columns<D, FP8>(a.c, group, k & 7, g);
 #pragma unroll
-              for (int r = 0; r < kNr; ++r) poisoned[r] |= see[r] >> k & 1 ? columns : 0u;
+              for (int r = 0; r < kNr; ++r) odd_marks.add(r, see[r] >> k & 1, columns);
             }
           }
         }
@@ -400,7 +399,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
         for (int t = 0; t < F::kDTiles; ++t) o[t] = acc[r][t][j];
         store_columns<D, FP8>(a, plan, seq, i, head, 4 * g + j, part.whole, piece, ref[r], total, sum16[r][0],
-                              poisoned[r] >> F::kDTiles * j, o);
+                              odd_marks.template of<F::kDTiles>(r, j), o);
       }
     }
     if (!next_tile(a, plan, part.stop, range)) break;
