@@ -385,8 +385,10 @@ __device__ __forceinline__ void store_columns(const CacheAttentionArgs& a, const
   const bool empty = is_zero(rounded);
   const float norm = whole ? (empty ? 0.0f : (FP8 ? 1.0f : 1.0f / 6.0f) / rounded) : 1.0f;
   float x[kCols];
+  unsigned nan = 0x7fc00000u;  // as bits: a compiler told that there are no NaNs may drop the choice of one
+  asm("" : "+v"(nan));
 #pragma unroll
-  for (int j = 0; j < kCols; ++j) x[j] = (FP8 ? odd >> j & 1 : odd) ? as_float(0x7fc00000u) : o[j] * norm;
+  for (int j = 0; j < kCols; ++j) x[j] = as_float((FP8 ? odd >> j & 1 : odd) ? nan : as_uint(o[j] * norm));
   if (whole) {
     const int t = divide(i, a.G);
     const int64_t at = (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
