@@ -272,7 +272,7 @@ fp4attn_status check_cache_attention(const fp4attn::CacheView& c, int64_t q_head
   if (q_heads > 0x7fffffff || max_q > 0x7fffffff / q_heads)
     return fail(FP4ATTN_ERR_UNSUPPORTED, "max_q=%lld tokens of %lld heads are too many", (long long)max_q,
                 (long long)q_heads);
-  *plan = fp4attn::cache_plan(B, c.H, q_heads / c.H, c.d, max_q, max_pages << c.page_shift);
+  *plan = fp4attn::cache_plan(B, c.H, q_heads / c.H, c.d, c.fp8 != 0, max_q, max_pages << c.page_shift);
   if (!plan->fits)
     return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_q=%lld max_pages=%lld: too many workgroups for one launch", (long long)B,
                 (long long)max_q, (long long)max_pages);

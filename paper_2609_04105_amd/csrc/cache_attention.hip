@@ -414,7 +414,7 @@ void launch_format(const CacheAttentionArgs& a, const CachePlan& plan, hipStream
 }  // namespace
 
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream) {
-  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
+  const CachePlan plan = cache_plan(a.B, a.c.H, a.G, a.c.d, a.c.fp8 != 0, a.max_q, (int64_t)a.max_pages << a.c.page_shift);
   if (a.c.d == 64 && a.c.fp8) launch_format<64, true>(a, plan, stream);
   else if (a.c.d == 64) launch_format<64, false>(a, plan, stream);
   else if (a.c.fp8) launch_format<128, true>(a, plan, stream);

@@ -31,20 +31,28 @@ constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 // sequences of 16384 keys and 8 key heads; at three waves 140.)
 constexpr int waves_per_simd(int d, int nr) { return 6 - d / 64 - nr; }
 
-inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, int64_t max_q, int64_t max_keys) {
+inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t max_keys) {
   CachePlan p{};
   const int64_t rows = max_q * G, units = (max_keys + kUnit - 1) / kUnit;
   auto tiles_of = [&](int64_t tile) { return (rows + tile - 1) / tile; };
   // Rows of a tile.  Up to 16 rows the matrix products have one column tile of them.  More: the 128-row
-  // kernel converts a key's codes once for 128 rows, the other once for 32, but it needs more work to
-  // fill the chip: two workgroups of 128 rows for every CU with d = 64 (half the products to a conversion), one
-  // with d = 128, half of one if there are many keys to cut up.  MXFP4, 8 key heads of 8 query heads, us at tile 32 / 128:
-  //   d = 128, 32 sequences, 64 tokens (1024 workgroups of 128 rows), 2048 keys 184 / 154, 12 (384), 1024 keys 57 / 46;
+  // kernel converts a key's codes once for 128 rows, the other once for 32, but
+  // - it needs more work to fill the chip: rows for two workgroups on every CU with d = 64 (half the products to a
+  //   conversion), for one with d = 128, for half of one if there are many keys to cut up;
+  // - a workgroup takes as long with few of its rows in use as with all, as long as three 32-row tiles with d = 64,
+  //   two with d = 128, and in a full chip one with MXFP8, whose codes are twice the bytes.
+  // 8 key heads of 8 query heads, us at tile 32 / 128:
+  //   d = 128, MXFP4, 32 sequences, 64 tokens (rows for 1024 workgroups), 2048 keys 184 / 154, 12 (384), 1024 keys 57 / 46;
   //   24 sequences, 16 tokens (192), 4096 keys 89 / 84, 8192 keys 149 / 135, 2048 keys 53 / 54, 1024 keys 36 / 38;
   //   16 sequences, 16 tokens (128), 8192 keys MXFP4 96 / 95, MXFP8 145 / 108, 4096 keys 60 / 63;
-  //   d = 64, 16 sequences, 64 tokens (512), 1024 keys 45 / 39, 4096 keys 121 / 125; 32, 16 tokens (256), 2048 keys 44 / 53.
-  const int64_t wide = B * H * tiles_of(kRowsTile);
-  const bool rows128 = wide >= 512 || (d == 128 && (wide >= 256 || (wide >= 128 && wide * max_keys >= 3 << 18)));
+  //   64 sequences, 4096 keys, MXFP4: 4 tokens 78 / 138, 8 126 / 158, 10 164 / 163, 12 173 / 165, 16 222 / 175; MXFP8: 110 / 149,
+  //   203 / 162, 247 / 171, 275 / 171, 336 / 184; 32 sequences, MXFP4, 4 tokens 45 / 85, 8 71 / 97, 10 86 / 102, 16 118 / 109;
+  //   d = 64, 16 sequences, 64 tokens (512), 1024 keys 45 / 39, 4096 keys 121 / 125; 32, 16 tokens (256), 2048 keys 44 / 53;
+  //   64 sequences, 1024 keys, 4 tokens 18 / 35, 12 40 / 40, 16 51 / 40, 17 51 / 76, 24 67 / 76, 32 92 / 77.
+  const int64_t wide = B * H * rows / kRowsTile;  // workgroups of 128 rows, if all are in use
+  const int64_t least = d == 64 ? 3 : (fp8 && wide >= 256 ? 1 : 2);
+  const bool rows128 = tiles_of(32) > least * tiles_of(kRowsTile) &&
+                       (wide >= 512 || (d == 128 && (wide >= 256 || (wide >= 128 && wide * max_keys >= 3 << 18))));
   p.tile = rows <= 16 ? 16 : (rows128 ? kRowsTile : 32);
   const int64_t row_tiles = tiles_of(p.tile);
   p.row_tiles = (int)row_tiles;

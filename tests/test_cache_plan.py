@@ -15,7 +15,7 @@ pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ is not 
 
 @pytest.fixture(scope="module")
 def plans(tmp_path_factory):
-    """plans(calls) -> a Plan for each (B, heads, query heads a head, d, max_q, max_keys)."""
+    """plans(calls) -> a Plan for each (B, heads, query heads a head, d, fp8, max_q, max_keys)."""
     exe = tmp_path_factory.mktemp("plan") / "cache_plan"
     res = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror",
                           os.path.join(ROOT, "tests", "cache_plan.cpp"), "-o", str(exe)],
@@ -23,7 +23,7 @@ def plans(tmp_path_factory):
     assert res.returncode == 0, res.stderr
 
     def ask(calls):
-        run = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True,
+        run = subprocess.run([str(exe)], input="\n".join(" ".join(str(int(x)) for x in c) for c in calls), capture_output=True,
                              text=True, timeout=60)
         assert run.returncode == 0
         got = [Plan(*map(int, line.split())) for line in run.stdout.splitlines()]
@@ -40,13 +40,13 @@ def _calls():
             for B in (1, 3, 64, 1000):
                 for G, max_q in ((1, 1), (7, 1), (16, 1), (8, 3), (1, 64), (8, 64), (4, 513)):
                     for keys in (16, 1024, 1040, 1600, 2064, 8192, 1 << 20):
-                        yield B, H, G, d, max_q, keys
+                        yield B, H, G, d, (B + H) % 2 == 0, max_q, keys
 
 
 def test_tiles_cover_the_rows(plans):
     calls = list(_calls())
     for c, p in zip(calls, plans(calls)):
-        B, H, G, d, max_q, keys = c
+        B, H, G, d, fp8, max_q, keys = c
         rows = max_q * G
         assert p.tile in (16, 32, 128) and (p.tile > 16) == (rows > 16), c
         assert p.row_tiles == -(-rows // p.tile) and p.tile_rows == min(rows, p.tile), c
@@ -61,9 +61,43 @@ def test_cut_calls_have_a_workspace(plans):
     calls = list(_calls())
     cut = 0
     for c, p in zip(calls, plans(calls)):
-        B, H, G, d, max_q, keys = c
+        B, H, G, d, fp8, max_q, keys = c
         if p.split:
             cut += 1
             assert p.ranges >= 2, c
             assert p.workspace >= 16 * p.ranges + 2 * p.ranges * H * p.tile_rows * (4 * d + 16), c
     assert cut > len(calls) // 10
+
+
+def test_tile_follows_the_rows_in_use(plans):
+    """8 key heads of 8 query heads: the tile measured faster, by 6 % or more, of 32 and 128 rows."""
+    points = [(32, 128, False, 4, 1024, 32), (32, 128, False, 4, 4096, 32), (32, 128, False, 8, 1024, 32),
+              (32, 128, False, 8, 4096, 32), (32, 128, False, 10, 4096, 32), (32, 128, False, 16, 1024, 128),
+              (32, 128, False, 32, 4096, 128), (32, 128, True, 4, 4096, 32), (32, 128, True, 8, 4096, 32),
+              (32, 128, True, 16, 4096, 128), (64, 128, False, 3, 4096, 32), (64, 128, False, 4, 4096, 32),
+              (64, 128, False, 6, 4096, 32), (64, 128, False, 8, 4096, 32), (64, 128, False, 10, 1024, 128),
+              (64, 128, False, 12, 1024, 128), (64, 128, False, 16, 4096, 128), (64, 128, True, 4, 4096, 32),
+              (64, 128, True, 8, 4096, 128), (64, 128, True, 12, 4096, 128), (160, 128, False, 4, 2048, 32),
+              (160, 128, False, 8, 2048, 32), (160, 128, False, 10, 512, 128), (160, 128, True, 4, 512, 32),
+              (160, 128, True, 6, 512, 128), (160, 128, True, 8, 2048, 128), (48, 128, False, 8, 4096, 32),
+              (48, 128, True, 8, 1024, 32), (48, 128, True, 12, 4096, 128), (24, 128, False, 16, 8192, 128),
+              (16, 128, False, 8, 12288, 32), (16, 128, False, 20, 4096, 32), (64, 64, False, 4, 1024, 32),
+              (64, 64, False, 16, 1024, 128), (64, 64, False, 17, 1024, 32), (64, 64, False, 24, 1024, 32),
+              (64, 64, False, 32, 1024, 128), (160, 64, False, 8, 512, 32), (160, 64, True, 16, 2048, 128),
+              (32, 64, False, 16, 4096, 32), (64, 64, True, 8, 4096, 32), (64, 64, True, 17, 1024, 32)]
+    got = plans([(B, 8, 8, d, fp8, tokens, keys) for B, d, fp8, tokens, keys, _ in points])
+    for point, p in zip(points, got):
+        assert p.tile == point[-1], point
+
+
+def test_gpu_tables_reach_every_kernel(plans):
+    """The batches of the GPU tests that plant hidden values run every kernel of each format, cut and whole."""
+    from test_gpu_serving import FULL_TILES, HIDDEN_TOKENS
+    for d in (64, 128):
+        for fp8 in (False, True):
+            seen = set()
+            for G, idle in ((2, 0), (5, 0), (20, 0), (20, FULL_TILES)):
+                for keys in (256, 6000):
+                    p = plans([(1 + -(-idle // 2), 2, G, d, fp8, HIDDEN_TOKENS, keys)])[0]
+                    seen.add((p.tile, p.split))
+            assert seen == {(t, s) for t in (16, 32, 128) for s in (0, 1)}, (d, fp8)

@@ -888,3 +888,16 @@ def test_hidden_nan_codes_in_every_tiling(fa, d, G, idle, width):
     out = b.call(fa)
     assert torch.equal(torch.isnan(out), bad)
     assert torch.equal(out[~bad], clean[False][~bad])
+
+
+HIDDEN_TOKENS = 6    # drafted tokens of the batches with hidden values
+FULL_TILES = 1100    # row tiles of idle sequences beside them that fill the chip for every format
+
+
+@pytest.mark.parametrize("width", [1, 6000])
+@pytest.mark.parametrize("d,fp8", FORMATS)
+def test_hidden_values_in_a_full_chip(fa, d, fp8, width):
+    """The hidden values of the tests above in the kernel of 128 rows, for every format."""
+    test_hidden_and_missing_in_every_tiling(fa, d, fp8, 20, FULL_TILES, width)
+    if fp8:
+        test_hidden_nan_codes_in_every_tiling(fa, d, 20, FULL_TILES, width)
