@@ -316,9 +316,10 @@ fp4attn_status fp4attn_rotary(const void* x, void* out, int dtype, int64_t B, in
  *            i of d (D/16 values), then the token: the attention's operand order
  *   v_scales [pages, heads, page_size/8, head_dim/32, 8]
  *
- * struct_size must equal sizeof(fp4attn_cache).  Attention reads V blocks of amplitude 2^126
- * or more (fp8: 2^120), and K values that pass the bf16 range at 6 times their size (fp8: at their
- * size), as non-finite.
+ * struct_size must equal sizeof(fp4attn_cache).  Attention works in bf16, whose range it leaves for K
+ * values of 2^128 / 6 or more (fp8: 2^128) and may leave for V blocks of amplitude 2^126 or more (fp8:
+ * 2^120): rows that see such a V block may be non-finite in its 32 channels.  fp4attn_cache_read gives
+ * the finite values.
  */
 typedef struct fp4attn_cache {
   uint32_t struct_size;
@@ -337,8 +338,8 @@ typedef struct fp4attn_cache {
  * Quantizes n tokens into the cache: token i of k and v ([heads, head_dim] contiguous,
  * tokens k_stride and v_stride elements apart) into slot slots[i].  A slot outside
  * [0, pages * page_size) marks a padding token, which is skipped.  Other slots keep
- * their bytes.  A slot that occurs twice in one call ends with bytes of either token, no
- * other slot is touched by that.
+ * their bytes.  A slot that occurs twice in one call ends with bytes of either token, codes and
+ * scales mixed; no other slot is touched by that.
  *
  * Errors: those of the cache (below), INVALID_ARG for null or misaligned pointers,
  * n < 0, strides negative or no multiple of 16 bytes, a bad src_dtype; UNSUPPORTED for more
@@ -366,8 +367,10 @@ fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slo
  *   q           [n, q_heads, head_dim] bf16, tokens q_stride elements apart; query head h
  *               reads key head h / (q_heads / heads)
  *   page_table  [B, max_pages] int32: key j of sequence b is in page
- *               page_table[b][j / page_size], place j % page_size.  Only entries of pages
- *               that hold keys are read; keys in a page outside the cache do not exist.
+ *               page_table[b][j / page_size], place j % page_size.  Entries of pages that
+ *               hold no key may hold anything; keys in a page outside the cache do not exist.
+ *               max_pages (the table's width) chooses the launch before the lengths are known:
+ *               a table no wider than the longest sequence needs is the fastest.
  *   lengths     [B] int32: keys of each sequence, its new tokens included (below 0: 0;
  *               keys past max_pages * page_size do not exist)
  *   q_starts    [B + 1] int32, ascending: sequence b's tokens are rows q_starts[b] ..
@@ -384,7 +387,9 @@ fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slo
  *               NULL for 0 bytes); calls that may run at the same time need one each
  *
  * A row that sees no key gets zeros and -inf.  Keys that a row does not see never reach
- * it, whatever they hold.  P is rounded to bf16 for the PV product.  n = 0: no work.
+ * it, whatever they hold.  P is rounded to bf16 for the PV product, which moves an output by up to
+ * 2^-8 of the weighted mean of |v - o|.  out, lse and workspace must not overlap each other or the
+ * inputs.  n = 0: no work.
  *
  * Errors: those of the cache, INVALID_ARG for null or misaligned pointers, sizes < 1,
  * q_heads no multiple of heads, a q_stride that is negative or no multiple of 8,

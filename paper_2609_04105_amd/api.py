@@ -551,6 +551,9 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
     has n / B tokens; with it (int32 [B + 1]) sequence b has rows ``q_starts[b]`` to
     ``q_starts[b + 1]``, at most ``max_q`` of them, and other rows of ``out`` and ``lse`` are left as they were.
 
+    The table's width chooses the launch before the lengths are known: one no wider than the
+    longest sequence needs is the fastest.
+
     Token t of T sees the keys up to its own, or with ``tree`` (int64 [n], or [n, words] for more
     than 64 tokens) the keys before the new tokens and the new tokens u whose bit is set.
     ``lse`` (fp32 [n, Hq]) receives the log normaliser.  A row that sees no key is 0 (-inf)."""
