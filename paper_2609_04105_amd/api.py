@@ -404,13 +404,31 @@ def rotary_frequencies(rotary_dim, base=10000.0, scaling=None, factor=1.0, origi
     return freq.to(device), magnitude
 
 
+class _Rotary(torch.autograd.Function):
+    """:func:`rotary` with its gradient, the turn back of the result's gradient."""
+
+    @staticmethod
+    def forward(ctx, x, positions, inv_freq, interleaved, magnitude, inverse):
+        y = rotary(x, positions, inv_freq, interleaved, magnitude, inverse)
+        ctx.save_for_backward(positions, inv_freq)
+        ctx.back = (interleaved, magnitude, not inverse)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        return (rotary(dy.contiguous(), *ctx.saved_tensors, *ctx.back), *(None,) * 5)
+
+
 def rotary(x, positions, inv_freq, interleaved=False, magnitude=1.0, inverse=False, out=None):
     """Rotary positions on ``x`` (bf16 or fp32): [n, H, d] with ``positions`` [n], or [B, H, N, d]
     with ``positions`` [N] or [B, N] (int64).  The first ``2 * len(inv_freq)`` channels of
     every head turn by ``position * inv_freq[j]`` (fp64, :func:`rotary_frequencies`); pairs are
     (j, j + r / 2), or (2 j, 2 j + 1) with ``interleaved``.  ``inverse`` turns back: applied
-    to the gradient of the result it gives the gradient of ``x``.  ``x`` may have any strides
-    with d contiguous; ``out`` may be ``x`` (in place)."""
+    to the gradient of the result it gives the gradient of ``x``, which is what autograd does for an ``x``
+    that requires one (``positions`` and ``inv_freq`` have none).  ``x`` may have any strides
+    with d contiguous; ``out`` may be ``x`` (in place), and autograd does not see what is written to it."""
+    if out is None and getattr(x, "requires_grad", False) and torch.is_grad_enabled():
+        return _Rotary.apply(x, positions, inv_freq, interleaved, magnitude, inverse)
     r = _binding.rotary(x, positions, inv_freq, interleaved, magnitude, inverse, out)
     if r is not None:
         return _native(r)

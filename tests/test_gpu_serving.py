@@ -901,3 +901,43 @@ def test_hidden_values_in_a_full_chip(fa, d, fp8, width):
     test_hidden_and_missing_in_every_tiling(fa, d, fp8, 20, FULL_TILES, width)
     if fp8:
         test_hidden_nan_codes_in_every_tiling(fa, d, 20, FULL_TILES, width)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("shape", [(2, 3, 5, 64), (7, 4, 64)])
+def test_rotary_under_autograd(fa, shape, interleaved, dtype):
+    """A leaf's gradient through rotary is the inverse turn of the result's, whatever the strides of the latter;
+    against autograd on the formula in fp64; twice differentiated; and without a graph the same values."""
+    g = torch.Generator().manual_seed(len(shape))
+    x, dy = (torch.randn(shape, generator=g).to(dtype) for _ in range(2))
+    n = shape[0] if len(shape) == 3 else shape[2]
+    at = torch.randint(0, 100000, (n,), generator=g)
+    freq = fa.rotary_frequencies(48, device="cpu")[0]
+    o = dict(interleaved=interleaved, magnitude=0.8)
+    args = at.cuda(), freq.cuda()
+    leaf = x.cuda().requires_grad_()
+    y = fa.rotary(leaf, *args, **o)
+    assert y.requires_grad
+    with torch.no_grad():
+        plain = fa.rotary(leaf, *args, **o)
+    assert not plain.requires_grad and torch.equal(plain, y)
+    back = fa.rotary(dy.cuda(), *args, inverse=True, **o)
+    assert not back.requires_grad
+    grad, = torch.autograd.grad(y, leaf, dy.cuda(), retain_graph=True)
+    assert torch.equal(grad, back)
+    strided = dy.cuda().transpose(0, 1).contiguous().transpose(0, 1)
+    assert torch.equal(torch.autograd.grad(y, leaf, strided, retain_graph=True)[0], back)
+    ones = torch.autograd.grad(y.sum(), leaf, retain_graph=True)[0]   # an expanded gradient
+    assert torch.equal(ones, fa.rotary(torch.ones_like(leaf, requires_grad=False), *args, inverse=True, **o))
+    # the formula: [n, H, d] as [1, H, n, d]
+    def heads_first(t):
+        return t.transpose(0, 1)[None] if len(shape) == 3 else t
+    _check_rotary(_f64(heads_first(grad)), _f64(heads_first(dy)), at.numpy(), freq.numpy(), dtype, inverse=True, **o)
+    # linear: the gradient of <grad, w> with respect to dy is rotary of w
+    v = dy.cuda().requires_grad_()
+    w = torch.randn(shape, generator=g).to(dtype).cuda()
+    grad, = torch.autograd.grad(y, leaf, v, create_graph=True)
+    assert torch.equal(torch.autograd.grad(grad, v, w)[0], fa.rotary(w, *args, **o))
+    turned_back = fa.rotary(leaf, *args, inverse=True, **o)
+    assert torch.equal(torch.autograd.grad(turned_back, leaf, dy.cuda())[0], fa.rotary(dy.cuda(), *args, **o))
