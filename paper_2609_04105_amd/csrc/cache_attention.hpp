@@ -111,7 +111,9 @@ __device__ __forceinline__ int row_tiles_of(const CacheAttentionArgs& a, const C
 
 // The row tiles of all sequences laid end to end in one line, each as kSetup places for what
 // starting one costs and then its keys' units; range w takes places [w per, (w + 1) per): equal parts
-// for every workgroup, whatever the lengths and the numbers of rows.  (Places to a start, 64 sequences of 128 to
+// for every workgroup, whatever the lengths and the numbers of rows.  A causal row tile has places for all keys of its
+// sequence and walks those up to its last row's: of the last 2048 of 8192 tokens the busiest workgroup has 1.14 times
+// the mean work, of a prompt of 8192 twice.  (Places to a start, 64 sequences of 128 to
 // 16384 keys: 4 47.9 us, 3 47.3, 2 48.3, 1 50.5; trees of 16 tokens over 8 of 2047 keys: 22.6, 22.2, 24.2, 25.0.)
 struct Range {
   int begin, end;

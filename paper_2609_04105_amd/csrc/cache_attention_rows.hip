@@ -11,8 +11,9 @@
 // a step; the second workgroup of a CU fills them.
 //
 // Measured, d = 128, MXFP4, 32 sequences of 8192 keys and less, trees of 64 tokens, 8 key heads of 8 query heads:
-// 357 us, 748 TFLOP/s; 2048 new tokens over 8192 keys 556 us, 989 (a large bf16 matrix product: 1170).  Counters of
-// the first: the matrix unit is busy 33 % of the time, vector instructions take 42 %, LDS 33 %; two waves a SIMD
+// 362 us, 738 TFLOP/s (a large bf16 matrix product: 1170); the last 2048 of 8192 tokens, causal, 564 us, 854 over the keys
+// that their rows see, d = 64 456 us, 527; a prompt of 8192 tokens 2101 us, 523 (its cut is uneven: cache_attention.hpp).
+// Counters of the first: the matrix unit is busy 33 % of the time, vector instructions take 42 %, LDS 33 %; two waves a SIMD
 // overlap them in part.  Work put between the products of the same wave (converting V and K, the second tile's
 // probabilities) made it 1 to 3 % slower, four sums side by side in the K products changed nothing.
 #include "cache_attention.hpp"
