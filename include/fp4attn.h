@@ -319,7 +319,7 @@ fp4attn_status fp4attn_rotary(const void* x, void* out, int dtype, int64_t B, in
  * struct_size must equal sizeof(fp4attn_cache).  Attention works in bf16, whose range it leaves for K
  * values of 2^128 / 6 or more (fp8: 2^128) and may leave for V blocks of amplitude 2^126 or more (fp8:
  * 2^120): rows that see such a V block may be non-finite in its 32 channels.  fp4attn_cache_read gives
- * the finite values.
+ * the finite values.  A block of E8M0 byte 255 is NaN, and so is a value of an E4M3 NaN code.
  */
 typedef struct fp4attn_cache {
   uint32_t struct_size;
