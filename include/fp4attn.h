@@ -411,6 +411,51 @@ int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_
                                           int64_t max_q);
 
 /*
+ * Pages and slots of a step's tokens, from the keys that each sequence held before the step and
+ * has after it: page tables grow by pages of a pool and return the pages that they no longer need.
+ *
+ *   page_table  [B, max_pages] int32, read and written.  Of sequence b, places 0 .. h - 1 hold its pages,
+ *               h = max(ceil(held[b] / page_size), shared[b] / page_size).  Other places may hold anything.
+ *   held        [B] int32: keys before the step (a new sequence: 0)
+ *   lengths     [B] int32: keys after it, the new tokens included (a sequence that ends: 0)
+ *   new_tokens  [B] int32: its new tokens, the last of its lengths[b] keys; held - (lengths - new_tokens) is what
+ *               the step takes back, as rejected drafts.  NULL: tokens / B each.
+ *   shared      [B] int32 or NULL (0): the first shared[b] / page_size pages of the row are not the sequence's own (a
+ *               prefix that others use too): they are there before it starts, and stay there
+ *   pool_pages  [pool_size] int32, read and written: free pages, in a ring: number i of all pages that
+ *               came to the pool so far is at i % pool_size.  pool_size is at least the number of pages that there are.
+ *   pool_counts [2] int64: pages taken from the pool so far, pages that came to it (the difference is free)
+ *
+ *   slots       [tokens] int64: where fp4attn_cache_write puts the tokens, sequence by sequence.  -1, which it skips: tokens
+ *               whose key lies in a shared page, before the sequence's first, or in a refused sequence; padding.
+ *   positions   [tokens] int64: of the tokens in their sequences, for fp4attn_rotary (padding, and below 0: 0)
+ *   q_starts    [B + 1] int32: the sums of new_tokens, at most `tokens`: tokens past that have no slot
+ *   lengths_out [B] int32, counts_out [2] int64: lengths and counts after the step (may be held and pool_counts themselves)
+ *   workspace   at least fp4attn_cache_assign_workspace(B) bytes, 16-byte aligned; calls that may run at
+ *               the same time need one each
+ *
+ * Pages go to the sequences in their order.  A sequence whose pages, together with all that the sequences before
+ * it asked for, exceed the pool is refused, as is one of more than max_pages pages: it keeps its
+ * row and its held[b] keys, which lengths_out tells, and takes nothing.  Pages returned in a step are for later
+ * ones.  Negative numbers count as 0, held[b] and shared[b] past the table's end as its end.
+ * Outputs must not overlap inputs or each other but for lengths_out and counts_out as above.
+ *
+ * Errors: INVALID_ARG for null or misaligned pointers, B, max_pages or pool_size < 1, tokens < 0 (0: slots and positions
+ * may be NULL), a page_size that is no power of two or below 16, tokens not a multiple of B without
+ * new_tokens, a workspace that is too small; UNSUPPORTED for B above 65535, tokens above 2^24, page_size above 2^20,
+ * max_pages * page_size above 2^30, B * max_pages or pool_size of 2^31 or more.
+ */
+fp4attn_status fp4attn_cache_assign(int32_t* page_table, int64_t B, int64_t max_pages, int64_t page_size,
+                                    const int32_t* held, const int32_t* lengths, const int32_t* new_tokens,
+                                    const int32_t* shared, int32_t* pool_pages, int64_t pool_size,
+                                    const int64_t* pool_counts, int64_t tokens, int64_t* slots, int64_t* positions,
+                                    int32_t* q_starts, int32_t* lengths_out, int64_t* counts_out, void* workspace,
+                                    int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that such a call needs; -1 for a B that it refuses. */
+int64_t fp4attn_cache_assign_workspace(int64_t B);
+
+/*
  * Test hook: runs exactly the forward kernel of fp4attn_forward_mxfp4_ex (same
  * launch configuration and arguments, `opts` NULL = the defaults, writes `out`
  * too) and additionally

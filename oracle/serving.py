@@ -89,3 +89,39 @@ def tree_mask(words, T, n, length):
         for j in np.flatnonzero((u >= 0) & (u < 64 * words.shape[1])):
             see[t, j] = bool(int(words[t, u[j] // 64]) >> int(u[j] % 64) & 1)
     return see
+
+
+def assign(table, held, lengths, ring, counts, page, tokens, new=None, shared=None):
+    """One step's pages, slots and positions, sequence by sequence.  table (a list of rows) and ring (a list) are
+    changed; returns slots, positions, starts, lengths and counts after the step."""
+    B, width = len(table), len(table[0])
+    capacity, (taken, returned) = width * page, counts
+    new = [tokens // B] * B if new is None else [max(0, n) for n in new]
+    shared = [0] * B if shared is None else [min(max(s, 0), capacity) // page for s in shared]
+    room = min(max(returned - taken, 0), len(ring))
+    slots, positions, starts, after, gone = [], [], [0], [], []
+    asked = 0
+    for b in range(B):
+        keys, want = min(max(held[b], 0), capacity), max(lengths[b], 0)
+        had, now = max(-(-keys // page), shared[b]), max(-(-want // page), shared[b])
+        served = want <= capacity
+        if served and now > had:
+            asked += now - had
+            served = asked <= room
+            for j in range(had, now if served else had):
+                table[b][j] = ring[taken % len(ring)]
+                taken += 1
+        elif served:
+            gone += table[b][now:had]
+        for t in range(min(new[b], tokens - len(slots))):
+            at = lengths[b] - new[b] + t
+            ok = served and shared[b] * page <= at < capacity
+            number = table[b][at // page] if ok else -1
+            slots.append(number * page + at % page if number >= 0 else -1)
+            positions.append(max(at, 0))
+        starts.append(len(slots))
+        after.append(want if served else keys)
+    for j, p in enumerate(gone):
+        ring[(returned + j) % len(ring)] = p
+    rest = tokens - len(slots)
+    return slots + [-1] * rest, positions + [0] * rest, starts, after, [taken, returned + len(gone)]

@@ -15,9 +15,13 @@ from ._lib import (  # noqa: F401
     lib,
 )
 from .api import (  # noqa: F401
+    CacheStep,
     KVCache,
+    KVPool,
     attention_mxfp4,
+    cache_assign,
     cache_attention,
+    cache_pool,
     cache_read,
     cache_write,
     debug_directp_mxfp4,

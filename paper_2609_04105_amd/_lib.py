@@ -44,6 +44,8 @@ SIGNATURES = {
     "fp4attn_rotary": [_c_p, _c_p, _int] + [_i64] * 4 + [_c_p] * 3 + [_i64, _c_p, _i64, _f32, _int, _int, _c_p],
     "fp4attn_cache_write": [ctypes.POINTER(Cache), _c_p, _c_p, _int, _i64, _i64, _i64, _c_p, _c_p],
     "fp4attn_cache_read": [ctypes.POINTER(Cache), _c_p, _i64, _c_p, _c_p, _int, _c_p],
+    "fp4attn_cache_assign": [_c_p, _i64, _i64, _i64] + [_c_p] * 5 + [_i64, _c_p, _i64] + [_c_p] * 6 + [_i64, _c_p],
+    "fp4attn_cache_assign_workspace": [_i64],
     "fp4attn_cache_attention": [ctypes.POINTER(Cache), _c_p, _i64, _i64, _i64, _i64, _c_p, _i64, _c_p, _c_p, _i64, _c_p,
                                 _i64, _f32, _c_p, _int, _c_p, _c_p, _i64, _c_p],
     "fp4attn_cache_attention_workspace": [ctypes.POINTER(Cache)] + [_i64] * 4,
@@ -54,7 +56,7 @@ SIGNATURES = {
 }
 RESTYPES = {"fp4attn_status_string": ctypes.c_char_p, "fp4attn_last_error": ctypes.c_char_p,
             "fp4attn_abi_version": ctypes.c_int, "fp4attn_forward_options_init": None,
-            "fp4attn_cache_attention_workspace": ctypes.c_int64}
+            "fp4attn_cache_attention_workspace": ctypes.c_int64, "fp4attn_cache_assign_workspace": ctypes.c_int64}
 
 
 class Fp4AttnError(RuntimeError):

@@ -28,7 +28,7 @@ class _NoBinding:
         return None
 
     forward = quantize_qkv = attention = forward_bf16 = _leave
-    rotary = cache_write = cache_read = cache_attention = _leave
+    rotary = cache_write = cache_read = cache_assign = cache_attention = _leave
 
 
 try:
@@ -557,6 +557,80 @@ def cache_read(cache, slots, out_dtype=torch.float32):
         _launch(dev, lib.fp4attn_cache_read, ctypes.byref(c), _ptr(slots), n, _ptr(k), _ptr(v), _DTYPES[out_dtype],
                 _stream(slots))
     return k, v
+
+
+class KVPool(NamedTuple):
+    """Free pages of a cache (fp4attn_cache_assign in include/fp4attn.h): ``free`` int32 [size], a ring, and
+    ``counts`` int64 [2], the pages taken from it and those that came to it so far."""
+    free: torch.Tensor
+    counts: torch.Tensor
+
+
+class CacheStep(NamedTuple):
+    """What :func:`cache_assign` makes for a step: ``slots`` (:func:`cache_write`) and ``positions``
+    (:func:`rotary`) int64 [tokens], ``q_starts`` int32 [B + 1] and ``lengths`` int32 [B]
+    (:func:`cache_attention`), and the pool after it."""
+    slots: torch.Tensor
+    positions: torch.Tensor
+    q_starts: torch.Tensor
+    lengths: torch.Tensor
+    pool: KVPool
+
+
+def cache_pool(pages, first=0, device="cuda"):
+    """A :class:`KVPool` of pages ``first`` to ``pages - 1`` of a cache, all free, with room for the others."""
+    if not 0 <= first < pages:
+        raise ValueError(f"no pool of pages {first} to {pages - 1}")
+    free = torch.arange(first, first + pages, dtype=torch.int32, device=device)
+    free[pages - first:] = -1
+    return KVPool(free, torch.tensor([0, pages - first], dtype=torch.int64, device=device))
+
+
+def cache_assign(page_table, held, lengths, pool, page_size, tokens, new=None, shared=None, in_place=False):
+    """Pages, slots and positions of a step's ``tokens`` tokens; returns a :class:`CacheStep`.
+
+    ``page_table`` [B, max_pages], ``held`` and ``lengths`` [B] (keys before the step, and after it with the new
+    tokens) are int32.  Rows of ``page_table`` grow by pages of ``pool``, whose ``free`` takes the pages that are
+    returned (both are written in place).  ``new`` (int32 [B]): new tokens of each sequence, the last of its keys; without it
+    ``tokens / B`` each; tokens past their sum are padding.  ``shared`` (int32 [B]): keys at the start of a
+    sequence whose whole pages belong to others.
+
+    Pages go out in the order of the sequences; one that the pool cannot serve keeps what it held: its
+    length in the result is ``held``, and its tokens have slot -1.  ``in_place`` writes the
+    lengths and counts after the step into ``held`` and ``pool.counts``, for captured steps."""
+    r = _binding.cache_assign(page_table, held, lengths, pool, page_size, tokens, new, shared, in_place)
+    if r is not None:
+        slots, positions, starts, after, counts = _native(r)
+        return CacheStep(slots, positions, starts, after, KVPool(pool[0], counts))
+    _need(page_table, "page_table", torch.int32, 2)
+    B, width = page_table.shape
+    if len(pool) != 2:
+        raise ValueError("a pool is (free, counts)")
+    free, counts = pool
+    if not isinstance(page_size, int) or not isinstance(tokens, int):
+        raise TypeError("page_size and tokens must be integers")
+    named = ((held, "held", torch.int32, B), (lengths, "lengths", torch.int32, B), (new, "new", torch.int32, B),
+             (shared, "shared", torch.int32, B), (free, "pool.free", torch.int32, None), (counts, "pool.counts", torch.int64, 2))
+    used = [page_table]
+    for t, name, dtype, size in named:
+        if t is None and name in ("new", "shared"):
+            continue
+        _need(t, name, dtype, 1)
+        if size is not None and t.numel() != size:
+            raise ValueError(f"{name} has {t.numel()} entries, expected {size}")
+        used.append(t)
+    dev = _same_device(*used)
+    n = max(tokens, 0)   # below 0: the call says so
+    slots, positions = (torch.empty(n, dtype=torch.int64, device=dev) for _ in range(2))
+    starts = torch.empty(B + 1, dtype=torch.int32, device=dev)
+    after, counts_after = (held, counts) if in_place else (torch.empty_like(held), torch.empty_like(counts))
+    size = lib.fp4attn_cache_assign_workspace(B)
+    work = torch.empty(max(size, 16), dtype=torch.uint8, device=dev)
+    _launch(dev, lib.fp4attn_cache_assign, _ptr(page_table), B, width, page_size, _ptr(held), _ptr(lengths),
+            None if new is None else _ptr(new), None if shared is None else _ptr(shared), _ptr(free), free.numel(),
+            _ptr(counts), tokens, _ptr(slots), _ptr(positions), _ptr(starts), _ptr(after), _ptr(counts_after), _ptr(work),
+            max(size, 0), _stream(page_table))
+    return CacheStep(slots, positions, starts, after, KVPool(free, counts_after))
 
 
 def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tree=None, softmax_scale=None, out=None,

@@ -535,6 +535,70 @@ fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slo
   return from_hip(fp4attn::launch_cache_read(a, static_cast<hipStream_t>(stream)), "cache read launch");
 }
 
+int64_t fp4attn_cache_assign_workspace(int64_t B) {
+  return B < 1 || B > 65535 ? -1 : fp4attn::cache_assign_workspace(B);
+}
+
+fp4attn_status fp4attn_cache_assign(int32_t* page_table, int64_t B, int64_t max_pages, int64_t page_size,
+                                    const int32_t* held, const int32_t* lengths, const int32_t* new_tokens,
+                                    const int32_t* shared, int32_t* pool_pages, int64_t pool_size,
+                                    const int64_t* pool_counts, int64_t tokens, int64_t* slots, int64_t* positions,
+                                    int32_t* q_starts, int32_t* lengths_out, int64_t* counts_out, void* workspace,
+                                    int64_t workspace_bytes, void* stream) {
+  if (B < 1 || max_pages < 1 || pool_size < 1 || tokens < 0)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "B, max_pages and pool_size must be >= 1, tokens >= 0");
+  if (page_size < 16 || (page_size & (page_size - 1)) != 0)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "page_size=%lld must be a power of two >= 16", (long long)page_size);
+  if (new_tokens == nullptr && tokens % B != 0)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "tokens=%lld is no multiple of B=%lld, and there are no new_tokens", (long long)tokens,
+                (long long)B);
+  if (B > 65535 || tokens > (1 << 24) || pool_size > 0x7fffffff)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld tokens=%lld pool_size=%lld: at most 65535, 2^24 and 2^31 - 1", (long long)B,
+                (long long)tokens, (long long)pool_size);
+  if (page_size > (1 << 20) || max_pages > fp4attn::kMaxCacheKeys / page_size || max_pages > 0x7fffffff / B)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_pages=%lld page_size=%lld: more than 2^30 keys a sequence or 2^31 pages",
+                (long long)B, (long long)max_pages, (long long)page_size);
+  REQUIRE_INDEX(page_table);
+  REQUIRE_INDEX(held);
+  REQUIRE_INDEX(lengths);
+  if (new_tokens != nullptr) REQUIRE_INDEX(new_tokens);
+  if (shared != nullptr) REQUIRE_INDEX(shared);
+  REQUIRE_INDEX(pool_pages);
+  REQUIRE_INDEX(pool_counts);
+  if (tokens > 0) {
+    REQUIRE_INDEX(slots);
+    REQUIRE_INDEX(positions);
+  }
+  REQUIRE_INDEX(q_starts);
+  REQUIRE_INDEX(lengths_out);
+  REQUIRE_INDEX(counts_out);
+  REQUIRE_PTR(workspace);
+  if (workspace_bytes < fp4attn::cache_assign_workspace(B))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "workspace of %lld bytes, %lld are needed", (long long)workspace_bytes,
+                (long long)fp4attn::cache_assign_workspace(B));
+  fp4attn::CacheAssignArgs a{};
+  a.page_table = page_table;
+  a.held = held;
+  a.lengths = lengths;
+  a.fresh = new_tokens;
+  a.shared = shared;
+  a.ring = pool_pages;
+  a.counts = pool_counts;
+  a.counts_out = counts_out;
+  a.lengths_out = lengths_out;
+  a.slots = slots;
+  a.positions = positions;
+  a.starts = q_starts;
+  a.workspace = workspace;
+  a.B = (int)B;
+  a.max_pages = (int)max_pages;
+  a.page_shift = __builtin_ctzll((unsigned long long)page_size);
+  a.each = (int)(tokens / B);
+  a.tokens = (int)tokens;
+  a.capacity = (int)pool_size;
+  return from_hip(fp4attn::launch_cache_assign(a, static_cast<hipStream_t>(stream)), "cache assign launch");
+}
+
 int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_heads, int64_t B, int64_t max_pages,
                                           int64_t max_q) {
   fp4attn::CacheView c{};

@@ -472,6 +472,51 @@ PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// page_table, held, lengths, pool, page_size, tokens, new, shared, in_place; the tensors of a step
+PyObject* cache_assign(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 9) return nullptr;
+    const c10::DeviceIndex device = c10::hip::current_device();
+    const Tensor* table = index_tensor(a[0], device, at::kInt, 2);
+    if (!table || !PyTuple_Check(a[3]) || PyTuple_GET_SIZE(a[3]) != 2) return nullptr;
+    const int64_t B = table->size(0), pages = table->size(1);
+    int32_t page_size, tokens;
+    bool in_place;
+    if (!as_int(a[4], &page_size) || !as_int(a[5], &tokens) || tokens < 0 || !as_bool(a[8], &in_place)) return nullptr;
+    auto ints = [&](PyObject* o) -> const Tensor* {
+      const Tensor* t = index_tensor(o, device, at::kInt, 1);
+      return t && t->numel() == B ? t : nullptr;
+    };
+    const Tensor *held = ints(a[1]), *lengths = ints(a[2]), *fresh = a[6] == Py_None ? nullptr : ints(a[6]),
+                 *shared = a[7] == Py_None ? nullptr : ints(a[7]);
+    const Tensor *ring = index_tensor(PyTuple_GET_ITEM(a[3], 0), device, at::kInt, 1),
+                 *counts = index_tensor(PyTuple_GET_ITEM(a[3], 1), device, at::kLong, 1);
+    if (!held || !lengths || (!fresh && a[6] != Py_None) || (!shared && a[7] != Py_None) || !ring || !counts ||
+        counts->numel() != 2)
+      return nullptr;
+    const int64_t bytes = fp4attn_cache_assign_workspace(B);
+    if (bytes < 0) return nullptr;
+    Tensor out[5] = {gpu_empty({tokens}, at::kLong, device), gpu_empty({tokens}, at::kLong, device),
+                     gpu_empty({B + 1}, at::kInt, device), in_place ? *held : gpu_empty({B}, at::kInt, device),
+                     in_place ? *counts : gpu_empty({2}, at::kLong, device)};
+    Tensor work = gpu_empty({bytes}, at::kByte, device);
+    auto p32 = [](const Tensor* t) { return t ? static_cast<int32_t*>(t->data_ptr()) : nullptr; };
+    auto p64 = [](const Tensor* t) { return static_cast<int64_t*>(t->data_ptr()); };
+    void *wp = work.data_ptr(), *stream = stream_of(device);
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fp4attn_cache_assign(p32(table), B, pages, page_size, p32(held), p32(lengths), p32(fresh), p32(shared), p32(ring),
+                              ring->numel(), p64(counts), tokens, p64(&out[0]), p64(&out[1]), p32(&out[2]), p32(&out[3]),
+                              p64(&out[4]), wp, bytes, stream);
+    Py_END_ALLOW_THREADS
+    if (st != FP4ATTN_OK) return PyLong_FromLong(st);
+    PyObject* t = PyTuple_New(5);
+    if (t)
+      for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(t, i, THPVariable_Wrap(std::move(out[i])));
+    return t;
+  });
+}
+
 // q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype
 PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -557,6 +602,7 @@ PyMethodDef methods[] = {
     {"rotary", (PyCFunction)(void (*)())rotary, METH_FASTCALL, nullptr},
     {"cache_write", (PyCFunction)(void (*)())cache_write, METH_FASTCALL, nullptr},
     {"cache_read", (PyCFunction)(void (*)())cache_read, METH_FASTCALL, nullptr},
+    {"cache_assign", (PyCFunction)(void (*)())cache_assign, METH_FASTCALL, nullptr},
     {"cache_attention", (PyCFunction)(void (*)())cache_attention, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,200 @@
+// Pages, slots and positions of a step's tokens, from the keys that each sequence held and has now.
+//
+// With f = shared / page, h = max(ceil(held / page), f) and p = max(ceil(length / page), f) pages of
+// sequence b, need = max(p - h, 0), back = max(h - p, 0) and their exclusive sums N, R over the sequences:
+//   table[b][h + i] = ring[(taken + N_b + i) mod capacity]         i < need, where the pool has that many
+//   ring[(returned + R_b + i) mod capacity] = table[b][p + i]      i < back
+//   slot of token t: key j = length - new + t in page table[b][j / page]
+// Three prefix sums over the sequences, then every token and every page by itself: the sums go through one
+// workgroup, the rest over as many as there are tokens; a thread finds its sequence by bisection.
+// What bounds it: latency.  The data of a step are a few KB.
+#include "gfx950.hpp"
+#include "serving.hpp"
+
+namespace fp4attn {
+
+namespace {
+
+constexpr int kScanThreads = 1024, kScanWaves = kScanThreads / 64;
+constexpr int kFillThreads = 256;
+
+// Of the whole call; the arrays of B ints behind it are Sums.
+struct Totals {
+  unsigned take0, give0;  // places of the ring where pages are taken and returned
+  int takes, gives;       // pages
+};
+struct Sums {
+  Totals* totals;
+  int* need;  // [B] exclusive sum of the pages that the sequences before ask for
+  int* back;  // [B] of the pages that they return
+  int* had;   // [B] pages before the step, ~pages if the sequence was refused
+  int* now;   // [B] pages after it
+};
+__device__ __forceinline__ Sums sums(const CacheAssignArgs& a) {
+  Sums s;
+  s.totals = static_cast<Totals*>(a.workspace);
+  s.need = reinterpret_cast<int*>(s.totals + 1);
+  s.back = s.need + a.B;
+  s.had = s.back + a.B;
+  s.now = s.had + a.B;
+  return s;
+}
+
+__device__ __forceinline__ int scan_wave(int x) {  // inclusive
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// What one sequence asks for.
+struct Request {
+  int had, now, keys, fresh;
+  bool fits;
+};
+__device__ __forceinline__ int new_tokens(const CacheAssignArgs& a, int b) {
+  const int n = a.fresh ? a.fresh[b] : a.each;
+  return n < 0 ? 0 : n;
+}
+__device__ __forceinline__ int shared_pages(const CacheAssignArgs& a, int b) {
+  const int s = a.shared ? a.shared[b] : 0, capacity = a.max_pages << a.page_shift;
+  return (s < 0 ? 0 : (s > capacity ? capacity : s)) >> a.page_shift;
+}
+__device__ __forceinline__ Request request(const CacheAssignArgs& a, int b) {
+  Request r;
+  const int held = a.held[b], length = a.lengths[b], first = shared_pages(a, b);
+  const int capacity = a.max_pages << a.page_shift, page = 1 << a.page_shift;  // 2^30 at most
+  r.fresh = new_tokens(a, b);
+  r.fits = length <= capacity;
+  r.keys = held < 0 ? 0 : (held > capacity ? capacity : held);
+  const int want = length < 0 ? 0 : (r.fits ? length : capacity);
+  const int had = (r.keys + page - 1) >> a.page_shift, now = (want + page - 1) >> a.page_shift;
+  r.had = had > first ? had : first;
+  r.now = now > first ? now : first;
+  return r;
+}
+
+// One workgroup: the sums, the starts, the lengths and counts after the step.
+__global__ __launch_bounds__(kScanThreads) void cache_assign_sums_kernel(const CacheAssignArgs a) {
+  __shared__ int lds[3][kScanWaves];
+  __shared__ int lds_takes;
+  const Sums s = sums(a);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t taken = a.counts[0], returned = a.counts[1];
+  const int64_t left = (int64_t)((uint64_t)returned - (uint64_t)taken);
+  const int room = left < 0 ? 0 : (left > a.capacity ? a.capacity : (int)left);
+  if (threadIdx.x == 0) lds_takes = 0;
+  int need0 = 0, back0 = 0, start0 = 0;  // of the sequences before
+  for (int b0 = 0; b0 < a.B; b0 += kScanThreads) {
+    const int b = b0 + threadIdx.x;
+    Request r{};
+    int need = 0, back = 0, fresh = 0;
+    if (b < a.B) {
+      r = request(a, b);
+      need = r.fits && r.now > r.had ? r.now - r.had : 0;
+      back = r.fits && r.had > r.now ? r.had - r.now : 0;
+      fresh = r.fresh > a.tokens ? a.tokens : r.fresh;
+    }
+    const int need1 = scan_wave(need), back1 = scan_wave(back), fresh1 = scan_wave(fresh);  // 64 * 2^24 tokens at most
+    __syncthreads();
+    if (lane == 63) {
+      lds[0][wave] = need1;
+      lds[1][wave] = back1;
+      lds[2][wave] = fresh1 > a.tokens ? a.tokens : fresh1;
+    }
+    __syncthreads();
+    int before[3] = {need0, back0, start0};
+#pragma unroll
+    for (int w = 0; w < kScanWaves; ++w) {
+      if (w == wave) {
+        before[0] = need0;
+        before[1] = back0;
+        before[2] = start0;
+      }
+      need0 += lds[0][w];
+      back0 += lds[1][w];
+      start0 = start0 + lds[2][w] > a.tokens ? a.tokens : start0 + lds[2][w];
+    }
+    if (b < a.B) {
+      const int upto = before[0] + need1;
+      const bool served = r.fits && (need == 0 || upto <= room);
+      const int end = before[2] + fresh1;
+      s.need[b] = upto - need;
+      s.back[b] = before[1] + back1 - back;
+      s.had[b] = served ? r.had : ~r.had;
+      s.now[b] = r.now;
+      const int length = a.lengths[b];
+      a.starts[b + 1] = end > a.tokens ? a.tokens : end;
+      a.lengths_out[b] = served ? (length < 0 ? 0 : length) : r.keys;
+      if (served && need > 0) atomicMax(&lds_takes, upto);  // (the largest, in whatever order)
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.starts[0] = 0;
+    const int64_t n = a.capacity;
+    *s.totals = Totals{(unsigned)((taken % n + n) % n), (unsigned)((returned % n + n) % n), lds_takes, back0};
+    a.counts_out[0] = taken + lds_takes;
+    a.counts_out[1] = returned + back0;
+  }
+}
+
+// The last of n ascending values that is not above x (the first is not).
+__device__ __forceinline__ int find_last(const int* v, int n, int x) {
+  int lo = 0, hi = n;  // v[lo] <= x, v[hi] above (or the end)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (v[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kFillThreads) void cache_assign_fill_kernel(const CacheAssignArgs a) {
+  const Sums s = sums(a);
+  const Totals total = *s.totals;
+  const int first = blockIdx.x * kFillThreads + threadIdx.x, step = gridDim.x * kFillThreads;
+  const unsigned ring = (unsigned)a.capacity;
+  auto taken_page = [&](int k) { return a.ring[(total.take0 + (unsigned)k) % ring]; };
+  const int used = a.starts[a.B];
+  for (int i = first; i < a.tokens; i += step) {
+    int64_t slot = -1, at = 0;
+    if (i < used) {
+      const int b = find_last(a.starts, a.B, i), had = s.had[b];
+      at = (int64_t)a.lengths[b] - new_tokens(a, b) + (i - a.starts[b]);
+      const int64_t capacity = (int64_t)a.max_pages << a.page_shift;
+      if (had >= 0 && at >= (int64_t)shared_pages(a, b) << a.page_shift && at < capacity) {
+        const int place = (int)(at >> a.page_shift);
+        const int page = place >= had ? taken_page(s.need[b] + place - had) : a.page_table[(int64_t)b * a.max_pages + place];
+        if (page >= 0) slot = ((int64_t)page << a.page_shift) + (at & ((1 << a.page_shift) - 1));
+      }
+    }
+    a.slots[i] = slot;
+    a.positions[i] = at < 0 ? 0 : at;
+  }
+  for (int k = first; k < total.takes; k += step) {
+    const int b = find_last(s.need, a.B, k);
+    a.page_table[(int64_t)b * a.max_pages + s.had[b] + (k - s.need[b])] = taken_page(k);
+  }
+  for (int k = first; k < total.gives; k += step) {
+    const int b = find_last(s.back, a.B, k);
+    a.ring[(total.give0 + (unsigned)k) % ring] = a.page_table[(int64_t)b * a.max_pages + s.now[b] + (k - s.back[b])];
+  }
+}
+
+}  // namespace
+
+int64_t cache_assign_workspace(int64_t B) { return (int64_t)sizeof(Totals) + 16 * B; }
+
+hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream) {
+  cache_assign_sums_kernel<<<1, kScanThreads, 0, stream>>>(a);
+  const int64_t items = a.tokens > a.B ? a.tokens : a.B;
+  const int64_t groups = (items + kFillThreads - 1) / kFillThreads;
+  cache_assign_fill_kernel<<<(unsigned)(groups < 1024 ? groups : 1024), kFillThreads, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace fp4attn

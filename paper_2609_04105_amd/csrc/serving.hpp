@@ -1,5 +1,5 @@
 // Host-side launchers of the operators around a key/value cache:
-// rotary positions, the cache's quantizer and reader, attention over it.  Arguments
+// rotary positions, the cache's quantizer and reader, its pages, attention over it.  Arguments
 // are already validated by the C-ABI layer (api.hip).
 #pragma once
 
@@ -56,6 +56,27 @@ struct CacheReadArgs {
 
 hipError_t launch_cache_write(const CacheWriteArgs& a, hipStream_t stream);
 hipError_t launch_cache_read(const CacheReadArgs& a, hipStream_t stream);
+
+// Pages and slots of a step's tokens (csrc/cache_assign.hip).
+struct CacheAssignArgs {
+  int* page_table;     // [B, max_pages]
+  const int* held;     // [B]
+  const int* lengths;  // [B]
+  const int* fresh;    // [B] new tokens, or null: `each`
+  const int* shared;   // [B] or null: 0
+  int* ring;           // [capacity] free pages
+  const int64_t* counts;
+  int64_t* counts_out;
+  int* lengths_out;
+  int64_t* slots;      // [tokens]
+  int64_t* positions;  // [tokens]
+  int* starts;         // [B + 1]
+  void* workspace;
+  int B, max_pages, page_shift, each, tokens, capacity;
+};
+
+int64_t cache_assign_workspace(int64_t B);
+hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream);
 
 struct CachePlan;  // cache_plan.hpp
 
