@@ -411,6 +411,56 @@ int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_
                                           int64_t max_q);
 
 /*
+ * Scores, masks and batches beyond fp4attn_cache_attention.  With token t of sequence b at position
+ * p = lengths[b] - T + t, key j has the score
+ *
+ *   z = softmax_scale q.k;  z = softcap tanh(z / softcap) if softcap > 0;  z -= slopes[h] |p - j| if slopes,
+ *
+ * and is seen where j < lengths[b], and j <= p or j < prefix[b], and j > p - window (0: no window).  A row that sees
+ * no key gets zeros and -inf, as there.
+ *
+ *   slopes   [q_heads] fp32 or NULL, of the query heads
+ *   window   keys that a token sees up to its own; pages of keys that no token sees may hold anything, also -1
+ *   prefix   [B] int32 or NULL: the first prefix[b] keys are seen by every new token of sequence b
+ *   shared   the first `shared` keys (and their values) of every sequence are the same, whose pages need not be.  A hint: the
+ *            result is that of shared = 0 but for the order of sums.  Keys that all rows read once are taken from
+ *            the pages of one sequence whose new tokens come after them; sequences with fewer keys are
+ *            served by themselves.
+ *
+ * Initialise with fp4attn_cache_attention_options_init (no option set); struct_size must equal
+ * sizeof(fp4attn_cache_attention_options).
+ */
+typedef struct fp4attn_cache_attention_options {
+  uint32_t struct_size;
+  float softcap;
+  const float* slopes;
+  int64_t window;
+  const int32_t* prefix;
+  int64_t shared;
+} fp4attn_cache_attention_options;
+
+void fp4attn_cache_attention_options_init(fp4attn_cache_attention_options* opts);
+
+/*
+ * fp4attn_cache_attention with options (NULL: none).  Without one the two are the same call.
+ *
+ * Errors: those of fp4attn_cache_attention; INVALID_ARG for a wrong struct_size, a softcap other than 0 outside
+ * [2^-64, 2^64], a negative window, misaligned slopes or prefix, shared outside [0, max_pages * page_size]; UNSUPPORTED for a window
+ * above 2^30, and for slopes, a window or a prefix with a tree.
+ */
+fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
+                                          int64_t q_stride, int64_t B, const int32_t* page_table, int64_t max_pages,
+                                          const int32_t* lengths, const int32_t* q_starts, int64_t max_q,
+                                          const int64_t* tree, int64_t tree_words, float softmax_scale,
+                                          const fp4attn_cache_attention_options* opts, void* out, int out_dtype,
+                                          float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that such a call needs; -1 for sizes and options that the call refuses. */
+int64_t fp4attn_cache_attention_ex_workspace(const fp4attn_cache* cache, int64_t n, int64_t q_heads, int64_t B,
+                                             int64_t max_pages, int64_t max_q,
+                                             const fp4attn_cache_attention_options* opts);
+
+/*
  * Pages and slots of a step's tokens, from the keys that each sequence held before the step and
  * has after it: page tables grow by pages of a pool and return the pages that they no longer need.
  *

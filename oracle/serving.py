@@ -125,3 +125,44 @@ def assign(table, held, lengths, ring, counts, page, tokens, new=None, shared=No
         ring[(returned + j) % len(ring)] = p
     rest = tokens - len(slots)
     return slots + [-1] * rest, positions + [0] * rest, starts, after, [taken, returned + len(gone)]
+
+
+def shaped_mask(T, n, length, window=0, prefix=0):
+    """Token t of T at position p = length - T + t sees keys j <= p and j < prefix, with a window only j > p - window."""
+    key, at = np.arange(n)[None, :], (length - T + np.arange(T))[:, None]
+    see = (key <= at) | (key < prefix)
+    return see & (key > at - window) if window else see
+
+
+def shaped_attention(q, k, v, visible, softmax_scale, softcap=0.0, slopes=None, length=0):
+    """`attention` with z capped, softcap tanh(z / softcap), and then slopes[h] times its distance less for every key;
+    the tokens stand at positions length - T ...  The sizes that error bounds need follow: as there, and the largest
+    |capped score| and the largest |bias| of a row [T, Hq]."""
+    T, Hq, d = q.shape
+    G = Hq // k.shape[1] if len(k) else 1
+    out, lse = np.zeros((T, Hq, d)), np.full((T, Hq), -math.inf)
+    spread, size = np.zeros((T, Hq, d)), np.zeros((T, Hq, d))
+    reach, high, bias = (np.zeros((T, Hq)) for _ in range(3))
+    for t in range(T):
+        seen = np.flatnonzero(visible[t])
+        if len(seen) == 0:
+            continue
+        far = np.abs(length - T + t - seen)
+        for h in range(Hq):
+            kk, vv = k[seen, h // G], v[seen, h // G]
+            z = kk @ q[t, h] * softmax_scale
+            if softcap:
+                z = softcap * np.tanh(z / softcap)
+            high[t, h] = np.abs(z).max()
+            if slopes is not None:
+                z = z - slopes[h] * far
+                bias[t, h] = np.abs(slopes[h] * far).max()
+            top = z.max()
+            w = np.exp(z - top)
+            lse[t, h] = top + math.log(w.sum())
+            w = w / w.sum()
+            out[t, h] = w @ vv
+            spread[t, h] = w @ np.abs(vv - out[t, h])
+            size[t, h] = w @ np.abs(vv)
+            reach[t, h] = (np.abs(kk) @ np.abs(q[t, h])).max() * softmax_scale
+    return out, lse, spread, size, reach, high, bias

@@ -29,6 +29,12 @@ class Cache(ctypes.Structure):
                 ("v_scales", _c_p)]
 
 
+class AttentionOptions(ctypes.Structure):
+    """fp4attn_cache_attention_options (include/fp4attn.h)."""
+    _fields_ = [("struct_size", ctypes.c_uint32), ("softcap", ctypes.c_float), ("slopes", _c_p), ("window", _i64),
+                ("prefix", _c_p), ("shared", _i64)]
+
+
 # name -> argtypes; entry points not in RESTYPES return a status int
 SIGNATURES = {
     "fp4attn_quantize_mxfp4": [_c_p, _int, _i64, _i64, _i64, _int, _c_p, _c_p, _c_p],
@@ -49,6 +55,10 @@ SIGNATURES = {
     "fp4attn_cache_attention": [ctypes.POINTER(Cache), _c_p, _i64, _i64, _i64, _i64, _c_p, _i64, _c_p, _c_p, _i64, _c_p,
                                 _i64, _f32, _c_p, _int, _c_p, _c_p, _i64, _c_p],
     "fp4attn_cache_attention_workspace": [ctypes.POINTER(Cache)] + [_i64] * 4,
+    "fp4attn_cache_attention_options_init": [ctypes.POINTER(AttentionOptions)],
+    "fp4attn_cache_attention_ex": [ctypes.POINTER(Cache), _c_p, _i64, _i64, _i64, _i64, _c_p, _i64, _c_p, _c_p, _i64, _c_p,
+                                   _i64, _f32, ctypes.POINTER(AttentionOptions), _c_p, _int, _c_p, _c_p, _i64, _c_p],
+    "fp4attn_cache_attention_ex_workspace": [ctypes.POINTER(Cache)] + [_i64] * 5 + [ctypes.POINTER(AttentionOptions)],
     "fp4attn_debug_mfma_stream": [_c_p, _c_p, _int, _int, _c_p, _c_p],
     "fp4attn_status_string": [_int],
     "fp4attn_last_error": [],
@@ -56,7 +66,8 @@ SIGNATURES = {
 }
 RESTYPES = {"fp4attn_status_string": ctypes.c_char_p, "fp4attn_last_error": ctypes.c_char_p,
             "fp4attn_abi_version": ctypes.c_int, "fp4attn_forward_options_init": None,
-            "fp4attn_cache_attention_workspace": ctypes.c_int64, "fp4attn_cache_assign_workspace": ctypes.c_int64}
+            "fp4attn_cache_attention_workspace": ctypes.c_int64, "fp4attn_cache_attention_ex_workspace": ctypes.c_int64,
+            "fp4attn_cache_attention_options_init": None, "fp4attn_cache_assign_workspace": ctypes.c_int64}
 
 
 class Fp4AttnError(RuntimeError):

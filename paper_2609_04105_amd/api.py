@@ -17,7 +17,7 @@ from typing import NamedTuple
 
 import torch
 
-from ._lib import FP4ATTN_BF16, FP4ATTN_F32, Cache, ForwardOptions, check, lib
+from ._lib import FP4ATTN_BF16, FP4ATTN_F32, AttentionOptions, Cache, ForwardOptions, check, lib
 
 
 class _NoBinding:
@@ -634,7 +634,7 @@ def cache_assign(page_table, held, lengths, pool, page_size, tokens, new=None, s
 
 
 def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tree=None, softmax_scale=None, out=None,
-                    lse=None, out_dtype=torch.float32):
+                    lse=None, out_dtype=torch.float32, softcap=None, slopes=None, window=None, prefix=None, shared=0):
     """Attention of new tokens over ``cache``; returns O [n, Hq, d] (``out_dtype``, or ``out``).
 
     ``q`` [n, Hq, d] bf16 (tokens may lie apart), Hq a multiple of the cache's heads;
@@ -648,8 +648,18 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
 
     Token t of T sees the keys up to its own, or with ``tree`` (int64 [n], or [n, words] for more
     than 64 tokens) the keys before the new tokens and the new tokens u whose bit is set.
-    ``lse`` (fp32 [n, Hq]) receives the log normaliser.  A row that sees no key is 0 (-inf)."""
-    r = _binding.cache_attention(q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype)
+    ``lse`` (fp32 [n, Hq]) receives the log normaliser.  A row that sees no key is 0 (-inf).
+
+    With a token at position p: ``softcap`` c caps its scores, z becomes c tanh(z / c); ``slopes`` (fp32 [Hq]) then take
+    slope |p - j| off the score of key j; ``window`` hides keys up to p - window; ``prefix``
+    (int32 [B]) shows the first keys of a sequence to all of its new tokens.  A tree goes with ``softcap`` only.
+
+    ``shared``: the first ``shared`` keys of every sequence are the same (a system prompt, in the same pages or in
+    copies).  They are then read once for the batch where that is faster; the result is the same but for the order of sums."""
+    if slopes is not None and getattr(slopes, "requires_grad", False) and torch.is_grad_enabled():
+        raise ValueError("slopes get no gradient here: detach them, or call under torch.no_grad()")
+    r = _binding.cache_attention(q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype,
+                                 softcap, slopes, window, prefix, shared)
     if r is not None:
         return _native(r)
     c = _cache(cache)
@@ -682,6 +692,30 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
             raise ValueError(f"tree has shape {tuple(tree.shape)}, expected [{n}] or [{n}, words]")
         words = tree.shape[1] if tree.ndim == 2 else 1
         used.append(tree)
+    o = AttentionOptions(ctypes.sizeof(AttentionOptions))
+    if softcap is not None:
+        if not softcap > 0:
+            raise ValueError(f"softcap={softcap} must be positive")
+        o.softcap = softcap
+    if window is not None:
+        if not isinstance(window, int) or window < 1:
+            raise ValueError(f"window={window} must be a positive integer")
+        o.window = min(window, 1 << 40)   # (above 2^30 the call refuses it)
+    if not isinstance(shared, int):
+        raise TypeError(f"shared={shared} must be an integer")
+    o.shared = max(-1, min(shared, 1 << 40))
+    if slopes is not None:
+        _need(slopes, "slopes", torch.float32, 1)
+        if slopes.numel() != Hq:
+            raise ValueError(f"slopes have {slopes.numel()} entries for {Hq} heads")
+        o.slopes = slopes.data_ptr()
+        used.append(slopes)
+    if prefix is not None:
+        _need(prefix, "prefix", torch.int32, 1)
+        if prefix.numel() != B:
+            raise ValueError(f"prefix has {prefix.numel()} entries for {B} sequences")
+        o.prefix = prefix.data_ptr()
+        used.append(prefix)
     if out is None:
         if out_dtype not in _DTYPES:
             raise TypeError(f"out_dtype {out_dtype} is not one of {tuple(_DTYPES)}")
@@ -698,12 +732,12 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
     dev = _same_device(*used, out)
     if n == 0:
         return out
-    ref = ctypes.byref(c)
-    size = lib.fp4attn_cache_attention_workspace(ref, Hq, B, page_table.shape[1], max_q)
+    ref, opts = ctypes.byref(c), ctypes.byref(o)
+    size = lib.fp4attn_cache_attention_ex_workspace(ref, n, Hq, B, page_table.shape[1], max_q, opts)
     work = torch.empty(size, dtype=torch.uint8, device=dev) if size > 0 else None   # -1: the call says why
-    _launch(dev, lib.fp4attn_cache_attention, ref, _ptr(q), n, Hq, stride if n > 1 else 0, B, _ptr(page_table),
+    _launch(dev, lib.fp4attn_cache_attention_ex, ref, _ptr(q), n, Hq, stride if n > 1 else 0, B, _ptr(page_table),
             page_table.shape[1], _ptr(lengths), None if q_starts is None else _ptr(q_starts), max_q,
             None if tree is None else _ptr(tree), words, 1.0 / math.sqrt(d) if softmax_scale is None else softmax_scale,
-            _ptr(out), _DTYPES[out.dtype], None if lse is None else _ptr(lse), None if work is None else _ptr(work),
+            opts, _ptr(out), _DTYPES[out.dtype], None if lse is None else _ptr(lse), None if work is None else _ptr(work),
             max(size, 0), _stream(q))
     return out

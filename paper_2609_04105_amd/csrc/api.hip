@@ -279,6 +279,68 @@ fp4attn_status check_cache_attention(const fp4attn::CacheView& c, int64_t q_head
   return FP4ATTN_OK;
 }
 
+// The plan of an attention call with options: of its own pass, and of the one over the shared prefix.
+struct AttentionPlan {
+  fp4attn::CachePlan plan;
+  fp4attn::PrefixPlan prefix;
+  bool shaped;  // some option is set
+  int shared;   // keys of the prefix that has a pass of its own; 0: none
+  int64_t join_bytes, workspace;
+};
+fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int64_t q_heads, int64_t B, int64_t max_pages,
+                                    int64_t max_q, const fp4attn_cache_attention_options* opts, AttentionPlan* p) {
+  *p = AttentionPlan{};
+  fp4attn_status st = check_cache_attention(c, q_heads, B, max_pages, max_q, &p->plan);
+  if (st != FP4ATTN_OK) return st;
+  p->workspace = p->plan.workspace;
+  if (opts == nullptr) return FP4ATTN_OK;
+  if (opts->struct_size != sizeof(*opts))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "options struct_size %u, expected %zu", opts->struct_size, sizeof(*opts));
+  const int64_t max_keys = max_pages << c.page_shift;
+  constexpr float kLeastCap = 0x1p-64f, kMostCap = 0x1p64f;  // z / softcap and softcap stay normal numbers
+  if (opts->softcap != 0.0f && !(opts->softcap >= kLeastCap && opts->softcap <= kMostCap))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "softcap=%g must be 0 or in [2^-64, 2^64]", (double)opts->softcap);
+  if (opts->window < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "window=%lld must not be negative", (long long)opts->window);
+  if (opts->window > fp4attn::kMaxCacheKeys)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "window=%lld is above 2^30", (long long)opts->window);
+  if (opts->shared < 0 || opts->shared > max_keys)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "shared=%lld keys are not in [0, max_pages * page_size = %lld]", (long long)opts->shared,
+                (long long)max_keys);
+  if (opts->slopes != nullptr) REQUIRE_INDEX(opts->slopes);
+  if (opts->prefix != nullptr) REQUIRE_INDEX(opts->prefix);
+  p->shaped = opts->softcap > 0.0f || opts->slopes != nullptr || opts->window > 0 || opts->prefix != nullptr;
+  const int64_t G = q_heads / c.H;
+  int64_t span = max_keys;  // keys that a row tile walks at most
+  if (opts->window > 0) {
+    // few rows see the prefix: it gets no pass of its own
+    const int64_t units = fp4attn::window_units(fp4attn::kRowsTile, (int)G, (int)opts->window);
+    if (opts->prefix == nullptr && units * fp4attn::kUnit < span) span = units * fp4attn::kUnit;
+  } else if (n > 0 && n <= 0x7fffffff / q_heads && fp4attn::shares_prefix(B, G, max_q, opts->shared)) {
+    const int64_t keys = opts->shared / fp4attn::kUnit * fp4attn::kUnit;
+    const fp4attn::PrefixPlan prefix = fp4attn::prefix_plan(c.H, G, c.d, n, keys);
+    if (prefix.fits) {
+      p->shared = (int)keys;
+      p->prefix = prefix;
+      span -= keys;
+    }
+  }
+  if (!p->shaped && p->shared == 0) return FP4ATTN_OK;
+  p->shaped = true;
+  if (span < 1) span = 1;
+  p->plan = fp4attn::cache_plan(B, c.H, G, c.d, c.fp8 != 0, max_q, span);
+  // (a row tile smaller than the unshaped plan's, a sequence that does not join the shared prefix)
+  const int64_t places = B * p->plan.row_tiles * ((max_keys + fp4attn::kUnit - 1) / fp4attn::kUnit + fp4attn::kSetup);
+  if (!p->plan.fits || places + p->plan.ranges >= int64_t(1) << 31)
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_q=%lld max_pages=%lld: too many workgroups for one launch", (long long)B,
+                (long long)max_q, (long long)max_pages);
+  p->workspace = p->plan.workspace;
+  if (p->shared > 0) {
+    p->join_bytes = (p->plan.split ? (int64_t)p->plan.ranges * sizeof(int2) + 15 : 0) / 16 * 16;
+    p->workspace += p->join_bytes + p->prefix.pieces * p->prefix.rows * (16 + c.d * 4);
+  }
+  return FP4ATTN_OK;
+}
+
 }  // namespace
 
 namespace fp4attn {
@@ -601,13 +663,7 @@ fp4attn_status fp4attn_cache_assign(int32_t* page_table, int64_t B, int64_t max_
 
 int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_heads, int64_t B, int64_t max_pages,
                                           int64_t max_q) {
-  fp4attn::CacheView c{};
-  fp4attn::CachePlan plan;
-  if (check_cache_sizes(cache, &c) != FP4ATTN_OK ||
-      check_cache_attention(c, q_heads, B, max_pages, max_q, &plan) != FP4ATTN_OK)
-    return -1;
-  ok();
-  return plan.workspace;
+  return fp4attn_cache_attention_ex_workspace(cache, 0, q_heads, B, max_pages, max_q, nullptr);
 }
 
 fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
@@ -616,7 +672,36 @@ fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q
                                        const int64_t* tree, int64_t tree_words, float softmax_scale, void* out,
                                        int out_dtype, float* lse, void* workspace, int64_t workspace_bytes,
                                        void* stream) {
-  fp4attn::CacheAttentionArgs a{};
+  return fp4attn_cache_attention_ex(cache, q, n, q_heads, q_stride, B, page_table, max_pages, lengths, q_starts, max_q, tree,
+                                    tree_words, softmax_scale, nullptr, out, out_dtype, lse, workspace, workspace_bytes, stream);
+}
+
+void fp4attn_cache_attention_options_init(fp4attn_cache_attention_options* opts) {
+  if (opts != nullptr) {
+    *opts = fp4attn_cache_attention_options{};
+    opts->struct_size = sizeof(*opts);
+  }
+}
+
+int64_t fp4attn_cache_attention_ex_workspace(const fp4attn_cache* cache, int64_t n, int64_t q_heads, int64_t B,
+                                             int64_t max_pages, int64_t max_q,
+                                             const fp4attn_cache_attention_options* opts) {
+  fp4attn::CacheView c{};
+  AttentionPlan p;
+  if (check_cache_sizes(cache, &c) != FP4ATTN_OK ||
+      plan_cache_attention(c, n, q_heads, B, max_pages, max_q, opts, &p) != FP4ATTN_OK)
+    return -1;
+  ok();
+  return p.workspace;
+}
+
+fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
+                                          int64_t q_stride, int64_t B, const int32_t* page_table, int64_t max_pages,
+                                          const int32_t* lengths, const int32_t* q_starts, int64_t max_q,
+                                          const int64_t* tree, int64_t tree_words, float softmax_scale,
+                                          const fp4attn_cache_attention_options* opts, void* out, int out_dtype,
+                                          float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  fp4attn::ShapedAttentionArgs a{};
   fp4attn_status st = check_cache(cache, &a.c);
   if (st != FP4ATTN_OK) return st;
   if (n < 0) return fail(FP4ATTN_ERR_INVALID_ARG, "n=%lld must not be negative", (long long)n);
@@ -627,8 +712,8 @@ fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q
   st = check_stride(q_stride, FP4ATTN_BF16, "q_stride");
   if (st != FP4ATTN_OK) return st;
   if (n == 0) return ok();
-  fp4attn::CachePlan plan;
-  st = check_cache_attention(a.c, q_heads, B, max_pages, max_q, &plan);
+  AttentionPlan p;
+  st = plan_cache_attention(a.c, n, q_heads, B, max_pages, max_q, opts, &p);
   if (st != FP4ATTN_OK) return st;
   if (n > 0x7fffffff / q_heads)
     return fail(FP4ATTN_ERR_UNSUPPORTED, "n=%lld tokens of %lld heads are too many", (long long)n, (long long)q_heads);
@@ -638,6 +723,8 @@ fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q
   if (tree != nullptr && (tree_words < 1 || tree_words > (1 << 24) || tree_words * 64 < max_q))
     return fail(FP4ATTN_ERR_INVALID_ARG, "tree_words=%lld must hold max_q=%lld bits", (long long)tree_words,
                 (long long)max_q);
+  if (tree != nullptr && opts != nullptr && (opts->slopes != nullptr || opts->window != 0 || opts->prefix != nullptr))
+    return fail(FP4ATTN_ERR_UNSUPPORTED, "a tree of tokens has no slopes, window or prefix: its tokens' places are not their order");
   REQUIRE_PTR(q);
   REQUIRE_PTR(out);
   REQUIRE_INDEX(page_table);
@@ -645,11 +732,11 @@ fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q
   if (q_starts != nullptr) REQUIRE_INDEX(q_starts);
   if (tree != nullptr) REQUIRE_INDEX(tree);
   if (lse != nullptr) REQUIRE_INDEX(lse);
-  if (plan.workspace > 0) {
+  if (p.workspace > 0) {
     REQUIRE_PTR(workspace);
-    if (workspace_bytes < plan.workspace)
+    if (workspace_bytes < p.workspace)
       return fail(FP4ATTN_ERR_INVALID_ARG, "workspace of %lld bytes, %lld are needed", (long long)workspace_bytes,
-                  (long long)plan.workspace);
+                  (long long)p.workspace);
   }
   a.q = q;
   a.q_stride = q_stride;
@@ -669,7 +756,31 @@ fp4attn_status fp4attn_cache_attention(const fp4attn_cache* cache, const void* q
   a.out_bf16 = out_dtype == FP4ATTN_BF16;
   a.lse = lse;
   a.workspace = workspace;
-  return from_hip(fp4attn::launch_cache_attention(a, static_cast<hipStream_t>(stream)), "cache attention launch");
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!p.shaped) return from_hip(fp4attn::launch_cache_attention(a, p.plan, s), "cache attention launch");
+  a.softcap = opts->softcap;
+  a.slopes = opts->slopes;
+  a.window = (int)opts->window;
+  a.open_keys = opts->prefix;
+  if (p.shared > 0) {
+    char* w = static_cast<char*>(workspace) + p.plan.workspace;
+    a.shared = p.shared;
+    a.prefix_pieces = p.prefix.pieces;
+    a.prefix_units = p.prefix.units;
+    a.join_prefix = reinterpret_cast<int2*>(w);
+    w += p.join_bytes;
+    a.prefix_stat = reinterpret_cast<float4*>(w);
+    w += p.prefix.pieces * p.prefix.rows * 16;
+    a.prefix_acc = reinterpret_cast<float*>(w);
+    fp4attn::PrefixAttentionArgs pre{};
+    static_cast<fp4attn::ShapedAttentionArgs&>(pre) = a;
+    pre.tree = nullptr;  // its rows see the whole prefix
+    pre.tree_words = 0;
+    pre.open_keys = nullptr;
+    st = from_hip(fp4attn::launch_prefix_attention(pre, p.prefix.plan, s), "shared prefix launch");
+    if (st != FP4ATTN_OK) return st;
+  }
+  return from_hip(fp4attn::launch_shaped_attention(a, p.plan, s), "cache attention launch");
 }
 
 fp4attn_status fp4attn_debug_mfma_stream(const uint8_t* a_codes, const uint8_t* b_codes, int blocks, int iters,

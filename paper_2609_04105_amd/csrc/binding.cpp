@@ -517,10 +517,11 @@ PyObject* cache_assign(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype
+// q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype, softcap, slopes, window, prefix,
+// shared
 PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    if (n != 11) return nullptr;
+    if (n != 16) return nullptr;
     const c10::DeviceIndex device = c10::hip::current_device();
     int64_t stride;
     fp4attn_cache c;
@@ -569,7 +570,24 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       if (!t || !is_shape(*t, {tokens, Hq})) return nullptr;
       lse = static_cast<float*>(t->data_ptr());
     }
-    const int64_t bytes = fp4attn_cache_attention_workspace(&c, Hq, B, pages, max_q);
+    fp4attn_cache_attention_options opts;
+    fp4attn_cache_attention_options_init(&opts);
+    if (a[11] != Py_None && (!as_float(a[11], &opts.softcap) || !(opts.softcap > 0.0f))) return nullptr;
+    if (a[12] != Py_None) {
+      const Tensor* t = index_tensor(a[12], device, at::kFloat, 1);
+      if (!t || t->numel() != Hq) return nullptr;
+      opts.slopes = static_cast<const float*>(t->data_ptr());
+    }
+    int32_t window = 0, shared;
+    if ((a[13] != Py_None && (!as_int(a[13], &window) || window < 1)) || !as_int(a[15], &shared)) return nullptr;
+    opts.window = window;
+    opts.shared = shared;
+    if (a[14] != Py_None) {
+      const Tensor* t = index_tensor(a[14], device, at::kInt, 1);
+      if (!t || t->numel() != B) return nullptr;
+      opts.prefix = static_cast<const int32_t*>(t->data_ptr());
+    }
+    const int64_t bytes = fp4attn_cache_attention_ex_workspace(&c, tokens, Hq, B, pages, max_q, &opts);
     if (bytes < 0) return nullptr;
     if (!out.defined()) out = gpu_empty(q->sizes(), type, device);
     Tensor work;
@@ -582,8 +600,8 @@ PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int ctype = c_dtype(out.scalar_type());
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = fp4attn_cache_attention(&c, qp, tokens, Hq, stride, B, tp, pages, lp, sp, max_q, bp, words, scale, op, ctype, lse,
-                                 wp, bytes, stream);
+    st = fp4attn_cache_attention_ex(&c, qp, tokens, Hq, stride, B, tp, pages, lp, sp, max_q, bp, words, scale, &opts, op, ctype,
+                                    lse, wp, bytes, stream);
     Py_END_ALLOW_THREADS
     if (st != FP4ATTN_OK) return PyLong_FromLong(st);
     if (a[8] != Py_None) {

@@ -68,8 +68,10 @@ __device__ __forceinline__ v4i probabilities(const v4f (&s)[2], float factor, fl
 
 // The arguments lie in four lines of the scalar cache, each a miss of 0.7 us when it is first used: one
 // value of each is read at the start, so that the misses overlap.
-__device__ __forceinline__ void fetch_arguments(const CacheAttentionArgs& a, const CachePlan& plan) {
+template <class Args>
+__device__ __forceinline__ void fetch_arguments(const Args& a, const CachePlan& plan) {
   asm volatile("" ::"s"(a.c.H), "s"(a.B), "s"(a.tree), "s"(plan.ranges));
+  if constexpr (Args::kShaped) asm volatile("" ::"s"(a.softcap), "s"(a.prefix_acc));
 }
 
 // Of numbers that are not negative (half the instructions of a signed division).
@@ -103,9 +105,39 @@ __device__ __forceinline__ Sequence sequence(const CacheAttentionArgs& a, int b)
   return s;
 }
 
-// Units of kUnit keys; at least one, so that rows without keys are written.
-__device__ __forceinline__ int units_of(const Sequence& s) { return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit; }
-__device__ __forceinline__ int row_tiles_of(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& s) {
+// Keys at the start of a sequence that its rows have from the shared prefix's pass: those of a sequence whose
+// new tokens all come after the prefix.
+template <class Args>
+__device__ __forceinline__ int shared_keys(const Args& a, const Sequence& s) {
+  if constexpr (Args::kShaped && !Args::kPrefix) return s.tokens > 0 && s.prefix >= a.shared && s.keys >= a.shared ? a.shared : 0;
+  return 0;
+}
+
+// With a window the first key that row tile `tile` sees, or earlier (kUnit-aligned).
+template <class Args>
+__device__ __forceinline__ int first_key(const Args& a, const CachePlan& plan, const Sequence& s, int tile) {
+  if constexpr (Args::kShaped)
+    if (a.window) {
+      const int low = s.prefix + divide(tile * plan.tile, a.G) + 1 - a.window;
+      return low < 0 ? 0 : (low > s.keys ? s.keys : low) & -kUnit;
+    }
+  return shared_keys(a, s);
+}
+
+// Units of kUnit keys that a row tile walks; at least one, so that rows without keys are written.
+template <class Args>
+__device__ __forceinline__ int units_of(const Args& a, const CachePlan& plan, const Sequence& s) {
+  if constexpr (Args::kShaped) {
+    const int keys = s.keys - shared_keys(a, s), units = keys == 0 ? 1 : (keys + kUnit - 1) / kUnit;
+    // (a prefix that every token sees reaches past the window's end)
+    if (a.window == 0 || a.open_keys) return units;
+    const int span = window_units(plan.tile, a.G, a.window);
+    return units < span ? units : span;
+  }
+  return s.keys == 0 ? 1 : (s.keys + kUnit - 1) / kUnit;
+}
+template <class Args>
+__device__ __forceinline__ int row_tiles_of(const Args& a, const CachePlan& plan, const Sequence& s) {
   return (s.tokens * a.G + plan.tile - 1) >> __builtin_ctz(plan.tile);
 }
 
@@ -121,6 +153,7 @@ struct Range {
   int at, units;       // its units are at places [at, at + units)
   Sequence seq;
   int per;
+  int piece;  // of the shared prefix
 };
 
 // Inclusive prefix sum over the wave's lanes: within rows of 16, then across them.
@@ -135,7 +168,8 @@ __device__ __forceinline__ int prefix_sum(int x) {
 }
 
 // Every wave finds its range by itself, 64 sequences at a time.
-__device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const CachePlan& plan, int w) {
+template <class Args>
+__device__ __forceinline__ Range find_range(const Args& a, const CachePlan& plan, int w) {
   const int lane = threadIdx.x & 63;
   Range r{};
   Sequence seq{};  // the lane's
@@ -144,7 +178,7 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
     own = 0;
     if (b0 + lane < a.B) {
       seq = sequence(a, b0 + lane);
-      own = row_tiles_of(a, plan, seq) * (units_of(seq) + kSetup);
+      own = row_tiles_of(a, plan, seq) * (units_of(a, plan, seq) + kSetup);
     }
     sum = prefix_sum(own);
   };
@@ -168,7 +202,7 @@ __device__ __forceinline__ Range find_range(const CacheAttentionArgs& a, const C
       r.seq.tokens = __builtin_amdgcn_readlane(seq.tokens, src);
       r.seq.keys = __builtin_amdgcn_readlane(seq.keys, src);
       r.seq.prefix = __builtin_amdgcn_readlane(seq.prefix, src);
-      r.units = units_of(r.seq);
+      r.units = units_of(a, plan, r.seq);
       r.tiles = row_tiles_of(a, plan, r.seq);
       const int start = __builtin_amdgcn_readlane(from, src), places = r.units + kSetup;
       r.tile = divide(r.begin - start, places);
@@ -375,15 +409,65 @@ struct OddMarks {
   }
 };
 
+// The pieces of the shared prefix that a row joins: their number, and what the bias by distance takes off their
+// references, which its pass counts from the prefix's end.
+struct PrefixPieces {
+  int count;
+  float lower;
+};
+template <class Args>
+__device__ __forceinline__ PrefixPieces prefix_pieces(const Args& a, int keys, int prefix, int token, int head) {
+  PrefixPieces p{0, 0.0f};
+  if constexpr (Args::kShaped && !Args::kPrefix)
+    if (keys) {
+      p.count = a.prefix_pieces;
+      if (a.slopes) p.lower = a.slopes[head] * kLog2e * (float)(prefix + token - keys);
+    }
+  return p;
+}
+
 // Joins and stores: D / 16 columns from D / 16 * c of row i of the sequence, as output if the
 // sequence is whole in this workgroup, else as a piece.  o are sums of probabilities times codes'
 // values, `rounded` the sum of the probabilities, ref their base-2 reference, sum the unrounded sum; columns
 // whose bit of `odd` is set are NaN (MXFP4: all or none).
-template <int D, bool FP8>
-__device__ __forceinline__ void store_columns(const CacheAttentionArgs& a, const CachePlan& plan, const Sequence& seq, int i,
-                                              int head, int c, bool whole, int64_t piece, float ref, float sum,
-                                              float rounded, unsigned odd, const float (&o)[D / 16]) {
+template <int D, bool FP8, class Args>
+__device__ __forceinline__ void store_columns(const Args& a, const CachePlan& plan, const Sequence& seq, int i, int head, int c,
+                                              bool whole, int64_t piece, float ref, float sum, float rounded, unsigned odd,
+                                              float (&o)[D / 16]) {
   constexpr int kCols = D / 16;
+  if constexpr (Args::kPrefix) {  // a piece of row (token, head) of the batch
+    const int t = divide(i, a.G);
+    piece += (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
+  }
+  if constexpr (Args::kShaped && !Args::kPrefix)
+    if (whole) {
+      const int t = divide(i, a.G), h = head * a.G + (i - t * a.G);
+      const int64_t at = (int64_t)(seq.first + t) * a.Hq + h, rows = a.n * a.Hq;
+      const PrefixPieces pre = prefix_pieces(a, shared_keys(a, seq), seq.prefix, t, h);
+      float top = ref;
+      for (int k = 0; k < pre.count; ++k) top = fmaxf(top, a.prefix_stat[k * rows + at].x - pre.lower);
+      const float mine = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
+      ref = top;
+      sum *= mine;
+      rounded *= mine;
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) o[j] *= mine;
+      for (int k = 0; k < pre.count; ++k) {
+        const float4 s = a.prefix_stat[k * rows + at];
+        const float its_ref = s.x - pre.lower, its = its_ref == top ? 1.0f : __builtin_amdgcn_exp2f(its_ref - top);
+        sum += s.y * its;
+        rounded += s.z * its;
+        const float4* acc = reinterpret_cast<const float4*>(a.prefix_acc + (k * rows + at) * D + c * kCols);
+#pragma unroll
+        for (int j = 0; j < kCols / 4; ++j) {
+          const float4 x = acc[j];
+          o[4 * j] += x.x * its;
+          o[4 * j + 1] += x.y * its;
+          o[4 * j + 2] += x.z * its;
+          o[4 * j + 3] += x.w * its;
+        }
+      }
+    }
   const bool empty = is_zero(rounded);
   const float norm = whole ? (empty ? 0.0f : (FP8 ? 1.0f : 1.0f / 6.0f) / rounded) : 1.0f;
   float x[kCols];
@@ -398,9 +482,18 @@ __device__ __forceinline__ void store_columns(const CacheAttentionArgs& a, const
     else store_row<kCols>(static_cast<float*>(a.out) + at * D + c * kCols, x);
     if (a.lse && c == 0) a.lse[at] = log_norm(ref, sum);
   } else {
-    const Partials p = partials(a, plan);
-    store_row<kCols>(p.acc + piece * D + c * kCols, x);
-    if (c == 0) p.stat[piece] = float4{ref, sum, rounded, 0.0f};
+    float4* stat;
+    float* acc;
+    if constexpr (Args::kPrefix) {
+      stat = a.prefix_stat;
+      acc = a.prefix_acc;
+    } else {
+      const Partials p = partials(a, plan);
+      stat = p.stat;
+      acc = p.acc;
+    }
+    store_row<kCols>(acc + piece * D + c * kCols, x);
+    if (c == 0) stat[piece] = float4{ref, sum, rounded, 0.0f};
   }
 }
 
@@ -415,9 +508,44 @@ __device__ __forceinline__ Place place_of(const CachePlan& plan) {
   return {item - head * plan.ranges, head};
 }
 
+// The workgroup's range of the shared prefix: piece w / row_tiles of row tile w % row_tiles of all tokens
+// together.  Its pages are those of the first sequence that joins it (if there is none, the range is empty).
+template <class Args>
+__device__ __forceinline__ Range open_prefix(const Args& a, const CachePlan& plan, const Place& p) {
+  Range range{};
+  const int lane = threadIdx.x & 63;
+  int b = -1;
+  for (int b0 = 0; b0 < a.B && b < 0; b0 += 64) {
+    bool joins = false;
+    if (b0 + lane < a.B) {
+      const Sequence seq = sequence(a, b0 + lane);
+      joins = seq.tokens > 0 && seq.prefix >= a.shared && seq.keys >= a.shared;
+    }
+    const uint64_t found = __ballot(joins);
+    if (found) b = b0 + __ffsll((unsigned long long)found) - 1;
+  }
+  range.piece = divide(p.w, plan.row_tiles);
+  range.tile = p.w - range.piece * plan.row_tiles;
+  range.b = b;
+  range.tiles = 1;
+  int64_t tokens = a.n;
+  if (a.q_starts) {  // rows past the last sequence's belong to none
+    const int last = a.q_starts[a.B];
+    tokens = last < 0 ? 0 : (last < tokens ? last : tokens);
+  }
+  range.seq = Sequence{0, (int)tokens, a.shared, a.shared};
+  range.units = a.shared / kUnit;
+  range.begin = range.piece * a.prefix_units;
+  range.end = range.begin + a.prefix_units < range.units ? range.begin + a.prefix_units : range.units;
+  if (b < 0 || (int64_t)range.tile * plan.tile >= tokens * a.G) range.end = range.begin;
+  return range;
+}
+
 // The workgroup's range, and (from one of its threads) the record for the row tile that crosses
 // into it for the first time.
-__device__ __forceinline__ Range open_range(const CacheAttentionArgs& a, const CachePlan& plan, const Place& p) {
+template <class Args>
+__device__ __forceinline__ Range open_range(const Args& a, const CachePlan& plan, const Place& p) {
+  if constexpr (Args::kPrefix) return open_prefix(a, plan, p);
   Range range{};
   if (plan.split) {
     range = find_range(a, plan, p.w);
@@ -426,21 +554,40 @@ __device__ __forceinline__ Range open_range(const CacheAttentionArgs& a, const C
       if (range.begin < range.end && range.begin > range.at && range.at >= range.begin - range.per)
         join = int4{divide(range.at + range.units - 1, range.per) - p.w + 2, range.seq.first, range.seq.tokens * a.G, range.tile};
       partials(a, plan).joins[p.w] = join;
+      if constexpr (Args::kShaped)
+        if (a.shared) a.join_prefix[p.w] = int2{shared_keys(a, range.seq), range.seq.prefix};
     }
   } else {  // range w: row tile w % row_tiles of sequence w / row_tiles
     range.b = divide(p.w, plan.row_tiles);
     range.tile = p.w - range.b * plan.row_tiles;
     range.seq = sequence(a, range.b);
     range.tiles = row_tiles_of(a, plan, range.seq);
-    range.units = units_of(range.seq);
+    range.units = units_of(a, plan, range.seq);
     range.end = range.tile < range.tiles ? range.units : 0;
   }
   return range;
 }
 
+// The range's part of its row tile: keys [begin, end).
+struct Part {
+  int begin, end, stop;  // stop: place of the line where it ends
+  bool whole, first;     // all keys of the row tile; its first piece
+  int common;            // keys below are seen by every row of the tile (from `from` on)
+  int tree_tokens;       // new tokens that have a bit in the tree
+  int low, from;         // with a window: keys below are seen by no row, by not every row
+};
+// Where a row of the range's row tile (for the shared prefix: any row, store_columns adds its number) has its piece.
+template <class Args>
+__device__ __forceinline__ int64_t piece_row(const Args& a, const CachePlan& plan, const Range& range, const Place& place,
+                                             const Part& part, int row) {
+  if constexpr (Args::kPrefix) return range.piece * a.n * a.Hq;
+  else return partial_row(a, plan, place.w, part.first ? 1 : 0, place.head) + row;
+}
+
 // Goes on to the next row tile, which begins at place `stop`; false at the end of the range.
-__device__ __forceinline__ bool next_tile(const CacheAttentionArgs& a, const CachePlan& plan, int stop, Range& range) {
-  if (stop >= range.end) return false;
+template <class Args>
+__device__ __forceinline__ bool next_tile(const Args& a, const CachePlan& plan, int stop, Range& range) {
+  if (Args::kPrefix || stop >= range.end) return false;
   if (++range.tile >= range.tiles) {
     range.tile = 0;
     do {
@@ -448,49 +595,136 @@ __device__ __forceinline__ bool next_tile(const CacheAttentionArgs& a, const Cac
       range.seq = sequence(a, range.b);
       range.tiles = row_tiles_of(a, plan, range.seq);
     } while (range.tiles == 0);
-    range.units = units_of(range.seq);
+    range.units = units_of(a, plan, range.seq);
   }
   range.at = stop + kSetup;
   return true;
 }
 
-// The range's part of its row tile: keys [begin, end).
-struct Part {
-  int begin, end, stop;  // stop: place of the line where it ends
-  bool whole, first;     // all keys of the row tile; its first piece
-  int common;            // keys below are seen by every row of the tile
-  int tree_tokens;       // new tokens that have a bit in the tree
-};
-__device__ __forceinline__ bool open_part(const CacheAttentionArgs& a, const CachePlan& plan, const Range& range,
-                                          Part* part) {
+template <class Args>
+__device__ __forceinline__ bool open_part(const Args& a, const CachePlan& plan, const Range& range, Part* part) {
   const Sequence& seq = range.seq;
   const int from = range.begin > range.at ? range.begin : range.at, seq_end = range.at + range.units;
   part->stop = seq_end < range.end ? seq_end : range.end;
   if (from >= part->stop) return false;  // only places of its setup are left of the range
   part->first = from == range.at;
   part->whole = part->first && part->stop == seq_end;
-  part->begin = (from - range.at) * kUnit;
-  part->end = part->stop < seq_end ? (part->stop - range.at) * kUnit : seq.keys;
+  const int key0 = first_key(a, plan, seq, range.tile);
+  part->begin = key0 + (from - range.at) * kUnit;
+  part->end = part->stop < seq_end ? key0 + (part->stop - range.at) * kUnit : seq.keys;
+  part->low = part->from = 0;
   const int rows = seq.tokens * a.G, row0 = range.tile * plan.tile, row1 = row0 + plan.tile < rows ? row0 + plan.tile : rows;
   if (a.tree) {
     part->common = seq.prefix;
   } else {  // causal: the first and the last row's token
-    const int last = seq.prefix + divide(row1 - 1, a.G) + 1;
+    int last = seq.prefix + divide(row1 - 1, a.G) + 1;
     part->common = seq.prefix + divide(row0, a.G) + 1;
+    if constexpr (Args::kShaped) {
+      if (a.window) {
+        part->low = part->common - a.window;
+        part->from = last - a.window;
+      }
+      if (a.open_keys) {
+        const int open = a.open_keys[range.b];
+        last = last > open ? last : open;
+        part->common = part->common > open ? part->common : open;
+      }
+    }
     part->end = part->end > last ? last : part->end;
   }
+  // (a window's units may reach past the keys, and a prefix may be longer than they are)
+  if constexpr (Args::kShaped) part->end = part->end > seq.keys ? seq.keys : part->end;
   part->common = part->common > seq.keys ? seq.keys : part->common;
   part->tree_tokens = seq.keys - seq.prefix;
   part->tree_tokens = part->tree_tokens > 64 * a.tree_words ? 64 * a.tree_words : part->tree_tokens;
   return true;
 }
 
-// Keys key .. key + 7 that a row of token t sees.
-__device__ __forceinline__ unsigned row_sees(const CacheAttentionArgs& a, const Sequence& seq, const Part& part, int t,
-                                             int key) {
+// Keys key .. key + 7 that a row of token t of sequence b sees.
+template <class Args>
+__device__ __forceinline__ unsigned row_sees(const Args& a, const Sequence& seq, const Part& part, int b, int t, int key) {
   int limit = a.tree ? seq.prefix : seq.prefix + t + 1;
+  unsigned hidden = 0;
+  if constexpr (Args::kShaped) {
+    if (a.window) hidden = below(limit - a.window - key);
+    if (a.open_keys) {
+      const int open = a.open_keys[b];
+      limit = limit > open ? limit : open;
+    }
+  }
   limit = limit > seq.keys ? seq.keys : limit;
-  return seen8(limit, a.tree + (int64_t)(seq.first + t) * a.tree_words, key, seq.prefix, part.tree_tokens, a.tree_words);
+  return ~hidden & seen8(limit, a.tree + (int64_t)(seq.first + t) * a.tree_words, key, seq.prefix, part.tree_tokens, a.tree_words);
+}
+
+// Whether keys [key, key + n) hide one from some row of the tile (their pages aside).
+template <class Args>
+__device__ __forceinline__ bool some_hidden(const Args& a, const Part& part, int key, int n) {
+  return key + n > part.common || (Args::kShaped && key < part.from);
+}
+// Of keys key .. key + 7 below `end`, those that some row may see.
+template <class Args>
+__device__ __forceinline__ unsigned may_see(const Args& a, const Part& part, int end, int key) {
+  unsigned see = below(end - key);
+  if constexpr (Args::kShaped) see &= ~below(part.low - key);
+  return see;
+}
+
+// How a product of codes q . k becomes the exponent of a probability, in binades.  Plain: times `factor`.  Shaped,
+// y = C tanh(z / c) - slope |distance| with z = softmax_scale q . k and C = c log2(e), which the scores
+// are replaced by; their factor is then 1.
+struct ScoreShape {
+  float factor;
+  float inside, cap;  // z / c of a product; C (0: no cap)
+  bool on;
+};
+template <bool FP8, class Args>
+__device__ __forceinline__ ScoreShape score_shape(const Args& a) {
+  ScoreShape s{};
+  const float z = a.softmax_scale * (FP8 ? 1.0f : 1.0f / 6.0f);
+  s.factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
+  if constexpr (Args::kShaped) {
+    s.on = a.softcap > 0.0f || a.slopes;
+    s.inside = a.softcap > 0.0f ? z / a.softcap : s.factor;
+    s.cap = a.softcap * kLog2e;
+    if (s.on) s.factor = 1.0f;
+  }
+  return s;
+}
+// A row's slope in binades, and the token's place that its distances count from.
+struct RowBias {
+  float slope;
+  int at;
+};
+template <class Args>
+__device__ __forceinline__ RowBias row_bias(const Args& a, const Sequence& seq, int token, int head) {
+  RowBias r{0.0f, 0};
+  if constexpr (Args::kShaped) {
+    if (a.slopes) r.slope = a.slopes[head] * kLog2e;
+    r.at = Args::kPrefix ? seq.keys : seq.prefix + token;
+  }
+  return r;
+}
+// tanh(x) / x = P(x^2) for |x| <= 0.8, a least-squares fit weighted until its largest relative errors were equal: 5.8e-8, a half
+// step of fp32; beyond, 1 - 2 / (e^2x + 1), where nothing cancels.
+constexpr float kTanhNear = 0.8f;
+__device__ __forceinline__ float tanh_near(float x) {
+  const float u = x * x;
+  return x * fmaf(fmaf(fmaf(fmaf(fmaf(-0.00435529975f, u, 0.0190933011f), u, -0.0531143174f), u, 0.13321048f), u, -0.333326757f), u, 0.99999994f);
+}
+__device__ __forceinline__ float tanh_far(float x) {
+  return fmaf(-2.0f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.0f * kLog2e)) + 1.0f), 1.0f);
+}
+// A lane's eight scores, of keys key .. key + 7.
+template <class Args>
+__device__ __forceinline__ void shape_scores(const Args& a, const ScoreShape& shape, const RowBias& bias, int key, v4f (&s)[2]) {
+  const float far = (float)(bias.at - key);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float x = s[j / 4][j % 4] * shape.inside;
+    if (shape.cap > 0.0f) x = shape.cap * (fabsf(x) <= kTanhNear ? tanh_near(x) : tanh_far(x));
+    if (a.slopes) x = fmaf(-bias.slope, fabsf(far - (float)j), x);
+    s[j / 4][j % 4] = x;
+  }
 }
 
 }  // namespace fp4attn

@@ -1,7 +1,7 @@
 // Attention over the cache for many rows (tokens times heads of a group): trees of drafted
 // tokens, chunks of a prompt.
 //
-// The same mathematics and operand orders as cache_attention.hip; what bounds it is another:
+// The same mathematics and operand orders as cache_attention_tiles.hpp; what bounds it is another:
 // with 128 rows a key costs 128 * 4 D flop and 136 bytes (MXFP4, D 128), so the matrix unit and the
 // softmax's vector work do, and turning codes into bf16 must not be repeated by every wave.
 // The four waves of a workgroup take 32 rows each and walk the same keys; the codes of a step of 64
@@ -16,6 +16,8 @@
 // Counters of the first: the matrix unit is busy 33 % of the time, vector instructions take 42 %, LDS 33 %; two waves a SIMD
 // overlap them in part.  Work put between the products of the same wave (converting V and K, the second tile's
 // probabilities) made it 1 to 3 % slower, four sums side by side in the K products changed nothing.
+#pragma once
+
 #include "cache_attention.hpp"
 
 namespace fp4attn {
@@ -121,8 +123,8 @@ struct Share {
   }
 };
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const CacheAttentionArgs a, const CachePlan plan) {
+template <int D, bool FP8, class Args>
+__global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const Args a, const CachePlan plan) {
   using F = Format<D, FP8>;
   using Codes = Share<D, FP8>;
   constexpr int kRing = FP8 && D == 128 ? 2 : 3;  // steps whose codes are in LDS or on the way (LDS for two workgroups)
@@ -138,7 +140,8 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
   if (head >= a.c.H) return;
   Range range = open_range(a, plan, place);
   if (range.begin >= range.end) return;
-  const float factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
+  const ScoreShape shape = score_shape<FP8>(a);
+  const float factor = shape.factor;
 
   // Of a CU's two workgroups the one that came first, of the first half of the grid, is served first: a step took it
   // 2.17 us and the other 2.62, and it ended 60 us of 370 earlier.  The later one goes before it in every
@@ -151,12 +154,14 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
     int token[kNr];  // of the sequence
+    RowBias bias[kNr];
     v4i q[kNr][F::kSteps];
 #pragma unroll
     for (int r = 0; r < kNr; ++r) {
       const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
       token[r] = divide(ic, a.G);
       const int h = head * a.G + (ic - token[r] * a.G);
+      bias[r] = row_bias(a, seq, token[r], h);
       const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
 #pragma unroll
       for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
@@ -201,10 +206,10 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         k_lds[my_tile][half][st][lane] = kk;
       });
       const bool page0 = is_page(a.c, pages.p0), page1 = is_page(a.c, pages.p1);
-      if (key0 + kTile > part.common || !page0 || !page1) {
+      if (some_hidden(a, part, key0, kTile) || !page0 || !page1) {
         // Keys that no row sees hold anything: their V codes and scales become zero.  A
         // non-finite block of the others becomes zero too, as a NaN code of MXFP8 does, and is looked for by the rows.
-        const unsigned there = (g >= 2 ? page1 : page0) ? below(part.end - (key0 + 8 * g)) >> (4 * half) : 0u;
+        const unsigned there = (g >= 2 ? page1 : page0) ? may_see(a, part, part.end, key0 + 8 * g) >> (4 * half) : 0u;
         unsigned odd = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -271,7 +276,13 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 #pragma unroll
           for (int r = 0; r < kNr; ++r) s[r][i / 2][i % 2] = mfma_16x16x32(kk[i][st], q[r][st], s[r][i / 2][i % 2]);
       }
-      bool all = key0 + kKeys <= part.common;
+      if constexpr (Args::kShaped)
+        if (shape.on)
+#pragma unroll
+          for (int tile = 0; tile < kTiles; ++tile)
+#pragma unroll
+            for (int r = 0; r < kNr; ++r) shape_scores(a, shape, bias[r], key0 + kTile * tile + 8 * g, s[r][tile]);
+      bool all = !some_hidden(a, part, key0, kKeys);
 #pragma unroll
       for (int tile = 0; tile < kTiles; ++tile) all = all && is_page(a.c, pages[tile].p0) && is_page(a.c, pages[tile].p1);
       if (!all) {  // uniform
@@ -279,16 +290,16 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         for (int tile = 0; tile < kTiles; ++tile) {
           const int first = key0 + kTile * tile, base = first + 8 * g;
           const bool page0 = is_page(a.c, pages[tile].p0), page1 = is_page(a.c, pages[tile].p1);
-          const unsigned there = (g >= 2 ? page1 : page0) ? below(part.end - base) : 0u;
+          const unsigned there = (g >= 2 ? page1 : page0) ? may_see(a, part, part.end, base) : 0u;
           unsigned see[kNr];
 #pragma unroll
           for (int r = 0; r < kNr; ++r) {
-            see[r] = there & row_sees(a, seq, part, token[r], base);
+            see[r] = there & row_sees(a, seq, part, range.b, token[r], base);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               s[r][tile][j / 4][j % 4] = see[r] >> j & 1 ? s[r][tile][j / 4][j % 4] : -__builtin_inff();
           }
-          const bool looked = first + kTile > part.common || !page0 || !page1;  // as convert did
+          const bool looked = some_hidden(a, part, first, kTile) || !page0 || !page1;  // as convert did
           if (looked && (odd_lds[tile][0] | odd_lds[tile][1])) {
 #pragma unroll
             for (int r = 0; r < kNr; ++r) see[r] = groups_or(see[r] << (8 * g));
@@ -393,13 +404,13 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       const int i = row0 + 16 * r + m;
       const float total = groups_sum(sum[r]);
       if (i >= rows) continue;
-      const int64_t piece = partial_row(a, plan, place.w, part.first ? 1 : 0, head) + (16 * kNr * wave + 16 * r + m);
+      const int64_t piece = piece_row(a, plan, range, place, part, 16 * kNr * wave + 16 * r + m);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float o[F::kDTiles];
 #pragma unroll
         for (int t = 0; t < F::kDTiles; ++t) o[t] = acc[r][t][j];
-        store_columns<D, FP8>(a, plan, seq, i, head, 4 * g + j, part.whole, piece, ref[r], total, sum16[r][0],
+        store_columns<D, FP8>(a, plan, seq, i, head, 4 * g + j, !Args::kPrefix && part.whole, piece, ref[r], total, sum16[r][0],
                               odd_marks.template of<F::kDTiles>(r, j), o);
       }
     }
@@ -408,14 +419,11 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
   }
 }
 
-}  // namespace
-
-void launch_cache_rows(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream) {
-  const unsigned grid = (unsigned)plan.workgroups;
-  if (a.c.d == 64 && a.c.fp8) cache_rows_kernel<64, true><<<grid, kThreads, 0, stream>>>(a, plan);
-  else if (a.c.d == 64) cache_rows_kernel<64, false><<<grid, kThreads, 0, stream>>>(a, plan);
-  else if (a.c.fp8) cache_rows_kernel<128, true><<<grid, kThreads, 0, stream>>>(a, plan);
-  else cache_rows_kernel<128, false><<<grid, kThreads, 0, stream>>>(a, plan);
+template <int D, bool FP8, class Args>
+void launch_rows(const Args& a, const CachePlan& plan, hipStream_t stream) {
+  cache_rows_kernel<D, FP8><<<(unsigned)plan.workgroups, kThreads, 0, stream>>>(a, plan);
 }
+
+}  // namespace
 
 }  // namespace fp4attn

@@ -31,6 +31,11 @@ constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 // sequences of 16384 keys and 8 key heads; at three waves 140.)
 constexpr int waves_per_simd(int d, int nr) { return 6 - d / 64 - nr; }
 
+// Units that a row tile touches of which every token sees `window` keys, wherever they begin.
+constexpr int window_units(int tile, int G, int window) {
+  return (window + (tile + G - 2) / G + kUnit - 2) / kUnit + 1;
+}
+
 inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t max_keys) {
   CachePlan p{};
   const int64_t rows = max_q * G, units = (max_keys + kUnit - 1) / kUnit;
@@ -79,5 +84,37 @@ inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8
   if (p.split) p.workspace = ranges * 16 + ranges * 2 * H * p.tile_rows * (d * 4 + 16);
   return p;
 }
+
+// The pass over a prefix of `keys` keys (whole units) that the sequences share: all n tokens' rows of a key head together in
+// row tiles, each with `pieces` parts of the prefix of `units` units, one to a workgroup.
+struct PrefixPlan {
+  CachePlan plan;
+  int pieces, units;
+  bool fits;
+  int64_t rows;  // n * H * G: of each piece
+};
+inline PrefixPlan prefix_plan(int64_t H, int64_t G, int64_t d, int64_t n, int64_t keys) {
+  PrefixPlan p{};
+  const int64_t rows = n * G, units = keys / kUnit;
+  CachePlan& c = p.plan;
+  c.tile = rows <= 16 ? 16 : (rows <= 64 ? 32 : kRowsTile);
+  const int64_t row_tiles = (rows + c.tile - 1) / c.tile;
+  c.row_tiles = (int)row_tiles;
+  c.tile_rows = (int)(rows < c.tile ? rows : c.tile);
+  const int64_t slots = 256 * (c.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, c.tile / 16));
+  int64_t pieces = slots / (row_tiles * H);
+  pieces = pieces < 1 ? 1 : (pieces > 16 ? 16 : pieces);
+  const int64_t per = (units + pieces - 1) / pieces;
+  p.units = (int)per;
+  p.pieces = (int)((units + per - 1) / per);
+  c.ranges = (int)(row_tiles * p.pieces);
+  c.workgroups = (row_tiles * p.pieces * H + 7) / 8 * 8;
+  p.rows = rows * H;
+  p.fits = c.workgroups <= 1 << 24;
+  return p;
+}
+
+// Whether the shared prefix gets a pass of its own.
+inline bool shares_prefix(int64_t B, int64_t G, int64_t max_q, int64_t keys) { return B > 1 && keys >= kUnit && max_q * G < kRowsTile; }
 
 }  // namespace fp4attn

@@ -81,6 +81,7 @@ hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream);
 struct CachePlan;  // cache_plan.hpp
 
 struct CacheAttentionArgs {
+  static constexpr bool kShaped = false, kPrefix = false;
   CacheView c;
   const void* q;
   int64_t q_stride;  // of a token, in elements
@@ -98,7 +99,27 @@ struct CacheAttentionArgs {
   void* workspace;
 };
 
-void launch_cache_rows(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
-hipError_t launch_cache_attention(const CacheAttentionArgs& a, hipStream_t stream);
+// Attention with shaped scores, other masks, a shared prefix.
+struct ShapedAttentionArgs : CacheAttentionArgs {
+  static constexpr bool kShaped = true;
+  float softcap;         // 0: none
+  int window;            // keys that a token sees up to its own, 0: all
+  const float* slopes;   // [Hq] or null
+  const int* open_keys;  // [B] keys that every new token sees, or null
+  // the shared prefix: its keys (a multiple of kUnit; 0: none), passed over in pieces of prefix_units units; of every
+  // piece and row of q {reference, sum, sum of the rounded values} and the accumulators
+  int shared, prefix_pieces, prefix_units;
+  float4* prefix_stat;  // [pieces][n * Hq]
+  float* prefix_acc;    // [pieces][n * Hq][d]
+  int2* join_prefix;    // [ranges] of the sequence in joins: its shared keys, keys before its new tokens
+};
+// The pass over the shared prefix itself.
+struct PrefixAttentionArgs : ShapedAttentionArgs {
+  static constexpr bool kPrefix = true;
+};
+
+hipError_t launch_cache_attention(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
+hipError_t launch_shaped_attention(const ShapedAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
+hipError_t launch_prefix_attention(const PrefixAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 
 }  // namespace fp4attn

@@ -1,0 +1,365 @@
+"""Attention over the cache with capped scores, biases by distance, windows, prefix masks and a shared prefix,
+against the fp64 oracle.
+
+Tolerances: those of plain attention over the cache (test_gpu_serving.py: P's rounding to bf16, 2^-8 of the weighted
+mean of |v - o|; sums, the exponential, scores), u = 2^-24, and of a score z with |z| <= high after the cap and a bias of
+magnitude `bias`:
+* the cap: its argument by 4 u relative; tanh by 3 u near zero (2.6 half steps of the fit as it is evaluated), beyond by at most
+  11 u (the exponential's argument 5 u, itself 2 u, the reciprocal 2 u, at |x| = 0.8, where they weigh most); two
+  products: 20 u high with all of them;
+* the bias: slope log2(e), the distance, its product and the sum, and with a shared prefix the step between the two
+  places that distances count from: 8 u (bias + high).
+Errors of the scores move the output by twice their sum times the weighted mean of |v|.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving
+from test_gpu_serving import FORMATS, HALF_STEP, U, Batch, _beside_idle, _f64, _tree
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fa():
+    import paper_2609_04105_amd as fa
+    return fa
+
+
+def _values(b, i):
+    """K and V [n, H, d] of a sequence, by the cache's documented layout (test_gpu_serving.py checks it key by key)."""
+    (p, off), (kc, ks, vc, vs) = divmod(b.slots[i], b.page), b.cache
+    if len(p) == 0:
+        return np.zeros((2, 0, b.H, b.d))
+    v = vc[p, :, off // 8, :, off % 8].reshape(len(p), b.H, -1)
+    return serving.values(kc[p, :, off], ks[p, :, off], b.fp8), serving.values(v, vs[p, :, off // 8, :, off % 8], b.fp8)
+
+
+def _check(b, out, lse=None, tree=None, softcap=None, slopes=None, window=None, prefix=None, only=None):
+    """out [n, Hq, d] and lse against the oracle."""
+    out_dtype, out = out.dtype, _f64(out)
+    for i, (t, n) in enumerate(zip(b.new, b.keys)):
+        if t == 0 or (only is not None and i not in only):
+            continue
+        rows = slice(b.starts[i], b.starts[i] + t)
+        k, v = _values(b, i)
+        if tree is not None:
+            see = serving.tree_mask(tree[rows].reshape(t, -1).view(np.uint64), t, n, n)
+        else:
+            see = serving.shaped_mask(t, n, n, window or 0, 0 if prefix is None else int(prefix[i]))
+        o, norm, spread, size, reach, high, bias = serving.shaped_attention(
+            _f64(b.q[rows]), np.nan_to_num(k), np.nan_to_num(v), see, b.scale, softcap or 0.0,
+            None if slopes is None else _f64(slopes), n)
+        e = 2 * ((b.d + 4) * U * reach + 20 * U * high + 8 * U * (bias + high) + (n + 64) * 2 * U + 4 * U)
+        tol = 2.0 ** -8 * (1 + 2.0 ** -7) * spread + e[..., None] * size
+        tol += HALF_STEP[out_dtype] * (np.abs(o) + tol)
+        err = np.abs(out[rows] - o)
+        assert np.all(err <= tol), f"sequence {i}: {np.max(err / np.maximum(tol, 1e-300)):.3g} of the tolerance"
+        if lse is not None:
+            got = _f64(lse[rows])
+            assert np.array_equal(np.isneginf(got), np.isneginf(norm)), i
+            fin = np.isfinite(norm)
+            got, norm, e = got[fin], norm[fin], e[fin]
+            assert np.all(np.abs(got - norm) <= e + 4 * U * np.abs(norm) + 8 * U), i
+
+
+def _gpu(x, dtype):
+    return None if x is None else torch.tensor(x, dtype=dtype, device="cuda")
+
+
+def _run(fa, b, tree=None, softcap=None, slopes=None, window=None, prefix=None, check=True, only=None, **o):
+    """One call with the normaliser, checked."""
+    slopes, lse = _gpu(slopes, torch.float32), torch.empty((b.q.shape[0], b.H * b.G), device="cuda")
+    out = b.call(fa, tree=tree, lse=lse, softcap=softcap, slopes=slopes, window=window, prefix=_gpu(prefix, torch.int32), **o)
+    if check:
+        _check(b, out, lse, tree, softcap, slopes, window, prefix, only)
+    return out, lse
+
+
+def _slopes(H):
+    return [2.0 ** (-8.0 * (h + 1) / H) for h in range(H)]
+
+
+# batches that reach every row tile, alone and in a chip full of them, cut and whole
+TILINGS = [(2, [1, 1, 1, 1], [517, 33, 1, 0], 0, 1), (16, [1, 1], [1300, 95], 0, 6000), (3, [4, 1, 7], [300, 130, 7], 0, 1),
+           (8, [30, 3, 0, 17], [400, 1100, 5, 17], 0, 6000), (3, [130, 5], [700, 260], 512, 1), (20, [9, 11], [900, 1500], 512, 6000)]
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,new,keys,idle,width", TILINGS)
+@pytest.mark.parametrize("softcap", [0.25, 3.0, 50.0, 1e6])
+def test_softcap(fa, softcap, G, new, keys, idle, width, d, fp8):
+    b = Batch(keys, new, 2, G, d, fp8, 32, seed=G + d)
+    _beside_idle(b, idle, width)
+    _run(fa, b, softcap=softcap)
+    if softcap == 3.0 and max(new) > 1:
+        tree = _tree(b.new, 3, G)
+        _run(fa, b, tree=tree, softcap=softcap)
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,new,keys,idle,width", TILINGS)
+@pytest.mark.parametrize("kind", ["geometric", "both signs", "with softcap"])
+def test_slopes(fa, kind, G, new, keys, idle, width, d, fp8):
+    b = Batch(keys, new, 2, G, d, fp8, 16, seed=G + d)
+    _beside_idle(b, idle, width)
+    slopes = _slopes(2 * G)
+    if kind == "both signs":
+        slopes = [(-1) ** h * 0.01 * h for h in range(2 * G)]
+    _run(fa, b, slopes=slopes, softcap=5.0 if kind == "with softcap" else None)
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,new,keys,idle,width", TILINGS)
+@pytest.mark.parametrize("window", [1, 31, 33, 128, 250, 1 << 30])
+def test_window(fa, window, G, new, keys, idle, width, d, fp8):
+    """Keys behind the window: their pages are gone, those on the window's first page are not numbers."""
+    b = Batch(keys, new, 2, G, d, fp8, 16, seed=G + d)
+    _beside_idle(b, idle, width)
+    for i, (t, n) in enumerate(zip(b.new, b.keys)):
+        low = n - t + 1 - window
+        if t == 0 or low <= 0:
+            continue
+        b.table[i, : low // 16] = -1
+        for j in range(low // 16 * 16, low):
+            p, off = divmod(int(b.slots[i][j]), 16)
+            for s, at in zip(b.cache, (off, off, (off // 8, slice(None), off % 8), (off // 8, slice(None), off % 8))):
+                s[(p, slice(None)) + (at if isinstance(at, tuple) else (at,))] = 0xFF
+    out, _ = _run(fa, b, window=window)
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,new,keys,idle,width", TILINGS)
+def test_prefix_mask(fa, G, new, keys, idle, width, d, fp8):
+    b = Batch(keys, new, 2, G, d, fp8, 16, seed=G + d)
+    _beside_idle(b, idle, width)
+    for share in (0.0, 0.7, 1.0, 2.0):
+        prefix = [int(share * n) - (3 if i % 2 else 0) for i, n in enumerate(b.keys)]
+        _run(fa, b, prefix=prefix)
+    prefix = [n - t // 2 for t, n in zip(b.new, b.keys)]
+    _run(fa, b, prefix=prefix, slopes=_slopes(2 * G), softcap=4.0)
+    for window in (1, 40, 300):
+        _run(fa, b, prefix=prefix, window=window, slopes=_slopes(2 * G))
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("window", [16, 1000])
+def test_long_window_calls(fa, window, d, fp8):
+    """Sequences far longer than their window, cut into ranges; single tokens and chunks."""
+    for new in ([1, 1, 1], [40, 3, 65]):
+        b = Batch([5000, 2100, 300], new, 2, 4, d, fp8, 64, seed=d + window)
+        _run(fa, b, window=window)
+        _run(fa, b, window=window, softcap=6.0, slopes=_slopes(8))
+        assert b.call(fa, window=window, out_dtype=torch.bfloat16).dtype == torch.bfloat16
+
+
+def test_options_that_change_nothing(fa):
+    b = Batch([300, 77, 3], [3, 2, 3], 2, 3, 128, False, 32, seed=1)
+    for o in ({}, dict(window=301), dict(window=1 << 30), dict(prefix=[0, -5, 0]), dict(slopes=[0.0] * 6), dict(slopes=[-0.0] * 6)):
+        out, lse = _run(fa, b, **o)
+        _check(b, out, lse)
+
+
+def test_odd_lengths(fa):
+    """Lengths past the table, below zero and shorter than the new tokens, with every option."""
+    b = Batch([192, 150, 130], [2, 2, 3], 2, 3, 128, False, 16, seed=4, spare=0)
+    real = list(b.keys)
+    k, v = serving.key_values(b.cache, b.slots[0], False)
+    for more in (0, 50):
+        length = 192 + more
+        b.keys[0] = length
+        for o in (dict(window=70), dict(slopes=_slopes(6)), dict(prefix=[100, 20, 130], softcap=2.0)):
+            out, _ = _run(fa, b, only=(1, 2), **o)
+            see = serving.shaped_mask(2, 192, length, o.get("window", 0), o.get("prefix", [0])[0])
+            want, _, spread, size, *_ = serving.shaped_attention(_f64(b.q[:2]), k, v, see, b.scale, o.get("softcap", 0.0),
+                                                                 o.get("slopes"), length)
+            assert np.all(np.abs(_f64(out[:2]) - want) <= 2.0 ** -8 * (1 + 2.0 ** -7) * spread + 2.0 ** -14 * size)
+    b.keys = [-5, 1, 130]
+    for o in (dict(window=70), dict(slopes=_slopes(6)), dict(softcap=2.0), dict(prefix=[100, 0, 0])):
+        out, lse = _run(fa, b, check=False, **o)
+        assert not out[:3].any() and torch.isneginf(lse[:3]).all() and torch.isfinite(lse[3:]).all()
+    b.keys = real
+    _run(fa, b, window=9)
+
+
+@pytest.mark.parametrize("o", [dict(softcap=2.0), dict(slopes=_slopes(4)), dict(window=30), dict(prefix=[47])])
+def test_hidden_values_never_reach_a_row(fa, o):
+    """NaN keys and value blocks of keys that a row does not see; rows that see one are NaN (values: in its 32 channels)."""
+    for d, fp8 in FORMATS:
+        b = Batch([50], [6], 2, 2, d, fp8, 16, seed=9)
+        clean, _ = _run(fa, b, **o)
+
+        def at(key):
+            return divmod(int(b.slots[0][key]), 16)
+        # the last key but one: a value block of head 0; the last: a key block of head 1
+        p, off = at(48)
+        b.cache[3][p, 0, off // 8, 1, off % 8] = 255
+        p, off = at(49)
+        b.cache[1][p, 1, off, 0] = 255
+        out, _ = _run(fa, b, check=False, **o)
+        bad = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+        bad[4:, :2, 32:64] = True
+        bad[5:, 2:] = True
+        assert torch.equal(~torch.isfinite(out), bad) and torch.equal(out[~bad], clean[~bad])
+        if "window" in o:   # the first rows see key 16, the later ones do not
+            b = Batch([50], [6], 2, 2, d, fp8, 16, seed=9)
+            p, off = at(16)
+            b.cache[1][p, 1, off, 0] = b.cache[3][p, 0, off // 8, 1, off % 8] = 255
+            out, _ = _run(fa, b, check=False, **o)
+            bad.zero_()
+            bad[:2, :2, 32:64] = True      # tokens at 44, 45: keys from 15, 16
+            bad[:2, 2:] = True
+            assert torch.equal(~torch.isfinite(out), bad) and torch.equal(out[~bad], clean[~bad])
+
+
+# ---------------------------------------------------------------- a shared prefix
+
+def _share(b, shared):
+    """Gives every sequence the first `shared` keys of the longest: whole pages in common, the rest copied."""
+    first = int(np.argmax(b.keys))
+    page = b.page
+    for i, n in enumerate(b.keys):
+        m = min(n, shared)
+        if i == first or m == 0:
+            continue
+        b.table[i, : m // page] = b.table[first, : m // page]
+        j = np.arange(n)
+        b.slots[i] = b.table[i][j // page].astype(np.int64) * page + j % page
+        for key in range(m // page * page, m):
+            (p, off), (r, at) = (divmod(int(b.slots[x][key]), page) for x in (i, first))
+            for s in b.cache[:2]:
+                s[p, :, off] = s[r, :, at]
+            for s in b.cache[2:]:
+                s[p, :, off // 8, :, off % 8] = s[r, :, at // 8, :, at % 8]
+    return b
+
+
+SHARED = [([1] * 5, [300, 260, 257, 400, 290], 256), ([1] * 3, [700, 0, 650], 600), ([1] * 2, [2000, 1400], 1331),
+          ([3, 1, 5, 0, 2], [400, 300, 270, 500, 310], 265), ([1] * 4, [129, 130, 128, 200], 128), ([9, 7], [900, 800], 777),
+          ([1] * 70, [200 + i for i in range(70)], 190), ([2, 2, 2], [1500, 40, 1501], 1400), ([1] * 4, [260, 256, 257, 255], 256)]
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,page,width", [(1, 16, 1), (4, 64, 1), (8, 32, 6000), (3, 256, 1)])
+@pytest.mark.parametrize("new,keys,shared", SHARED)
+def test_shared_prefix(fa, new, keys, shared, G, page, width, d, fp8):
+    """Sequences behind one prefix, of whole pages or not, beside idle ones and ones that end inside the prefix."""
+    if len(new) > 10 and (G, page) != (4, 64):
+        new, keys = new[:9], keys[:9]
+    b = _share(Batch(keys, new, 2, G, d, fp8, page, seed=G + len(new)), shared)
+    _beside_idle(b, 0, width)
+    _run(fa, b, shared=shared)
+    if d == 128:
+        _run(fa, b, shared=shared, softcap=3.0, slopes=_slopes(2 * G))
+        tree = _tree(b.new, 1, G)
+        _run(fa, b, tree=tree, shared=shared, softcap=8.0)
+        _run(fa, b, shared=shared, prefix=[n - t // 2 for t, n in zip(b.new, b.keys)], slopes=_slopes(2 * G))
+        _run(fa, b, shared=shared, window=200)
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+def test_shared_prefix_of_a_large_batch(fa, d, fp8):
+    """Rows enough for row tiles of 128, and single tokens without row starts."""
+    b = _share(Batch([2100 + 7 * i for i in range(48)], [1] * 48, 1, 8, d, fp8, 64, seed=3), 2000)
+    out, lse = _run(fa, b, shared=2000, starts=False)
+    again, norm = _run(fa, b, shared=2000, starts=False, check=False)
+    assert torch.equal(out, again) and torch.equal(lse, norm)
+    b = _share(Batch([1200 + 9 * i for i in range(12)], [13 - i for i in range(12)], 2, 4, d, fp8, 32, seed=3), 1100)
+    _run(fa, b, shared=1100)
+
+
+def test_shared_prefix_values(fa):
+    """A NaN in the prefix reaches every row that sees it; one behind it its own sequence; queries stay apart."""
+    for d, fp8 in FORMATS:
+        b = _share(Batch([400, 300, 290], [1, 1, 1], 2, 4, d, fp8, 16, seed=2), 256)
+        clean, _ = _run(fa, b, shared=256)
+        p, off = divmod(int(b.slots[0][70]), 16)
+        b.cache[3][p, 0, off // 8, 1, off % 8] = 255
+        out, _ = _run(fa, b, check=False, shared=256)
+        assert torch.isnan(out[:, :4, 32:64]).all()
+        out[:, :4, 32:64] = clean[:, :4, 32:64]
+        assert torch.equal(out, clean)
+        b.cache[3][p, 0, off // 8, 1, off % 8] = 120
+        b.cache[1][p, 1, off, 0] = 255
+        out, _ = _run(fa, b, check=False, shared=256)
+        assert torch.isnan(out[:, 4:]).all() and torch.isfinite(out[:, :4]).all()
+        b.cache[1][p, 1, off, 0] = 120
+        p, off = divmod(int(b.slots[1][270]), 16)
+        b.cache[1][p, 1, off, 0] = 255
+        out, _ = _run(fa, b, check=False, shared=256)
+        assert torch.isnan(out[1, 4:]).all() and torch.isfinite(out[1, :4]).all() and torch.isfinite(out[[0, 2]]).all()
+        b.cache[1][p, 1, off, 0] = 120
+        b.q[2, 3, 5] = float("nan")
+        out, _ = _run(fa, b, check=False, shared=256)
+        assert torch.isnan(out[2, 3]).all() and torch.isfinite(out[2, :3]).all() and torch.isfinite(out[:2]).all()
+
+
+def test_shared_prefix_rows_of_no_sequence_stay(fa):
+    b = _share(Batch([300, 290], [3, 5], 1, 4, 128, True, 32, seed=6), 256)
+    b.q = torch.cat((b.q[:2], b.q, torch.full_like(b.q[:3], float("nan"))))
+    b.starts += 2
+    out, lse = torch.full((13, 4, 128), 7.0, device="cuda"), torch.full((13, 4), 7.0, device="cuda")
+    assert b.call(fa, out=out, lse=lse, shared=256) is out
+    _check(b, out, lse)
+    want = out.clone()
+    assert bool((out[:2] == 7).all() and (out[10:] == 7).all() and (lse[:2] == 7).all() and (lse[10:] == 7).all())
+    b.new = [3, 4]   # max_q of 4 for five tokens: the last row stays
+    out.fill_(7)
+    b.call(fa, out=out, shared=256)
+    assert torch.equal(out[2:9], want[2:9]) and bool((out[9] == 7).all())
+
+
+def test_graph_replays(fa):
+    """Two captured calls, each with a workspace of its own, replayed with the program's work between."""
+    b = _share(Batch([3000, 2400, 2500, 2900], [1] * 4, 2, 4, 128, False, 64, seed=8), 2300)
+    cache = fa.KVCache(*(torch.from_numpy(t).cuda() for t in b.cache))
+    table, lengths = torch.from_numpy(b.table).cuda(), torch.tensor(b.keys, dtype=torch.int32, device="cuda")
+    q, slopes = b.q.cuda(), torch.tensor(_slopes(8), device="cuda")
+    calls = [dict(shared=2300), dict(shared=2300, softcap=4.0, slopes=slopes), dict(window=1500, softcap=4.0)]
+    want = [fa.cache_attention(q, cache, table, lengths, **o) for o in calls]
+    other = [fa.cache_attention(-q, cache, table, lengths - 50, **o) for o in calls]
+    side, graphs, outs = torch.cuda.Stream(), [], []
+    side.wait_stream(torch.cuda.current_stream())
+    for o in calls:
+        graph, out = torch.cuda.CUDAGraph(), torch.empty_like(want[0])
+        with torch.cuda.graph(graph, stream=side):
+            fa.cache_attention(q, cache, table, lengths, out=out, **o)
+        graphs.append(graph), outs.append(out)
+    for i in range(6):
+        sign = -1 if i % 2 else 1
+        q.copy_(b.q.cuda() * sign)
+        lengths.copy_(torch.tensor(b.keys, dtype=torch.int32) - (50 if i % 2 else 0))
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for out, x, y in zip(outs, want, other):
+            assert torch.equal(out, y if i % 2 else x), i
+        fa.cache_attention(q, cache, table, lengths, shared=2300).sum().item()
+
+
+def test_refusals_and_the_python_path(fa, monkeypatch):
+    b = _share(Batch([300, 290], [2, 2], 2, 2, 64, False, 16, seed=1), 256)
+    tree = np.full(4, 3, dtype=np.int64)
+    slopes, prefix = torch.tensor(_slopes(4), device="cuda"), torch.tensor([5, 6], dtype=torch.int32, device="cuda")
+    for o, error in ((dict(softcap=0.0), ValueError), (dict(softcap=-1.0), ValueError), (dict(softcap=float("nan")), ValueError),
+                     (dict(softcap=float("inf")), fa.Fp4AttnError), (dict(window=0), ValueError), (dict(window=-3), ValueError),
+                     (dict(window=2.0), ValueError), (dict(window=(1 << 30) + 1), fa.Fp4AttnError), (dict(window=1 << 70), fa.Fp4AttnError),
+                     (dict(slopes=slopes[:3]), ValueError), (dict(slopes=slopes.double()), TypeError), (dict(slopes=slopes.cpu()), ValueError),
+                     (dict(slopes=slopes.clone().requires_grad_()), ValueError), (dict(prefix=prefix[:1]), ValueError),
+                     (dict(prefix=prefix.long()), TypeError), (dict(shared=-1), fa.Fp4AttnError), (dict(shared=1 << 40), fa.Fp4AttnError),
+                     (dict(shared=1.0), TypeError), (dict(shared=b.table.shape[1] * 16 + 1), fa.Fp4AttnError),
+                     (dict(tree=tree, window=5), fa.Fp4AttnError), (dict(tree=tree, slopes=slopes), fa.Fp4AttnError),
+                     (dict(tree=tree, prefix=prefix), fa.Fp4AttnError)):
+        with pytest.raises(error):
+            b.call(fa, **o)
+    with torch.no_grad():
+        b.call(fa, slopes=slopes.clone().requires_grad_())
+    calls = (dict(softcap=3.0), dict(slopes=slopes), dict(window=77), dict(prefix=prefix), dict(shared=256), dict(shared=3),
+             dict(softcap=3, shared=256, slopes=slopes), dict(tree=tree, softcap=2.0, shared=200))
+    native = [b.call(fa, **o) for o in calls]
+    from paper_2609_04105_amd import api
+    monkeypatch.setattr(api, "_binding", api._NoBinding)
+    for o, want in zip(calls, native):
+        assert torch.equal(b.call(fa, **o), want)

@@ -1,0 +1,140 @@
+"""CPU checks of attention over the cache with options: refusals before any HIP call, the workspace, the launch plan of
+the shared prefix (csrc/cache_plan.hpp, compiled into a host program), and the oracle's masks and scores by hand."""
+import ctypes
+import math
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving
+from test_serving import PTR, _cache
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+needs_compiler = pytest.mark.skipif(shutil.which("g++") is None, reason="g++ is not installed")
+
+
+@pytest.fixture(scope="module")
+def fa():
+    import paper_2609_04105_amd as fa
+    return fa
+
+
+def _options(fa, **o):
+    opts = fa._lib.AttentionOptions()
+    fa.lib.fp4attn_cache_attention_options_init(ctypes.byref(opts))
+    assert (opts.struct_size, opts.softcap, opts.slopes, opts.window, opts.prefix, opts.shared) == (40, 0, None, 0, None, 0)
+    for k, v in o.items():
+        setattr(opts, k, v)
+    return ctypes.byref(opts)
+
+
+def test_refusals(fa):
+    f, size = fa.lib.fp4attn_cache_attention_ex, fa.lib.fp4attn_cache_attention_ex_workspace
+    c = ctypes.byref(_cache(fa))
+    good = dict(c=c, q=PTR[0], n=2, hq=4, qs=256, B=2, table=PTR[1], pages=3, lengths=PTR[2], starts=None, max_q=1, tree=None,
+                words=0, scale=0.1, opts=None, out=None, dtype=0, lse=None, work=None, bytes=0, s=None)
+
+    def status(o, **more):
+        return f(*dict(good, opts=_options(fa, **o), **more).values())
+    for o in (dict(struct_size=12), dict(struct_size=0), dict(softcap=-1.0), dict(softcap=math.nan), dict(softcap=math.inf),
+              dict(softcap=2.0 ** -65), dict(softcap=2.0 ** 65), dict(window=-1), dict(shared=-1), dict(shared=3 * 16 + 1),
+              dict(slopes=4098), dict(prefix=4097)):
+        assert status(o) == 1 and fa.lib.fp4attn_last_error(), o
+        assert size(c, 2, 4, 2, 3, 1, _options(fa, **o)) == -1, o
+    assert status(dict(window=(1 << 30) + 1)) == 2
+    for o in (dict(window=5), dict(slopes=4096), dict(prefix=4096)):
+        assert status(o, tree=PTR[4], words=1) == 2, o
+    # accepted options come as far as the missing output
+    for o in ({}, dict(softcap=2.0 ** -64), dict(softcap=2.0 ** 64), dict(window=1 << 30), dict(shared=48), dict(slopes=4096, prefix=4100)):
+        assert status(o) == 1 and b"out" in fa.lib.fp4attn_last_error(), o
+    assert f(*dict(good, n=0, opts=_options(fa, softcap=1.0)).values()) == 0
+
+
+def test_workspace(fa):
+    c = ctypes.byref(_cache(fa, heads=8, head_dim=128, page_size=64))
+    ex, plain = fa.lib.fp4attn_cache_attention_ex_workspace, fa.lib.fp4attn_cache_attention_workspace
+    for B in (1, 7, 64):
+        for hq in (8, 32):
+            for max_q in (1, 3):
+                for pages in (1, 16, 2048):
+                    n = B * max_q
+                    base = plain(c, hq, B, pages, max_q)
+                    assert base == ex(c, n, hq, B, pages, max_q, None) == ex(c, n, hq, B, pages, max_q, _options(fa, softcap=3.0))
+                    shared = ex(c, n, hq, B, pages, max_q, _options(fa, shared=64 * pages))
+                    # an accumulator and its state for every row of q and each piece of the prefix
+                    assert shared >= (n * hq * (128 * 4 + 16) if B > 1 and pages > 1 else 0)
+    # a window is a short table
+    assert ex(c, 64, 32, 64, 2048, 1, _options(fa, window=200)) < plain(c, 32, 64, 2048, 1)
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    exe = tmp_path_factory.mktemp("plan") / "shaped_plan"
+    res = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror", os.path.join(ROOT, "tests", "shaped_plan.cpp"),
+                          "-o", str(exe)], capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+
+    def ask(lines):
+        run = subprocess.run([str(exe)], input="\n".join(lines), capture_output=True, text=True, timeout=60)
+        assert run.returncode == 0
+        return [tuple(map(int, line.split())) for line in run.stdout.splitlines()]
+    return ask
+
+
+@needs_compiler
+def test_prefix_plan_covers_rows_and_keys(plans):
+    calls = [(H, G, d, n, units * 128) for H in (1, 2, 3, 8, 64, 1000, 65535) for G in (1, 4, 7, 64) for d in (64, 128)
+             for n in (1, 2, 5, 16, 64, 300, 4096, 20000) for units in (1, 2, 3, 63, 64, 65, 513, 8192)]
+    for c, (tile, row_tiles, pieces, units, ranges, workgroups, rows, fits) in zip(calls, plans(["P %d %d %d %d %d" % c for c in calls])):
+        H, G, d, n, keys = c
+        assert tile in (16, 32, 128) and (row_tiles - 1) * tile < n * G <= row_tiles * tile, c
+        assert 1 <= pieces and (pieces - 1) * units < keys // 128 <= pieces * units, c
+        assert rows == n * G * H, c
+        if fits:
+            assert ranges == row_tiles * pieces and workgroups % 8 == 0 and ranges * H <= workgroups <= 1 << 24, c
+
+
+@needs_compiler
+def test_window_units_cover_every_tile(plans):
+    """The units that a row tile's keys touch, from first window's begin to last token's own key, wherever they lie."""
+    cases = [(tile, G, window) for tile in (16, 32, 128) for G in (1, 2, 3, 7, 16, 33, 200) for window in (1, 2, 64, 127, 128, 129, 500)]
+    got = [u for u, in plans(["W %d %d %d" % c for c in cases])]
+    for (tile, G, window), units in zip(cases, got):
+        most = 0
+        for row0 in range(0, 40 * tile, tile):
+            first, last = row0 // G, (row0 + tile - 1) // G
+            span = window + last - first   # keys from first + 1 - window to last
+            most = max(most, (span + 126) // 128 + 1)
+        assert units >= most, (tile, G, window)
+
+
+def test_oracle_masks_and_scores():
+    see = serving.shaped_mask(3, 6, 6, window=2)
+    assert see.tolist() == [[j in (p - 1, p) for j in range(6)] for p in (3, 4, 5)]
+    see = serving.shaped_mask(3, 6, 6, prefix=5)
+    assert see.sum(1).tolist() == [5, 5, 6] and serving.shaped_mask(3, 6, 6, 3, 5).sum(1).tolist() == [4, 3, 3]   # 1-4, 2-4, 3-5
+    rng = np.random.default_rng(1)
+    q, k, v = rng.standard_normal((3, 4, 8)), rng.standard_normal((6, 2, 8)), rng.standard_normal((6, 2, 8))
+    slopes = [0.5, -0.25, 0.0, 1.0]
+    see = serving.causal_mask(3, 6, 6)
+    out, lse, *_ = serving.shaped_attention(q, k, v, see, 0.5, 2.0, slopes, 6)
+    for t in range(3):
+        for h in range(4):
+            z = np.array([2 * math.tanh(0.25 * float(k[j, h // 2] @ q[t, h])) - slopes[h] * abs(3 + t - j) for j in range(4 + t)])
+            w = np.exp(z)
+            assert np.allclose(out[t, h], w @ v[:4 + t, h // 2] / w.sum()) and np.isclose(lse[t, h], np.log(w.sum()))
+    plain = serving.attention(q, k, v, see, 0.5)
+    for x, y in zip(plain, serving.shaped_attention(q, k, v, see, 0.5)):
+        assert np.allclose(x, y)
+
+
+def test_python_refusals_without_a_gpu(fa):
+    x, at = torch.zeros(2, 4, 64).bfloat16(), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="must be a GPU tensor"):
+        fa.cache_attention(x, fa.kv_cache(2, 4, 16, 64, device="cpu"), at.view(2, 1), at, softcap=3.0)
+    with pytest.raises(ValueError, match="no gradient"):
+        fa.cache_attention(x, None, at, at, slopes=torch.ones(4, requires_grad=True))
