@@ -758,7 +758,7 @@ fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void
   a.workspace = workspace;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (!p.shaped) return from_hip(fp4attn::launch_cache_attention(a, p.plan, s), "cache attention launch");
-  a.softcap = opts->softcap;
+  a.cap = fp4attn::cap_shape((double)softmax_scale * (a.c.fp8 ? 1.0 : 1.0 / 6.0), opts->softcap);
   a.slopes = opts->slopes;
   a.window = (int)opts->window;
   a.open_keys = opts->prefix;

@@ -71,7 +71,7 @@ __device__ __forceinline__ v4i probabilities(const v4f (&s)[2], float factor, fl
 template <class Args>
 __device__ __forceinline__ void fetch_arguments(const Args& a, const CachePlan& plan) {
   asm volatile("" ::"s"(a.c.H), "s"(a.B), "s"(a.tree), "s"(plan.ranges));
-  if constexpr (Args::kShaped) asm volatile("" ::"s"(a.softcap), "s"(a.prefix_acc));
+  if constexpr (Args::kShaped) asm volatile("" ::"s"(a.cap.on), "s"(a.prefix_acc));
 }
 
 // Of numbers that are not negative (half the instructions of a signed division).
@@ -669,23 +669,21 @@ __device__ __forceinline__ unsigned may_see(const Args& a, const Part& part, int
   return see;
 }
 
-// How a product of codes q . k becomes the exponent of a probability, in binades.  Plain: times `factor`.  Shaped,
-// y = C tanh(z / c) - slope |distance| with z = softmax_scale q . k and C = c log2(e), which the scores
-// are replaced by; their factor is then 1.
+// How a product of codes s = q . k becomes the exponent of a probability, in binades.  Plain: times `factor`.  Shaped, scores
+// are replaced by y = C tanh(x) - slope |distance| with x = z / c, z = softmax_scale q . k, C = c log2(e) (capped), or by z log2(e)
+// less the bias; their factor is then 1.
 struct ScoreShape {
   float factor;
-  float inside, cap;  // z / c of a product; C (0: no cap)
+  float inside;  // of s: x, or z log2(e) without a cap
   bool on;
 };
 template <bool FP8, class Args>
 __device__ __forceinline__ ScoreShape score_shape(const Args& a) {
   ScoreShape s{};
-  const float z = a.softmax_scale * (FP8 ? 1.0f : 1.0f / 6.0f);
   s.factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
   if constexpr (Args::kShaped) {
-    s.on = a.softcap > 0.0f || a.slopes;
-    s.inside = a.softcap > 0.0f ? z / a.softcap : s.factor;
-    s.cap = a.softcap * kLog2e;
+    s.on = a.cap.on || a.slopes;
+    s.inside = a.cap.on ? a.cap.inside : s.factor;
     if (s.on) s.factor = 1.0f;
   }
   return s;
@@ -704,27 +702,51 @@ __device__ __forceinline__ RowBias row_bias(const Args& a, const Sequence& seq, 
   }
   return r;
 }
-// tanh(x) / x = P(x^2) for |x| <= 0.8, a least-squares fit weighted until its largest relative errors were equal: 5.8e-8, a half
-// step of fp32; beyond, 1 - 2 / (e^2x + 1), where nothing cancels.
-constexpr float kTanhNear = 0.8f;
-__device__ __forceinline__ float tanh_near(float x) {
-  const float u = x * x;
-  return x * fmaf(fmaf(fmaf(fmaf(fmaf(-0.00435529975f, u, 0.0190933011f), u, -0.0531143174f), u, 0.13321048f), u, -0.333326757f), u, 0.99999994f);
-}
-__device__ __forceinline__ float tanh_far(float x) {
-  return fmaf(-2.0f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (2.0f * kLog2e)) + 1.0f), 1.0f);
-}
-// A lane's eight scores, of keys key .. key + 7.
-template <class Args>
-__device__ __forceinline__ void shape_scores(const Args& a, const ScoreShape& shape, const RowBias& bias, int key, v4f (&s)[2]) {
-  const float far = (float)(bias.at - key);
+// A lane's scores of keys key .. key + 7, of N rows.  Where every |s| of the wave is at most cap.near, C tanh(x) is s K(s^2): 6
+// instructions a score.  Else x is formed, and beyond 0.6 C tanh(x) = C (1 - 2 / (e^2x + 1)), in which nothing cancels.
+template <class Args, int N>
+__device__ __forceinline__ void shape_scores(const Args& a, const ScoreShape& shape, const RowBias (&bias)[N], int key, v4f (&s)[N][2]) {
+  if (a.cap.on) {
+    float most = 0.0f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float x = s[j / 4][j % 4] * shape.inside;
-    if (shape.cap > 0.0f) x = shape.cap * (fabsf(x) <= kTanhNear ? tanh_near(x) : tanh_far(x));
-    if (a.slopes) x = fmaf(-bias.slope, fabsf(far - (float)j), x);
-    s[j / 4][j % 4] = x;
+    for (int r = 0; r < N; ++r)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(s[r][j / 4][j % 4]));
+    if (!__any(most > a.cap.near)) {
+#pragma unroll
+      for (int r = 0; r < N; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = s[r][j / 4][j % 4], u = x * x;
+          s[r][j / 4][j % 4] = x * fmaf(fmaf(fmaf(fmaf(a.cap.k[4], u, a.cap.k[3]), u, a.cap.k[2]), u, a.cap.k[1]), u, a.cap.k[0]);
+        }
+    } else {
+      constexpr float k0 = kTanh[0], k1 = kTanh[1], k2 = kTanh[2], k3 = kTanh[3], k4 = kTanh[4];
+#pragma unroll
+      for (int r = 0; r < N; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = s[r][j / 4][j % 4] * shape.inside, u = x * x;
+          const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
+          float lo = x * a.cap.most * fmaf(fmaf(fmaf(fmaf(k4, u, k3), u, k2), u, k1), u, k0);
+          float hi = fmaf(-2.0f * a.cap.most, __builtin_amdgcn_rcpf(e + 1.0f), a.cap.most);
+          asm("" : "+v"(lo), "+v"(hi));  // both, and a choice: the compiler made a branch for every score of it
+          s[r][j / 4][j % 4] = fabsf(x) <= (float)kTanhNear ? lo : hi;
+        }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < N; ++r)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] *= shape.inside;
   }
+  if (a.slopes)
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const float far = (float)(bias[r].at - key);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = fmaf(-bias[r].slope, fabsf(far - (float)j), s[r][j / 4][j % 4]);
+    }
 }
 
 }  // namespace fp4attn

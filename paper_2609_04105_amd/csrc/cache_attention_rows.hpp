@@ -279,9 +279,18 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       if constexpr (Args::kShaped)
         if (shape.on)
 #pragma unroll
-          for (int tile = 0; tile < kTiles; ++tile)
+          for (int tile = 0; tile < kTiles; ++tile) {
+            v4f x[kNr][2];
 #pragma unroll
-            for (int r = 0; r < kNr; ++r) shape_scores(a, shape, bias[r], key0 + kTile * tile + 8 * g, s[r][tile]);
+            for (int r = 0; r < kNr; ++r)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) x[r][h] = s[r][tile][h];
+            shape_scores(a, shape, bias, key0 + kTile * tile + 8 * g, x);
+#pragma unroll
+            for (int r = 0; r < kNr; ++r)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) s[r][tile][h] = x[r][h];
+          }
       bool all = !some_hidden(a, part, key0, kKeys);
 #pragma unroll
       for (int tile = 0; tile < kTiles; ++tile) all = all && is_page(a.c, pages[tile].p0) && is_page(a.c, pages[tile].p1);

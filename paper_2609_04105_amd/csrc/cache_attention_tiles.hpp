@@ -220,9 +220,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
         }
         t.load_k(a.c, next, ahead, head, lane);
         if constexpr (Args::kShaped)
-          if (shape.on)
-#pragma unroll
-            for (int r = 0; r < NR; ++r) shape_scores(a, shape, bias[r], key0 + 8 * g, s[r]);
+          if (shape.on) shape_scores(a, shape, bias, key0 + 8 * g, s);
         if (masked) {
           // Hidden scores become -inf.  Keys that no row sees hold anything: their V codes and
           // scales become zero.  A non-finite V block that some row may see becomes zero too, and a NaN
