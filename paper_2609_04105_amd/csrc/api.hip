@@ -285,7 +285,7 @@ struct AttentionPlan {
   fp4attn::PrefixPlan prefix;
   bool shaped;  // some option is set
   int shared;   // keys of the prefix that has a pass of its own; 0: none
-  int64_t join_bytes, workspace;
+  int64_t workspace;
 };
 fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int64_t q_heads, int64_t B, int64_t max_pages,
                                     int64_t max_q, const fp4attn_cache_attention_options* opts, AttentionPlan* p) {
@@ -334,10 +334,7 @@ fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int6
     return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_q=%lld max_pages=%lld: too many workgroups for one launch", (long long)B,
                 (long long)max_q, (long long)max_pages);
   p->workspace = p->plan.workspace;
-  if (p->shared > 0) {
-    p->join_bytes = (p->plan.split ? (int64_t)p->plan.ranges * sizeof(int2) + 15 : 0) / 16 * 16;
-    p->workspace += p->join_bytes + p->prefix.pieces * p->prefix.rows * (16 + c.d * 4);
-  }
+  if (p->shared > 0) p->workspace += p->prefix.pieces * p->prefix.rows * (16 + c.d * 4);
   return FP4ATTN_OK;
 }
 
@@ -767,8 +764,6 @@ fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void
     a.shared = p.shared;
     a.prefix_pieces = p.prefix.pieces;
     a.prefix_units = p.prefix.units;
-    a.join_prefix = reinterpret_cast<int2*>(w);
-    w += p.join_bytes;
     a.prefix_stat = reinterpret_cast<float4*>(w);
     w += p.prefix.pieces * p.prefix.rows * 16;
     a.prefix_acc = reinterpret_cast<float*>(w);

@@ -409,21 +409,35 @@ struct OddMarks {
   }
 };
 
-// The pieces of the shared prefix that a row joins: their number, and what the bias by distance takes off their
-// references, which its pass counts from the prefix's end.
-struct PrefixPieces {
-  int count;
-  float lower;
-};
-template <class Args>
-__device__ __forceinline__ PrefixPieces prefix_pieces(const Args& a, int keys, int prefix, int token, int head) {
-  PrefixPieces p{0, 0.0f};
-  if constexpr (Args::kShaped && !Args::kPrefix)
-    if (keys) {
-      p.count = a.prefix_pieces;
-      if (a.slopes) p.lower = a.slopes[head] * kLog2e * (float)(prefix + token - keys);
+// Adds piece k of the shared prefix to what a lane holds of a row (of q and head h): columns D / 16 * (4 g + i) + t in
+// register i of product t.  lower: what the bias by distance takes off the piece's reference, which its pass counts
+// from the prefix's end.
+template <int D, class Args>
+__device__ __forceinline__ void add_piece(const Args& a, int k, int64_t row, int g, float lower, float* ref, float* sum, v4f* sum16,
+                                          v4f (&acc)[D / 16]) {
+  constexpr int kCols = D / 16;
+  const int64_t at = k * (a.n * a.Hq) + row;
+  const float4 s = a.prefix_stat[at];
+  float4 x[4][kCols / 4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < kCols / 4; ++j) x[i][j] = reinterpret_cast<const float4*>(a.prefix_acc + at * D + (4 * g + i) * kCols)[j];
+  const float its_ref = s.x - lower, top = fmaxf(*ref, its_ref);
+  const float mine = *ref == top ? 1.0f : __builtin_amdgcn_exp2f(*ref - top);
+  const float its = its_ref == top ? 1.0f : __builtin_amdgcn_exp2f(its_ref - top);
+  *ref = top;
+  *sum = *sum * mine + (g == 0 ? s.y * its : 0.0f);  // (the lane groups' sums are added up later)
+  *sum16 = *sum16 * mine + s.z * its;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < kCols / 4; ++j) {
+      acc[4 * j][i] = acc[4 * j][i] * mine + x[i][j].x * its;
+      acc[4 * j + 1][i] = acc[4 * j + 1][i] * mine + x[i][j].y * its;
+      acc[4 * j + 2][i] = acc[4 * j + 2][i] * mine + x[i][j].z * its;
+      acc[4 * j + 3][i] = acc[4 * j + 3][i] * mine + x[i][j].w * its;
     }
-  return p;
 }
 
 // Joins and stores: D / 16 columns from D / 16 * c of row i of the sequence, as output if the
@@ -433,41 +447,12 @@ __device__ __forceinline__ PrefixPieces prefix_pieces(const Args& a, int keys, i
 template <int D, bool FP8, class Args>
 __device__ __forceinline__ void store_columns(const Args& a, const CachePlan& plan, const Sequence& seq, int i, int head, int c,
                                               bool whole, int64_t piece, float ref, float sum, float rounded, unsigned odd,
-                                              float (&o)[D / 16]) {
+                                              const float (&o)[D / 16]) {
   constexpr int kCols = D / 16;
   if constexpr (Args::kPrefix) {  // a piece of row (token, head) of the batch
     const int t = divide(i, a.G);
     piece += (int64_t)(seq.first + t) * a.Hq + head * a.G + (i - t * a.G);
   }
-  if constexpr (Args::kShaped && !Args::kPrefix)
-    if (whole) {
-      const int t = divide(i, a.G), h = head * a.G + (i - t * a.G);
-      const int64_t at = (int64_t)(seq.first + t) * a.Hq + h, rows = a.n * a.Hq;
-      const PrefixPieces pre = prefix_pieces(a, shared_keys(a, seq), seq.prefix, t, h);
-      float top = ref;
-      for (int k = 0; k < pre.count; ++k) top = fmaxf(top, a.prefix_stat[k * rows + at].x - pre.lower);
-      const float mine = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
-      ref = top;
-      sum *= mine;
-      rounded *= mine;
-#pragma unroll
-      for (int j = 0; j < kCols; ++j) o[j] *= mine;
-      for (int k = 0; k < pre.count; ++k) {
-        const float4 s = a.prefix_stat[k * rows + at];
-        const float its_ref = s.x - pre.lower, its = its_ref == top ? 1.0f : __builtin_amdgcn_exp2f(its_ref - top);
-        sum += s.y * its;
-        rounded += s.z * its;
-        const float4* acc = reinterpret_cast<const float4*>(a.prefix_acc + (k * rows + at) * D + c * kCols);
-#pragma unroll
-        for (int j = 0; j < kCols / 4; ++j) {
-          const float4 x = acc[j];
-          o[4 * j] += x.x * its;
-          o[4 * j + 1] += x.y * its;
-          o[4 * j + 2] += x.z * its;
-          o[4 * j + 3] += x.w * its;
-        }
-      }
-    }
   const bool empty = is_zero(rounded);
   const float norm = whole ? (empty ? 0.0f : (FP8 ? 1.0f : 1.0f / 6.0f) / rounded) : 1.0f;
   float x[kCols];
@@ -554,8 +539,6 @@ __device__ __forceinline__ Range open_range(const Args& a, const CachePlan& plan
       if (range.begin < range.end && range.begin > range.at && range.at >= range.begin - range.per)
         join = int4{divide(range.at + range.units - 1, range.per) - p.w + 2, range.seq.first, range.seq.tokens * a.G, range.tile};
       partials(a, plan).joins[p.w] = join;
-      if constexpr (Args::kShaped)
-        if (a.shared) a.join_prefix[p.w] = int2{shared_keys(a, range.seq), range.seq.prefix};
     }
   } else {  // range w: row tile w % row_tiles of sequence w / row_tiles
     range.b = divide(p.w, plan.row_tiles);
@@ -688,17 +671,19 @@ __device__ __forceinline__ ScoreShape score_shape(const Args& a) {
   }
   return s;
 }
-// A row's slope in binades, and the token's place that its distances count from.
+// A row's slope in binades, the token's place that its distances count from, and its number among the rows of q.
 struct RowBias {
   float slope;
   int at;
+  int row;
 };
 template <class Args>
 __device__ __forceinline__ RowBias row_bias(const Args& a, const Sequence& seq, int token, int head) {
-  RowBias r{0.0f, 0};
+  RowBias r{0.0f, 0, 0};
   if constexpr (Args::kShaped) {
     if (a.slopes) r.slope = a.slopes[head] * kLog2e;
     r.at = Args::kPrefix ? seq.keys : seq.prefix + token;
+    r.row = (seq.first + token) * a.Hq + head;  // below 2^31
   }
   return r;
 }

@@ -183,6 +183,13 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
       ref[r] = -__builtin_inff();
       sum[r] = 0.0f;
     }
+    if constexpr (Args::kShaped && !Args::kPrefix)
+      if (part.first && shared_keys(a, seq) && row0 < rows) {  // a row begins with the pieces of the shared prefix
+#pragma unroll
+        for (int r = 0; r < kNr; ++r)
+          for (int k = 0; k < a.prefix_pieces; ++k)
+            add_piece<D>(a, k, bias[r].row, g, bias[r].slope * (float)(bias[r].at - a.shared), &ref[r], &sum[r], &sum16[r], acc[r]);
+      }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
     auto pages_of = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
     // the wave's tile of every step and its halves there

@@ -184,6 +184,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
       sum[r] = 0.0f;
     }
 
+    if constexpr (Args::kShaped && !Args::kPrefix)
+      if (part.first && shared_keys(a, seq)) {  // the waves begin with the pieces of the shared prefix
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+          for (int k = wave; k < a.prefix_pieces; k += kWaves)
+            add_piece<D>(a, k, bias[r].row, g, bias[r].slope * (float)(bias[r].at - a.shared), &ref[r], &sum[r], &sum16[r], acc[r]);
+      }
+
     // The wave's tiles.  One set of registers: a tile's K is loaded when the one before has
     // become scores, its V when the one before is in the accumulators.
     if (key0 < part.end) {
@@ -351,31 +359,20 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 // has its own row and walks the pieces.
 // grid: (rows of a row tile and all key heads / rows of a workgroup, ranges - 1)
 constexpr int kJoinThreads = 256;
-template <int D, bool FP8, bool SPREAD, class Args>
-__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const Args a, const CachePlan plan) {
+template <int D, bool FP8, bool SPREAD>
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAttentionArgs a, const CachePlan plan) {
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
   fetch_arguments(a, plan);
   const Partials part = partials(a, plan);
   const int w = blockIdx.y + 1;
   const int4 job = part.joins[w];
-  const int own = job.x, first = job.y, rows = job.z;
-  if (own == 0) return;
+  const int pieces = job.x, first = job.y, rows = job.z;
+  if (pieces == 0) return;
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const int row = SPREAD ? (int)blockIdx.x : (int)blockIdx.x * kGroups + group;
   const int head = divide(row, plan.tile_rows), in_tile = row - head * plan.tile_rows;
   const int i = job.w * plan.tile + in_tile;
   const bool there = head < a.c.H && i < rows;
-  const int t = divide(i, a.G), h = head * a.G + (i - t * a.G);
-  const int64_t to_row = (int64_t)(first + t) * a.Hq + h;
-  // behind the row tile's own pieces those of the shared prefix
-  int pieces = own;
-  PrefixPieces pre{0, 0.0f};
-  if constexpr (Args::kShaped)
-    if (a.shared && there) {
-      const int2 of = a.join_prefix[w];
-      pre = prefix_pieces(a, of.x, of.y, t, h);
-      pieces += pre.count;
-    }
   float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
   float4 acc = {0, 0, 0, 0};
   auto join = [&](const float4& s, const float4& o) {
@@ -390,14 +387,6 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const Args a, 
   if (there) {
 #pragma unroll 4
     for (int k = SPREAD ? group : 0; k < pieces; k += SPREAD ? kGroups : 1) {
-      if constexpr (Args::kShaped)
-        if (k >= own) {
-          const int64_t at = (k - own) * a.n * a.Hq + to_row;
-          float4 s = a.prefix_stat[at];
-          s.x -= pre.lower;
-          join(s, reinterpret_cast<const float4*>(a.prefix_acc + at * D)[lane]);
-          continue;
-        }
       const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? 1 : 0, head) + in_tile;
       join(part.stat[at], reinterpret_cast<const float4*>(part.acc + at * D)[lane]);
     }
@@ -413,14 +402,16 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const Args a, 
     for (int k = 1; k < used; ++k) join(stat_lds[k], acc_lds[k][lane]);
   }
   if (!there) return;
+  const int t = divide(i, a.G);
+  const int64_t at = (int64_t)(first + t) * a.Hq + head * a.G + (i - t * a.G);
   const bool empty = is_zero(sum16);
   const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / sum16;
   const float o[4] = {empty ? 0.0f : acc.x * norm, empty ? 0.0f : acc.y * norm, empty ? 0.0f : acc.z * norm,
                       empty ? 0.0f : acc.w * norm};
-  const int64_t to = to_row * D + lane * 4;
+  const int64_t to = at * D + lane * 4;
   if (a.out_bf16) store_row<4>(static_cast<uint16_t*>(a.out) + to, o);
   else store_row<4>(static_cast<float*>(a.out) + to, o);
-  if (a.lse && lane == 0) a.lse[to_row] = log_norm(ref, sum);
+  if (a.lse && lane == 0) a.lse[at] = log_norm(ref, sum);
 }
 
 template <int D, bool FP8, class Args>
@@ -430,8 +421,8 @@ void launch_tiles(const Args& a, const CachePlan& plan, hipStream_t stream) {
   else cache_attention_kernel<D, FP8, 2><<<grid, kThreads, 0, stream>>>(a, plan);
 }
 
-template <int D, bool FP8, class Args>
-void launch_join(const Args& a, const CachePlan& plan, hipStream_t stream) {
+template <int D, bool FP8>
+void launch_join(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream) {
   const unsigned rows = (unsigned)(plan.tile_rows * a.c.H), per = kJoinThreads / (D / 4);
   // many pieces a row tile: a workgroup for each row
   if (plan.ranges >= 16 * a.B * plan.row_tiles)

@@ -135,7 +135,6 @@ struct ShapedAttentionArgs : CacheAttentionArgs {
   int shared, prefix_pieces, prefix_units;
   float4* prefix_stat;  // [pieces][n * Hq]
   float* prefix_acc;    // [pieces][n * Hq][d]
-  int2* join_prefix;    // [ranges] of the sequence in joins: its shared keys, keys before its new tokens
 };
 // The pass over the shared prefix itself.
 struct PrefixAttentionArgs : ShapedAttentionArgs {
