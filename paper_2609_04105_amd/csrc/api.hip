@@ -315,10 +315,10 @@ fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int6
     // few rows see the prefix: it gets no pass of its own
     const int64_t units = fp4attn::window_units(fp4attn::kRowsTile, (int)G, (int)opts->window);
     if (opts->prefix == nullptr && units * fp4attn::kUnit < span) span = units * fp4attn::kUnit;
-  } else if (n > 0 && n <= 0x7fffffff / q_heads && fp4attn::shares_prefix(B, G, max_q, opts->shared)) {
+  } else if (n > 0 && n <= 0x7fffffff / q_heads && B > 1 && opts->shared >= fp4attn::kUnit) {
     const int64_t keys = opts->shared / fp4attn::kUnit * fp4attn::kUnit;
     const fp4attn::PrefixPlan prefix = fp4attn::prefix_plan(c.H, G, c.d, n, keys);
-    if (prefix.fits) {
+    if (fp4attn::shares_prefix(p->plan, prefix, B, c.H, G, c.d, n, keys)) {
       p->shared = (int)keys;
       p->prefix = prefix;
       span -= keys;

@@ -85,6 +85,16 @@ inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8
   return p;
 }
 
+// Microseconds of walking `keys` keys for `tiles` row tiles, all key heads counted, in a chip that they fill, with the
+// launch and its start: from the times of 400 batches of 2 to 200 sequences, 1 to 16 tokens, 1 to 8 query heads a key head,
+// behind 1024 to 65536 keys (8 heads of d = 128 in MXFP4, 2 of d = 64 in MXFP8), by least squares; the worst are off by a quarter.
+inline double walk_time(int tile, int64_t d, int64_t tiles, int64_t keys, bool prefix) {
+  const double walks = (double)tiles * (double)keys * 1e-6;
+  if (tile == 16) return prefix ? 14 + 30 * walks : 12 + 15 * walks;  // (a pass over a prefix has one tile a key head)
+  if (tile == 32) return (prefix ? 18.5 : 16) + (prefix ? (d == 64 ? 20 : 25) : 22) * walks;
+  return 28 + (prefix ? 75 : 67) * walks;
+}
+
 // The pass over a prefix of `keys` keys (whole units) that the sequences share: all n tokens' rows of a key head together in
 // row tiles, each with `pieces` parts of the prefix of `units` units, one to a workgroup.
 struct PrefixPlan {
@@ -93,17 +103,26 @@ struct PrefixPlan {
   bool fits;
   int64_t rows;  // n * H * G: of each piece
 };
+// Row tiles: 16 where they hold all rows, else 32 or 128, whichever the times above say.  us at tile 32 / 128, 8 key heads, d =
+// 128, MXFP4: 192 rows, 4096 keys 23 / 32, 65536 keys 94 / 100; 768 rows, 4096 keys 40 / 44, 16384 keys 110 / 87, 65536 keys 384 / 265.
+// Pieces: as many workgroups as the chip holds at once, of four units at least: at least two or eight, 192 rows behind 4096 keys 23.4,
+// 23.3 against 23.3; 16 rows behind 16384 keys 21.9, 19.2 against 18.1; 64 rows behind 1024 keys 15.2, 20.9 against 16.9.
 inline PrefixPlan prefix_plan(int64_t H, int64_t G, int64_t d, int64_t n, int64_t keys) {
   PrefixPlan p{};
   const int64_t rows = n * G, units = keys / kUnit;
   CachePlan& c = p.plan;
-  c.tile = rows <= 16 ? 16 : (rows <= 64 ? 32 : kRowsTile);
-  const int64_t row_tiles = (rows + c.tile - 1) / c.tile;
+  auto tiles_of = [&](int64_t tile) { return (rows + tile - 1) / tile; };
+  c.tile = rows <= 16 ? 16 : 32;
+  if (rows > 16 && walk_time(kRowsTile, d, tiles_of(kRowsTile) * H, keys, true) < walk_time(32, d, tiles_of(32) * H, keys, true))
+    c.tile = kRowsTile;
+  const int64_t row_tiles = tiles_of(c.tile);
   c.row_tiles = (int)row_tiles;
   c.tile_rows = (int)(rows < c.tile ? rows : c.tile);
   const int64_t slots = 256 * (c.tile == kRowsTile ? kRowsPerCu : waves_per_simd((int)d, c.tile / 16));
+  constexpr int64_t kLeast = 4, kMost = 64;  // units of a piece, pieces
   int64_t pieces = slots / (row_tiles * H);
-  pieces = pieces < 1 ? 1 : (pieces > 16 ? 16 : pieces);
+  if (pieces > units / kLeast) pieces = units / kLeast;
+  pieces = pieces < 1 ? 1 : (pieces > kMost ? kMost : pieces);
   const int64_t per = (units + pieces - 1) / pieces;
   p.units = (int)per;
   p.pieces = (int)((units + per - 1) / per);
@@ -114,7 +133,16 @@ inline PrefixPlan prefix_plan(int64_t H, int64_t G, int64_t d, int64_t n, int64_
   return p;
 }
 
-// Whether the shared prefix gets a pass of its own.
-inline bool shares_prefix(int64_t B, int64_t G, int64_t max_q, int64_t keys) { return B > 1 && keys >= kUnit && max_q * G < kRowsTile; }
+// Whether n tokens of B sequences, which a call with `plan` serves one by one, gain by a pass over their shared prefix.  us without it /
+// with it, 8 key heads of 4 query heads, d = 128, MXFP4, one token each: 2 sequences behind 65536 keys 29 / 29; 4 31 / 29 of
+// 32768; 16 behind 1024 keys 12.9 / 16.9, 4096 keys 21.9 / 18.2; 48 behind 4096 keys 39 / 23, 65536 keys 363 / 94; 16 tokens each: 8
+// behind 65536 keys 190 / 177, 48 behind 16384 keys 281 / 314.  (Of the 400 batches the choice costs 1 % on average, 27 % at most.)
+inline bool shares_prefix(const CachePlan& plan, const PrefixPlan& prefix, int64_t B, int64_t H, int64_t G, int64_t d, int64_t n,
+                          int64_t keys) {
+  int64_t tiles = n * G / plan.tile + B;  // at most, of ragged sequences
+  if (tiles > B * plan.row_tiles) tiles = B * plan.row_tiles;
+  return prefix.fits && walk_time(prefix.plan.tile, d, prefix.plan.row_tiles * H, keys, true) <
+                            walk_time(plan.tile, d, tiles * H, keys, false);
+}
 
 }  // namespace fp4attn

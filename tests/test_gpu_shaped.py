@@ -11,6 +11,8 @@ magnitude `bias`:
   places that distances count from: 8 u (bias + high).
 Errors of the scores move the output by twice their sum times the weighted mean of |v|.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -27,30 +29,34 @@ def fa():
     return fa
 
 
-def _values(b, i):
-    """K and V [n, H, d] of a sequence, by the cache's documented layout (test_gpu_serving.py checks it key by key)."""
-    (p, off), (kc, ks, vc, vs) = divmod(b.slots[i], b.page), b.cache
+def _values(b, i, heads):
+    """K and V [n, heads, d] of a sequence, by the cache's documented layout (test_gpu_serving.py checks it key by key)."""
+    (p, off), heads = divmod(b.slots[i], b.page), np.array(list(heads))
     if len(p) == 0:
-        return np.zeros((2, 0, b.H, b.d))
-    v = vc[p, :, off // 8, :, off % 8].reshape(len(p), b.H, -1)
-    return serving.values(kc[p, :, off], ks[p, :, off], b.fp8), serving.values(v, vs[p, :, off // 8, :, off % 8], b.fp8)
+        return np.zeros((2, 0, len(heads), b.d))
+    p, off = p[:, None], off[:, None]
+    kc, ks, vc, vs = b.cache
+    v = vc[p, heads, off // 8, :, off % 8].reshape(len(p), len(heads), -1)
+    return serving.values(kc[p, heads, off], ks[p, heads, off], b.fp8), serving.values(v, vs[p, heads, off // 8, :, off % 8], b.fp8)
 
 
 def _check(b, out, lse=None, tree=None, softcap=None, slopes=None, window=None, prefix=None, only=None):
-    """out [n, Hq, d] and lse against the oracle."""
-    out_dtype, out = out.dtype, _f64(out)
+    """out [n, Hq, d] and lse against the oracle (of many key heads the first, a middle and the last one)."""
+    heads = sorted({0, b.H // 2, b.H - 1}) if b.H > 4 else range(b.H)
+    hq = [h * b.G + g for h in heads for g in range(b.G)]
+    out_dtype, out, lse = out.dtype, _f64(out[:, hq]), None if lse is None else lse[:, hq]
+    slopes = None if slopes is None else _f64(slopes)[hq]
     for i, (t, n) in enumerate(zip(b.new, b.keys)):
         if t == 0 or (only is not None and i not in only):
             continue
         rows = slice(b.starts[i], b.starts[i] + t)
-        k, v = _values(b, i)
+        k, v = _values(b, i, heads)
         if tree is not None:
             see = serving.tree_mask(tree[rows].reshape(t, -1).view(np.uint64), t, n, n)
         else:
             see = serving.shaped_mask(t, n, n, window or 0, 0 if prefix is None else int(prefix[i]))
         o, norm, spread, size, reach, high, bias = serving.shaped_attention(
-            _f64(b.q[rows]), np.nan_to_num(k), np.nan_to_num(v), see, b.scale, softcap or 0.0,
-            None if slopes is None else _f64(slopes), n)
+            _f64(b.q[rows])[:, hq], np.nan_to_num(k), np.nan_to_num(v), see, b.scale, softcap or 0.0, slopes, n)
         e = 2 * ((b.d + 4) * U * reach + 20 * U * high + 8 * U * (bias + high) + (n + 64) * 2 * U + 4 * U)
         tol = 2.0 ** -8 * (1 + 2.0 ** -7) * spread + e[..., None] * size
         tol += HALF_STEP[out_dtype] * (np.abs(o) + tol)
@@ -236,87 +242,139 @@ def _share(b, shared):
     return b
 
 
-SHARED = [([1] * 5, [300, 260, 257, 400, 290], 256), ([1] * 3, [700, 0, 650], 600), ([1] * 2, [2000, 1400], 1331),
-          ([3, 1, 5, 0, 2], [400, 300, 270, 500, 310], 265), ([1] * 4, [129, 130, 128, 200], 128), ([9, 7], [900, 800], 777),
-          ([1] * 70, [200 + i for i in range(70)], 190), ([2, 2, 2], [1500, 40, 1501], 1400), ([1] * 4, [260, 256, 257, 255], 256)]
+def _behind(fa, keys, new, G, d, fp8, page, shared, width=1, tile=None, seed=0):
+    """Such a batch with as few key heads as make the call pass over the prefix by itself (and in row tiles of 128 rows,
+    where `tile` says so: these need more)."""
+    need = -(-max(max(keys), width) // page) + 2
+    for H in (1, 2, 4, 8, 16, 32, 64, 128, 256, 512, 1024, 2048):
+        c = fa._lib.Cache(ctypes.sizeof(fa._lib.Cache), int(fp8), 4, H, page, d, 0, 0, 0, 0)
+        size = [fa.lib.fp4attn_cache_attention_ex_workspace(ctypes.byref(c), sum(new), H * G, len(new), need, max(new), ctypes.byref(
+            fa._lib.AttentionOptions(ctypes.sizeof(fa._lib.AttentionOptions), shared=s))) for s in (0, shared)]
+        # (the time of a pass over the prefix in row tiles of 128 rows falls below that in 32 rows)
+        whole = shared // 128 * 128
+        wide = 28 + 75e-6 * -(-sum(new) * G // 128) * H * whole < 18.5 + (20e-6 if d == 64 else 25e-6) * -(-sum(new) * G // 32) * H * whole
+        if size[1] > size[0] and (tile is None or wide):
+            b = Batch(keys, new, H, G, d, fp8, page, seed=seed)
+            return _beside_idle(_share(b, shared), 0, width)
+    raise AssertionError("no number of heads gains by the pass")
 
 
-@pytest.mark.parametrize("d,fp8", FORMATS)
-@pytest.mark.parametrize("G,page,width", [(1, 16, 1), (4, 64, 1), (8, 32, 6000), (3, 256, 1)])
+SHARED = [([1] * 5, [300, 260, 257, 400, 290], 256), ([1] * 5, [700, 0, 650, 610, 680], 600), ([1] * 4, [2000, 1400, 1350, 1333], 1331),
+          ([3, 1, 5, 0, 2, 1, 2], [400, 300, 270, 500, 310, 267, 300], 265), ([1] * 6, [129, 130, 128, 200, 131, 140], 128),
+          ([9, 7, 8, 9, 1], [900, 800, 790, 830, 778], 777), ([2] * 6, [1500, 40, 1501, 1402, 1450, 1499], 1400),
+          ([1] * 70, [200 + i for i in range(70)], 190), ([1] * 6, [260, 256, 257, 255, 1, 258], 256)]
+
+
+@pytest.mark.parametrize("G,page,width,d,fp8", [(1, 16, 1, 64, False), (4, 64, 1, 128, False), (2, 32, 6000, 128, True),
+                                                (3, 256, 1, 64, True), (4, 32, 1, 128, True)])
 @pytest.mark.parametrize("new,keys,shared", SHARED)
 def test_shared_prefix(fa, new, keys, shared, G, page, width, d, fp8):
     """Sequences behind one prefix, of whole pages or not, beside idle ones and ones that end inside the prefix."""
-    if len(new) > 10 and (G, page) != (4, 64):
-        new, keys = new[:9], keys[:9]
-    b = _share(Batch(keys, new, 2, G, d, fp8, page, seed=G + len(new)), shared)
-    _beside_idle(b, 0, width)
+    b = _behind(fa, keys, new, G, d, fp8, page, shared, width, seed=G + len(new))
     _run(fa, b, shared=shared)
-    if d == 128:
-        _run(fa, b, shared=shared, softcap=3.0, slopes=_slopes(2 * G))
+    if G in (1, 4):
+        _run(fa, b, shared=shared, softcap=3.0, slopes=_slopes(b.H * G))
         tree = _tree(b.new, 1, G)
         _run(fa, b, tree=tree, shared=shared, softcap=8.0)
-        _run(fa, b, shared=shared, prefix=[n - t // 2 for t, n in zip(b.new, b.keys)], slopes=_slopes(2 * G))
+        _run(fa, b, shared=shared, prefix=[n - t // 2 for t, n in zip(b.new, b.keys)], slopes=_slopes(b.H * G))
         _run(fa, b, shared=shared, window=200)
 
 
 @pytest.mark.parametrize("d,fp8", FORMATS)
 def test_shared_prefix_of_a_large_batch(fa, d, fp8):
-    """Rows enough for row tiles of 128, and single tokens without row starts."""
-    b = _share(Batch([2100 + 7 * i for i in range(48)], [1] * 48, 1, 8, d, fp8, 64, seed=3), 2000)
-    out, lse = _run(fa, b, shared=2000, starts=False)
-    again, norm = _run(fa, b, shared=2000, starts=False, check=False)
+    """Row tiles of 128 rows, single tokens without row starts, and a few of several."""
+    b = _behind(fa, [1103 + i % 9 for i in range(32)], [1] * 32, 8, d, fp8, 16, 1100, tile=128, seed=3)
+    out, lse = _run(fa, b, shared=1100, starts=False, slopes=_slopes(b.H * 8))
+    again, norm = _run(fa, b, shared=1100, starts=False, slopes=_slopes(b.H * 8), check=False)
     assert torch.equal(out, again) and torch.equal(lse, norm)
-    b = _share(Batch([1200 + 9 * i for i in range(12)], [13 - i for i in range(12)], 2, 4, d, fp8, 32, seed=3), 1100)
-    _run(fa, b, shared=1100)
+    if d == 128:
+        new = [1 + i % 4 for i in range(24)]
+        b = _behind(fa, [1104 + i % 7 + t for i, t in enumerate(new)], new, 4, d, fp8, 32, 1100, tile=128, seed=3)
+        _run(fa, b, shared=1100, softcap=4.0)
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+def test_few_keys_in_common(fa, d, fp8):
+    """Calls that gain nothing by a pass of its own, with any number of shared keys."""
+    b = _share(Batch([300, 290, 40], [1, 2, 1], 2, 4, d, fp8, 16, seed=7), 250)
+    want, _ = _run(fa, b)
+    for shared in (0, 1, 127, 128, 200, 250):
+        out, _ = _run(fa, b, shared=shared)
+        assert torch.equal(out, want)
 
 
 def test_shared_prefix_values(fa):
     """A NaN in the prefix reaches every row that sees it; one behind it its own sequence; queries stay apart."""
     for d, fp8 in FORMATS:
-        b = _share(Batch([400, 300, 290], [1, 1, 1], 2, 4, d, fp8, 16, seed=2), 256)
+        b = _behind(fa, [400, 300, 290, 261, 300], [1] * 5, 4, d, fp8, 16, 256, seed=2)
+        assert b.H >= 2
         clean, _ = _run(fa, b, shared=256)
         p, off = divmod(int(b.slots[0][70]), 16)
+        real = b.cache[1][p, 1, off, 0], b.cache[3][p, 0, off // 8, 1, off % 8]
         b.cache[3][p, 0, off // 8, 1, off % 8] = 255
         out, _ = _run(fa, b, check=False, shared=256)
         assert torch.isnan(out[:, :4, 32:64]).all()
         out[:, :4, 32:64] = clean[:, :4, 32:64]
         assert torch.equal(out, clean)
-        b.cache[3][p, 0, off // 8, 1, off % 8] = 120
+        b.cache[3][p, 0, off // 8, 1, off % 8] = real[1]
         b.cache[1][p, 1, off, 0] = 255
         out, _ = _run(fa, b, check=False, shared=256)
-        assert torch.isnan(out[:, 4:]).all() and torch.isfinite(out[:, :4]).all()
-        b.cache[1][p, 1, off, 0] = 120
+        assert torch.isnan(out[:, 4:8]).all()
+        out[:, 4:8] = clean[:, 4:8]
+        assert torch.equal(out, clean)
+        b.cache[1][p, 1, off, 0] = real[0]
         p, off = divmod(int(b.slots[1][270]), 16)
         b.cache[1][p, 1, off, 0] = 255
         out, _ = _run(fa, b, check=False, shared=256)
-        assert torch.isnan(out[1, 4:]).all() and torch.isfinite(out[1, :4]).all() and torch.isfinite(out[[0, 2]]).all()
+        assert torch.isnan(out[1, 4:8]).all()
+        out[1, 4:8] = clean[1, 4:8]
+        assert torch.equal(out, clean)
         b.cache[1][p, 1, off, 0] = 120
         b.q[2, 3, 5] = float("nan")
         out, _ = _run(fa, b, check=False, shared=256)
-        assert torch.isnan(out[2, 3]).all() and torch.isfinite(out[2, :3]).all() and torch.isfinite(out[:2]).all()
+        assert torch.isnan(out[2, 3]).all() and torch.isfinite(out[2, :3]).all() and torch.isfinite(out[[0, 1, 3, 4]]).all()
+
+
+def test_shared_prefix_missing_page(fa):
+    """A page of the prefix that is not in the cache: its keys do not exist, for any row."""
+    b = _behind(fa, [400, 300, 290, 261, 300], [1] * 5, 2, 128, False, 16, 256, seed=2)
+    keep = [s.copy() for s in b.slots]
+    b.table[:, 5] = 10 ** 6
+    out, lse = _run(fa, b, check=False, shared=256)
+    for i, n in enumerate(b.keys):   # the oracle's batch without those keys
+        b.slots[i] = np.delete(keep[i], range(80, 96))
+        b.keys[i] = n - 16
+    _check(b, out, lse)
 
 
 def test_shared_prefix_rows_of_no_sequence_stay(fa):
-    b = _share(Batch([300, 290], [3, 5], 1, 4, 128, True, 32, seed=6), 256)
+    b = _behind(fa, [300, 290, 280, 299], [3, 5, 1, 2], 4, 128, True, 32, 256, seed=6)
+    n = sum(b.new)
     b.q = torch.cat((b.q[:2], b.q, torch.full_like(b.q[:3], float("nan"))))
     b.starts += 2
-    out, lse = torch.full((13, 4, 128), 7.0, device="cuda"), torch.full((13, 4), 7.0, device="cuda")
+    out, lse = torch.full((n + 5, b.H * 4, 128), 7.0, device="cuda"), torch.full((n + 5, b.H * 4), 7.0, device="cuda")
     assert b.call(fa, out=out, lse=lse, shared=256) is out
     _check(b, out, lse)
     want = out.clone()
-    assert bool((out[:2] == 7).all() and (out[10:] == 7).all() and (lse[:2] == 7).all() and (lse[10:] == 7).all())
-    b.new = [3, 4]   # max_q of 4 for five tokens: the last row stays
+    rest = [0, 1, n + 2, n + 3, n + 4]
+    assert bool((out[rest] == 7).all() and (lse[rest] == 7).all())
+    b.new[1] = 4   # max_q of 4 for five tokens: the last row of the second sequence stays
     out.fill_(7)
     b.call(fa, out=out, shared=256)
-    assert torch.equal(out[2:9], want[2:9]) and bool((out[9] == 7).all())
+    assert bool((out[2 + 3 + 4] == 7).all())
+    _check(b, out, only=(0, 2, 3))
+    # its other rows: two results (a smaller max_q takes other row tiles), each off by 2^-8 (1 + 2^-7) of the mean of |v - o|, which is
+    # at most twice the largest |v|
+    most = np.abs(_values(b, 1, range(b.H))[1]).max()
+    assert (out[5:9] - want[5:9]).abs().max() <= 2 * 2.0 ** -8 * (1 + 2.0 ** -6) * 2 * most
 
 
 def test_graph_replays(fa):
-    """Two captured calls, each with a workspace of its own, replayed with the program's work between."""
-    b = _share(Batch([3000, 2400, 2500, 2900], [1] * 4, 2, 4, 128, False, 64, seed=8), 2300)
+    """Captured calls, each with a workspace of its own, replayed with the program's work between."""
+    b = _behind(fa, [3000, 2400, 2500, 2900], [1] * 4, 4, 128, False, 64, 2300, seed=8)
     cache = fa.KVCache(*(torch.from_numpy(t).cuda() for t in b.cache))
     table, lengths = torch.from_numpy(b.table).cuda(), torch.tensor(b.keys, dtype=torch.int32, device="cuda")
-    q, slopes = b.q.cuda(), torch.tensor(_slopes(8), device="cuda")
+    q, slopes = b.q.cuda(), torch.tensor(_slopes(b.H * 4), device="cuda")
     calls = [dict(shared=2300), dict(shared=2300, softcap=4.0, slopes=slopes), dict(window=1500, softcap=4.0)]
     want = [fa.cache_attention(q, cache, table, lengths, **o) for o in calls]
     other = [fa.cache_attention(-q, cache, table, lengths - 50, **o) for o in calls]
@@ -328,8 +386,7 @@ def test_graph_replays(fa):
             fa.cache_attention(q, cache, table, lengths, out=out, **o)
         graphs.append(graph), outs.append(out)
     for i in range(6):
-        sign = -1 if i % 2 else 1
-        q.copy_(b.q.cuda() * sign)
+        q.copy_(b.q.cuda() * (-1 if i % 2 else 1))
         lengths.copy_(torch.tensor(b.keys, dtype=torch.int32) - (50 if i % 2 else 0))
         for graph in graphs:
             graph.replay()
