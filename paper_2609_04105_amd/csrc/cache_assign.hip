@@ -18,21 +18,25 @@ namespace {
 constexpr int kScanThreads = 1024, kScanWaves = kScanThreads / 64;
 constexpr int kFillThreads = 256;
 
-// Of the whole call; the arrays of B ints behind it are Sums.
+// Of the whole call.
 struct Totals {
   unsigned take0, give0;  // places of the ring where pages are taken and returned
   int takes, gives;       // pages
 };
+// Of every sequence [B]: the exclusive sums of new tokens (and their end), of pages asked for and of pages returned by the
+// sequences before; its pages before the step, ~pages if it was refused, and after.
 struct Sums {
   Totals* totals;
-  int* need;  // [B] exclusive sum of the pages that the sequences before ask for
-  int* back;  // [B] of the pages that they return
-  int* had;   // [B] pages before the step, ~pages if the sequence was refused
-  int* now;   // [B] pages after it
+  int* start;
+  int* need;
+  int* back;
+  int* had;
+  int* now;
 };
 __device__ __forceinline__ Sums sums(const CacheAssignArgs& a) {
   Sums s;
   s.totals = static_cast<Totals*>(a.workspace);
+  s.start = a.starts;
   s.need = reinterpret_cast<int*>(s.totals + 1);
   s.back = s.need + a.B;
   s.had = s.back + a.B;
@@ -78,10 +82,9 @@ __device__ __forceinline__ Request request(const CacheAssignArgs& a, int b) {
 }
 
 // One workgroup: the sums, the starts, the lengths and counts after the step.
-__global__ __launch_bounds__(kScanThreads) void cache_assign_sums_kernel(const CacheAssignArgs a) {
+__device__ __forceinline__ void make_sums(const CacheAssignArgs& a, const Sums& s) {
   __shared__ int lds[3][kScanWaves];
   __shared__ int lds_takes;
-  const Sums s = sums(a);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t taken = a.counts[0], returned = a.counts[1];
   const int64_t left = (int64_t)((uint64_t)returned - (uint64_t)taken);
@@ -127,14 +130,16 @@ __global__ __launch_bounds__(kScanThreads) void cache_assign_sums_kernel(const C
       s.had[b] = served ? r.had : ~r.had;
       s.now[b] = r.now;
       const int length = a.lengths[b];
-      a.starts[b + 1] = end > a.tokens ? a.tokens : end;
+      const int stop = end > a.tokens ? a.tokens : end;
+      s.start[b + 1] = stop;
+      if (s.start != a.starts) a.starts[b + 1] = stop;
       a.lengths_out[b] = served ? (length < 0 ? 0 : length) : r.keys;
       if (served && need > 0) atomicMax(&lds_takes, upto);  // (the largest, in whatever order)
     }
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    a.starts[0] = 0;
+    s.start[0] = a.starts[0] = 0;
     const int64_t n = a.capacity;
     *s.totals = Totals{(unsigned)((taken % n + n) % n), (unsigned)((returned % n + n) % n), lds_takes, back0};
     a.counts_out[0] = taken + lds_takes;
@@ -142,29 +147,57 @@ __global__ __launch_bounds__(kScanThreads) void cache_assign_sums_kernel(const C
   }
 }
 
-// The last of n ascending values that is not above x (the first is not).
-__device__ __forceinline__ int find_last(const int* v, int n, int x) {
-  int lo = 0, hi = n;  // v[lo] <= x, v[hi] above (or the end)
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (v[mid] <= x) lo = mid;
-    else hi = mid;
+// The last of n ascending values that is not above x[j] (the first is not).  Every lane takes the same steps, and N
+// searches go side by side.
+template <int N>
+__device__ __forceinline__ void find_last(const int* v, int n, const int (&x)[N], int (&at)[N]) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) at[j] = 0;
+  for (int half = n > 1 ? 1 << (31 - __builtin_clz(n - 1)) : 0; half > 0; half >>= 1) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int mid = at[j] + half, in = mid < n ? mid : n - 1;
+      at[j] = v[in] <= x[j] ? in : at[j];
+    }
   }
-  return lo;
 }
 
-__global__ __launch_bounds__(kFillThreads) void cache_assign_fill_kernel(const CacheAssignArgs a) {
-  const Sums s = sums(a);
+// Moves pages first + i step, i < N, of `total`: sequence b's are those from before[b]; from(b, i, k) is page i of the
+// sequence, k of all, and to(b, i, k) takes it.  (N loads in flight: a load behind a store to what may be the same place waits.)
+template <int N, class From, class To>
+__device__ __forceinline__ void move_pages(const int* before, int B, int first, int step, int total, From&& from, To&& to) {
+  for (int k0 = first; k0 < total; k0 += N * step) {
+    int k[N], b[N], page[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) k[j] = k0 + j * step < total ? k0 + j * step : k0;
+    find_last(before, B, k, b);
+#pragma unroll
+    for (int j = 0; j < N; ++j) page[j] = from(b[j], k[j] - before[b[j]], k[j]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) to(b[j], k[j] - before[b[j]], k[j], page[j]);
+  }
+}
+
+// The tokens and pages of threads first, first + step, ..
+__device__ __forceinline__ void fill(const CacheAssignArgs& a, const Sums& s, int first, int step) {
   const Totals total = *s.totals;
-  const int first = blockIdx.x * kFillThreads + threadIdx.x, step = gridDim.x * kFillThreads;
   const unsigned ring = (unsigned)a.capacity;
   auto taken_page = [&](int k) { return a.ring[(total.take0 + (unsigned)k) % ring]; };
-  const int used = a.starts[a.B];
+  const int used = s.start[a.B];
   for (int i = first; i < a.tokens; i += step) {
     int64_t slot = -1, at = 0;
     if (i < used) {
-      const int b = find_last(a.starts, a.B, i), had = s.had[b];
-      at = (int64_t)a.lengths[b] - new_tokens(a, b) + (i - a.starts[b]);
+      int b = 0;
+      if (a.fresh) {
+        const int x[1] = {i};
+        int last[1];
+        find_last(s.start, a.B, x, last);
+        b = last[0];
+      } else {
+        b = i / a.each;
+      }
+      const int had = s.had[b];
+      at = (int64_t)a.lengths[b] - new_tokens(a, b) + (i - s.start[b]);
       const int64_t capacity = (int64_t)a.max_pages << a.page_shift;
       if (had >= 0 && at >= (int64_t)shared_pages(a, b) << a.page_shift && at < capacity) {
         const int place = (int)(at >> a.page_shift);
@@ -175,25 +208,44 @@ __global__ __launch_bounds__(kFillThreads) void cache_assign_fill_kernel(const C
     a.slots[i] = slot;
     a.positions[i] = at < 0 ? 0 : at;
   }
-  for (int k = first; k < total.takes; k += step) {
-    const int b = find_last(s.need, a.B, k);
-    a.page_table[(int64_t)b * a.max_pages + s.had[b] + (k - s.need[b])] = taken_page(k);
-  }
-  for (int k = first; k < total.gives; k += step) {
-    const int b = find_last(s.back, a.B, k);
-    a.ring[(total.give0 + (unsigned)k) % ring] = a.page_table[(int64_t)b * a.max_pages + s.now[b] + (k - s.back[b])];
-  }
+  auto row = [&](int b) { return a.page_table + (int64_t)b * a.max_pages; };
+  auto take = [&](int, int, int k) { return taken_page(k); };
+  auto keep = [&](int b, int i, int, int page) { row(b)[s.had[b] + i] = page; };
+  auto give = [&](int b, int i, int) { return row(b)[s.now[b] + i]; };
+  auto back = [&](int, int, int k, int page) { a.ring[(total.give0 + (unsigned)k) % ring] = page; };
+  if (total.takes <= step) move_pages<1>(s.need, a.B, first, step, total.takes, take, keep);
+  else move_pages<4>(s.need, a.B, first, step, total.takes, take, keep);
+  if (total.gives <= step) move_pages<1>(s.back, a.B, first, step, total.gives, give, back);
+  else move_pages<4>(s.back, a.B, first, step, total.gives, give, back);
+}
+
+// Small steps: everything in one workgroup, whose sums stay in LDS.
+__global__ __launch_bounds__(kScanThreads) void cache_assign_kernel(const CacheAssignArgs a) {
+  __shared__ Totals totals;
+  __shared__ int start[kAssignOne + 1], need[kAssignOne], back[kAssignOne], had[kAssignOne], now[kAssignOne];
+  const Sums s{&totals, start, need, back, had, now};
+  make_sums(a, s);
+  __syncthreads();
+  fill(a, s, threadIdx.x, kScanThreads);
+}
+
+__global__ __launch_bounds__(kScanThreads) void cache_assign_sums_kernel(const CacheAssignArgs a) { make_sums(a, sums(a)); }
+__global__ __launch_bounds__(kFillThreads) void cache_assign_fill_kernel(const CacheAssignArgs a) {
+  fill(a, sums(a), blockIdx.x * kFillThreads + threadIdx.x, gridDim.x * kFillThreads);
 }
 
 }  // namespace
 
-int64_t cache_assign_workspace(int64_t B) { return (int64_t)sizeof(Totals) + 16 * B; }
-
 hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream) {
-  cache_assign_sums_kernel<<<1, kScanThreads, 0, stream>>>(a);
-  const int64_t items = a.tokens > a.B ? a.tokens : a.B;
-  const int64_t groups = (items + kFillThreads - 1) / kFillThreads;
-  cache_assign_fill_kernel<<<(unsigned)(groups < 1024 ? groups : 1024), kFillThreads, 0, stream>>>(a);
+  if (a.B <= kAssignOne && a.tokens <= kAssignOneTokens) {
+    cache_assign_kernel<<<1, kScanThreads, 0, stream>>>(a);
+  } else {
+    // pages: at most the tables' and the ring's; a thread for every fourth, as few steps move many
+    const int64_t places = (int64_t)a.B * a.max_pages, pages = (places < a.capacity ? places : a.capacity) / 4;
+    const int64_t items = a.tokens > pages ? a.tokens : pages, groups = (items + kFillThreads - 1) / kFillThreads;
+    cache_assign_sums_kernel<<<1, kScanThreads, 0, stream>>>(a);
+    cache_assign_fill_kernel<<<(unsigned)(groups < 1 ? 1 : (groups < 1024 ? groups : 1024)), kFillThreads, 0, stream>>>(a);
+  }
   return hipGetLastError();
 }
 

@@ -75,7 +75,9 @@ struct CacheAssignArgs {
   int B, max_pages, page_shift, each, tokens, capacity;
 };
 
-int64_t cache_assign_workspace(int64_t B);
+// Sequences and tokens of a step that one workgroup serves, without a workspace.
+constexpr int kAssignOne = 1024, kAssignOneTokens = 4096;
+constexpr int64_t cache_assign_workspace(int64_t B) { return 16 + 16 * B; }
 hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream);
 
 struct CachePlan;  // cache_plan.hpp
