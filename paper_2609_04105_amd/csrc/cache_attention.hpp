@@ -656,8 +656,8 @@ __device__ __forceinline__ unsigned may_see(const Args& a, const Part& part, int
 // are replaced by y = C tanh(x) - slope |distance| with x = z / c, z = softmax_scale q . k, C = c log2(e) (capped), or by z log2(e)
 // less the bias; their factor is then 1.
 struct ScoreShape {
-  float factor;
-  float inside;  // of s: x, or z log2(e) without a cap
+  float factor;  // of what the scores are
+  float plain;   // of a product without a cap
   bool on;
 };
 template <bool FP8, class Args>
@@ -666,7 +666,7 @@ __device__ __forceinline__ ScoreShape score_shape(const Args& a) {
   s.factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
   if constexpr (Args::kShaped) {
     s.on = a.cap.on || a.slopes;
-    s.inside = a.cap.on ? a.cap.inside : s.factor;
+    s.plain = s.factor;
     if (s.on) s.factor = 1.0f;
   }
   return s;
@@ -687,51 +687,54 @@ __device__ __forceinline__ RowBias row_bias(const Args& a, const Sequence& seq, 
   }
   return r;
 }
-// A lane's scores of keys key .. key + 7, of N rows.  Where every |s| of the wave is at most cap.near, C tanh(x) is s K(s^2): 6
-// instructions a score.  Else x is formed, and beyond 0.6 C tanh(x) = C (1 - 2 / (e^2x + 1)), in which nothing cancels.
+// Capped scores of N times eight products, where |s| is at most cap.near, C tanh(x) = s K(s^2): 6 instructions a score.  Returns the
+// largest |s|.
 template <class Args, int N>
-__device__ __forceinline__ void shape_scores(const Args& a, const ScoreShape& shape, const RowBias (&bias)[N], int key, v4f (&s)[N][2]) {
-  if (a.cap.on) {
-    float most = 0.0f;
+__device__ __forceinline__ float cap_near(const Args& a, v4f (&s)[N][2]) {
+  float most = 0.0f;
 #pragma unroll
-    for (int r = 0; r < N; ++r)
+  for (int r = 0; r < N; ++r)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(s[r][j / 4][j % 4]));
-    if (!__any(most > a.cap.near)) {
-#pragma unroll
-      for (int r = 0; r < N; ++r)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float x = s[r][j / 4][j % 4], u = x * x;
-          s[r][j / 4][j % 4] = x * fmaf(fmaf(fmaf(fmaf(a.cap.k[4], u, a.cap.k[3]), u, a.cap.k[2]), u, a.cap.k[1]), u, a.cap.k[0]);
-        }
-    } else {
-      constexpr float k0 = kTanh[0], k1 = kTanh[1], k2 = kTanh[2], k3 = kTanh[3], k4 = kTanh[4];
-#pragma unroll
-      for (int r = 0; r < N; ++r)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float x = s[r][j / 4][j % 4] * shape.inside, u = x * x;
-          const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
-          float lo = x * a.cap.most * fmaf(fmaf(fmaf(fmaf(k4, u, k3), u, k2), u, k1), u, k0);
-          float hi = fmaf(-2.0f * a.cap.most, __builtin_amdgcn_rcpf(e + 1.0f), a.cap.most);
-          asm("" : "+v"(lo), "+v"(hi));  // both, and a choice: the compiler made a branch for every score of it
-          s[r][j / 4][j % 4] = fabsf(x) <= (float)kTanhNear ? lo : hi;
-        }
+    for (int j = 0; j < 8; ++j) {
+      const float x = s[r][j / 4][j % 4], u = x * x;
+      most = fmaxf(most, fabsf(x));
+      s[r][j / 4][j % 4] = x * fmaf(fmaf(fmaf(fmaf(a.cap.k[4], u, a.cap.k[3]), u, a.cap.k[2]), u, a.cap.k[1]), u, a.cap.k[0]);
     }
-  } else {
+  return most;
+}
+// Of any products: x is formed, and beyond 0.6 C tanh(x) = C (1 - 2 / (e^2x + 1)), in which nothing cancels.
+template <class Args, int N>
+__device__ __forceinline__ void cap_all(const Args& a, v4f (&s)[N][2]) {
+  constexpr float k0 = kTanh[0], k1 = kTanh[1], k2 = kTanh[2], k3 = kTanh[3], k4 = kTanh[4];
 #pragma unroll
-    for (int r = 0; r < N; ++r)
+  for (int r = 0; r < N; ++r)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] *= shape.inside;
+    for (int j = 0; j < 8; ++j) {
+      const float x = s[r][j / 4][j % 4] * a.cap.inside, u = x * x;
+      const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
+      float lo = x * a.cap.most * fmaf(fmaf(fmaf(fmaf(k4, u, k3), u, k2), u, k1), u, k0);
+      float hi = fmaf(-2.0f * a.cap.most, __builtin_amdgcn_rcpf(e + 1.0f), a.cap.most);
+      asm("" : "+v"(lo), "+v"(hi));  // both, and a choice: the compiler made a branch for every score of it
+      s[r][j / 4][j % 4] = fabsf(x) <= (float)kTanhNear ? lo : hi;
+    }
+}
+// Scores without a cap, in binades.
+template <int N>
+__device__ __forceinline__ void scale_scores(float factor, v4f (&s)[N][2]) {
+#pragma unroll
+  for (int r = 0; r < N; ++r)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] *= factor;
+}
+// The bias of keys key .. key + 7.
+template <int N>
+__device__ __forceinline__ void add_bias(const RowBias (&bias)[N], int key, v4f (&s)[N][2]) {
+#pragma unroll
+  for (int r = 0; r < N; ++r) {
+    const float far = (float)(bias[r].at - key);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = fmaf(-bias[r].slope, fabsf(far - (float)j), s[r][j / 4][j % 4]);
   }
-  if (a.slopes)
-#pragma unroll
-    for (int r = 0; r < N; ++r) {
-      const float far = (float)(bias[r].at - key);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = fmaf(-bias[r].slope, fabsf(far - (float)j), s[r][j / 4][j % 4]);
-    }
 }
 
 }  // namespace fp4attn

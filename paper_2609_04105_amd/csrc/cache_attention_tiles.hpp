@@ -228,7 +228,20 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
         }
         t.load_k(a.c, next, ahead, head, lane);
         if constexpr (Args::kShaped)
-          if (shape.on) shape_scores(a, shape, bias, key0 + 8 * g, s);
+          if (shape.on) {
+            if (a.cap.on) {
+              float most = 0.0f;
+#pragma unroll
+              for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(s[r][j / 4][j % 4]));
+              if (__any(most > a.cap.near)) cap_all(a, s);
+              else cap_near(a, s);
+            } else {
+              scale_scores(shape.plain, s);
+            }
+            if (a.slopes) add_bias(bias, key0 + 8 * g, s);
+          }
         if (masked) {
           // Hidden scores become -inf.  Keys that no row sees hold anything: their V codes and
           // scales become zero.  A non-finite V block that some row may see becomes zero too, and a NaN
