@@ -481,14 +481,15 @@ int64_t fp4attn_cache_attention_ex_workspace(const fp4attn_cache* cache, int64_t
  *   positions   [tokens] int64: of the tokens in their sequences, for fp4attn_rotary (padding, and below 0: 0)
  *   q_starts    [B + 1] int32: the sums of new_tokens, at most `tokens`: tokens past that have no slot
  *   lengths_out [B] int32, counts_out [2] int64: lengths and counts after the step (may be held and pool_counts themselves)
- *   workspace   at least fp4attn_cache_assign_workspace(B) bytes, 16-byte aligned; calls that may run at
- *               the same time need one each
+ *   workspace   at least fp4attn_cache_assign_workspace(B, tokens) bytes, 16-byte aligned (may be NULL for 0 bytes); calls that
+ *               may run at the same time need one each, and tables and pools of their own
  *
  * Pages go to the sequences in their order.  A sequence whose pages, together with all that the sequences before
  * it asked for, exceed the pool is refused, as is one of more than max_pages pages: it keeps its
  * row and its held[b] keys, which lengths_out tells, and takes nothing.  Pages returned in a step are for later
  * ones.  Negative numbers count as 0, held[b] and shared[b] past the table's end as its end.
- * Outputs must not overlap inputs or each other but for lengths_out and counts_out as above.
+ * Outputs must not overlap inputs or each other but for lengths_out and counts_out as above (a lengths_out that is
+ * lengths, new_tokens or shared is refused).
  *
  * Errors: INVALID_ARG for null or misaligned pointers, B, max_pages or pool_size < 1, tokens < 0 (0: slots and positions
  * may be NULL), a page_size that is no power of two or below 16, tokens not a multiple of B without
@@ -502,8 +503,8 @@ fp4attn_status fp4attn_cache_assign(int32_t* page_table, int64_t B, int64_t max_
                                     int32_t* q_starts, int32_t* lengths_out, int64_t* counts_out, void* workspace,
                                     int64_t workspace_bytes, void* stream);
 
-/* Bytes of workspace that such a call needs; -1 for a B that it refuses. */
-int64_t fp4attn_cache_assign_workspace(int64_t B);
+/* Bytes of workspace that such a call needs (0 for small ones); -1 for sizes that it refuses. */
+int64_t fp4attn_cache_assign_workspace(int64_t B, int64_t tokens);
 
 /*
  * Test hook: runs exactly the forward kernel of fp4attn_forward_mxfp4_ex (same

@@ -51,7 +51,7 @@ SIGNATURES = {
     "fp4attn_cache_write": [ctypes.POINTER(Cache), _c_p, _c_p, _int, _i64, _i64, _i64, _c_p, _c_p],
     "fp4attn_cache_read": [ctypes.POINTER(Cache), _c_p, _i64, _c_p, _c_p, _int, _c_p],
     "fp4attn_cache_assign": [_c_p, _i64, _i64, _i64] + [_c_p] * 5 + [_i64, _c_p, _i64] + [_c_p] * 6 + [_i64, _c_p],
-    "fp4attn_cache_assign_workspace": [_i64],
+    "fp4attn_cache_assign_workspace": [_i64, _i64],
     "fp4attn_cache_attention": [ctypes.POINTER(Cache), _c_p, _i64, _i64, _i64, _i64, _c_p, _i64, _c_p, _c_p, _i64, _c_p,
                                 _i64, _f32, _c_p, _int, _c_p, _c_p, _i64, _c_p],
     "fp4attn_cache_attention_workspace": [ctypes.POINTER(Cache)] + [_i64] * 4,

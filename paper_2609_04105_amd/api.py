@@ -624,12 +624,12 @@ def cache_assign(page_table, held, lengths, pool, page_size, tokens, new=None, s
     slots, positions = (torch.empty(n, dtype=torch.int64, device=dev) for _ in range(2))
     starts = torch.empty(B + 1, dtype=torch.int32, device=dev)
     after, counts_after = (held, counts) if in_place else (torch.empty_like(held), torch.empty_like(counts))
-    size = lib.fp4attn_cache_assign_workspace(B)
-    work = torch.empty(max(size, 16), dtype=torch.uint8, device=dev)
+    size = lib.fp4attn_cache_assign_workspace(B, tokens)
+    work = torch.empty(size, dtype=torch.uint8, device=dev) if size > 0 else None   # -1: the call says why
     _launch(dev, lib.fp4attn_cache_assign, _ptr(page_table), B, width, page_size, _ptr(held), _ptr(lengths),
             None if new is None else _ptr(new), None if shared is None else _ptr(shared), _ptr(free), free.numel(),
-            _ptr(counts), tokens, _ptr(slots), _ptr(positions), _ptr(starts), _ptr(after), _ptr(counts_after), _ptr(work),
-            max(size, 0), _stream(page_table))
+            _ptr(counts), tokens, _ptr(slots), _ptr(positions), _ptr(starts), _ptr(after), _ptr(counts_after),
+            None if work is None else _ptr(work), max(size, 0), _stream(page_table))
     return CacheStep(slots, positions, starts, after, KVPool(free, counts_after))
 
 

@@ -594,8 +594,8 @@ fp4attn_status fp4attn_cache_read(const fp4attn_cache* cache, const int64_t* slo
   return from_hip(fp4attn::launch_cache_read(a, static_cast<hipStream_t>(stream)), "cache read launch");
 }
 
-int64_t fp4attn_cache_assign_workspace(int64_t B) {
-  return B < 1 || B > 65535 ? -1 : fp4attn::cache_assign_workspace(B);
+int64_t fp4attn_cache_assign_workspace(int64_t B, int64_t tokens) {
+  return B < 1 || B > 65535 || tokens < 0 || tokens > 1 << 24 ? -1 : fp4attn::cache_assign_workspace(B, tokens);
 }
 
 fp4attn_status fp4attn_cache_assign(int32_t* page_table, int64_t B, int64_t max_pages, int64_t page_size,
@@ -631,10 +631,14 @@ fp4attn_status fp4attn_cache_assign(int32_t* page_table, int64_t B, int64_t max_
   REQUIRE_INDEX(q_starts);
   REQUIRE_INDEX(lengths_out);
   REQUIRE_INDEX(counts_out);
-  REQUIRE_PTR(workspace);
-  if (workspace_bytes < fp4attn::cache_assign_workspace(B))
-    return fail(FP4ATTN_ERR_INVALID_ARG, "workspace of %lld bytes, %lld are needed", (long long)workspace_bytes,
-                (long long)fp4attn::cache_assign_workspace(B));
+  if (lengths_out == lengths || lengths_out == new_tokens || lengths_out == shared)
+    return fail(FP4ATTN_ERR_INVALID_ARG, "lengths_out may be held, but no other input");
+  const int64_t need = fp4attn::cache_assign_workspace(B, tokens);
+  if (need > 0) {
+    REQUIRE_PTR(workspace);
+    if (workspace_bytes < need)
+      return fail(FP4ATTN_ERR_INVALID_ARG, "workspace of %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+  }
   fp4attn::CacheAssignArgs a{};
   a.page_table = page_table;
   a.held = held;

@@ -237,7 +237,7 @@ __global__ __launch_bounds__(kFillThreads) void cache_assign_fill_kernel(const C
 }  // namespace
 
 hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream) {
-  if (a.B <= kAssignOne && a.tokens <= kAssignOneTokens) {
+  if (assign_in_one(a.B, a.tokens)) {
     cache_assign_kernel<<<1, kScanThreads, 0, stream>>>(a);
   } else {
     // pages: at most the tables' and the ring's; a thread for every fourth, as few steps move many

@@ -18,16 +18,16 @@ def fa():
 
 def test_refusals(fa):
     f, size = fa.lib.fp4attn_cache_assign, fa.lib.fp4attn_cache_assign_workspace
-    need = size(3)
+    need = size(3, 5000)
     good = dict(table=PTR[0], B=3, pages=4, page=16, held=PTR[1], lengths=PTR[2], new=PTR[3], shared=PTR[4], ring=PTR[5],
-                ring_size=9, counts=PTR[6], tokens=7, slots=PTR[7], positions=PTR[8], starts=PTR[9], after=PTR[10],
+                ring_size=9, counts=PTR[6], tokens=5000, slots=PTR[7], positions=PTR[8], starts=PTR[9], after=PTR[10],
                 counts_out=PTR[11], work=PTR[12], bytes=need, stream=None)
 
     def status(**o):
         return f(*dict(good, **o).values())
     odd4, odd8 = ctypes.c_void_p(4098), ctypes.c_void_p(4100)
     for o in (dict(B=0), dict(B=-1), dict(pages=0), dict(ring_size=0), dict(tokens=-1), dict(page=8), dict(page=48),
-              dict(page=0), dict(page=-16), dict(new=None), dict(work=None), dict(work=odd8), dict(bytes=need - 1),
+              dict(page=0), dict(page=-16), dict(new=None), dict(after=PTR[2]), dict(after=PTR[3]), dict(after=PTR[4]), dict(work=None), dict(work=odd8), dict(bytes=need - 1),
               *(dict([(name, bad)]) for name in ("table", "held", "lengths", "ring", "starts", "after") for bad in (None, odd4)),
               *(dict([(name, bad)]) for name in ("counts", "slots", "positions", "counts_out") for bad in (None, odd8)),
               dict(new=odd4), dict(shared=odd4)):
@@ -36,7 +36,8 @@ def test_refusals(fa):
               dict(pages=(1 << 26) + 1), dict(pages=1 << 30, page=16), dict(B=65535, pages=32769, bytes=1 << 30),
               dict(pages=1 << 62)):
         assert status(**o) == 2, o
-    assert size(0) == size(65536) == -1 and 0 < size(1) <= size(65535) < 1 << 21
+    assert size(0, 1) == size(65536, 1) == size(1, -1) == size(1, (1 << 24) + 1) == -1
+    assert size(1, 1) == size(1024, 4096) == 0 and 0 < size(1, 4097) <= size(65535, 1) < 1 << 21
 
 
 def test_python_refusals_without_a_gpu(fa):

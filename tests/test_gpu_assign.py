@@ -180,7 +180,9 @@ def test_refusals_and_the_python_path(fa, monkeypatch):
                      (dict(pool=(pool.free, pool.counts[:1])), ValueError), (dict(pool=(pool.free.long(), pool.counts)), TypeError),
                      (dict(pool=(pool.free[:0], pool.counts)), fa.Fp4AttnError), (dict(page_size=24), fa.Fp4AttnError),
                      (dict(page_size=16.0), TypeError), (dict(tokens=3), fa.Fp4AttnError), (dict(tokens=-2), fa.Fp4AttnError),
-                     (dict(tokens=1 << 25), fa.Fp4AttnError), (dict(lengths=held.cpu()), ValueError)):
+                     (dict(tokens=1 << 25), fa.Fp4AttnError), (dict(lengths=held.cpu()), ValueError),
+                     (dict(lengths=held, in_place=True), fa.Fp4AttnError), (dict(new=held, in_place=True), fa.Fp4AttnError),
+                     (dict(shared=held, in_place=True), fa.Fp4AttnError)):
         with pytest.raises(error):
             fa.cache_assign(**dict(good, **o))
     assert table.tolist() == [[0, -1], [1, -1]] and pool.counts.tolist() == [0, 2]   # refused calls change nothing
