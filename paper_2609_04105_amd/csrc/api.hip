@@ -779,6 +779,11 @@ fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void
     st = from_hip(fp4attn::launch_prefix_attention(pre, p.prefix.plan, s), "shared prefix launch");
     if (st != FP4ATTN_OK) return st;
   }
+  if (!a.cap.on && a.slopes == nullptr) {
+    fp4attn::MaskedAttentionArgs masked{};
+    static_cast<fp4attn::ShapedAttentionArgs&>(masked) = a;
+    return from_hip(fp4attn::launch_masked_attention(masked, p.plan, s), "cache attention launch");
+  }
   return from_hip(fp4attn::launch_shaped_attention(a, p.plan, s), "cache attention launch");
 }
 

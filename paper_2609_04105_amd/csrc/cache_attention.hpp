@@ -71,7 +71,7 @@ __device__ __forceinline__ v4i probabilities(const v4f (&s)[2], float factor, fl
 template <class Args>
 __device__ __forceinline__ void fetch_arguments(const Args& a, const CachePlan& plan) {
   asm volatile("" ::"s"(a.c.H), "s"(a.B), "s"(a.tree), "s"(plan.ranges));
-  if constexpr (Args::kShaped) asm volatile("" ::"s"(a.cap.on), "s"(a.prefix_acc));
+  if constexpr (Args::kShaped) asm volatile("" ::"s"(a.window), "s"(a.prefix_acc));
 }
 
 // Of numbers that are not negative (half the instructions of a signed division).
@@ -658,35 +658,30 @@ __device__ __forceinline__ unsigned may_see(const Args& a, const Part& part, int
 struct ScoreShape {
   float factor;  // of what the scores are
   float plain;   // of a product without a cap
-  bool on;
 };
 template <bool FP8, class Args>
 __device__ __forceinline__ ScoreShape score_shape(const Args& a) {
   ScoreShape s{};
   s.factor = a.softmax_scale * kLog2e * (FP8 ? 1.0f : 1.0f / 6.0f);
-  if constexpr (Args::kShaped) {
-    s.on = a.cap.on || a.slopes;
+  if constexpr (Args::kScores) {
     s.plain = s.factor;
-    if (s.on) s.factor = 1.0f;
+    if (a.cap.on || a.slopes) s.factor = 1.0f;
   }
   return s;
 }
-// A row's slope in binades, the token's place that its distances count from, and its number among the rows of q.
-struct RowBias {
-  float slope;
-  int at;
-  int row;
-};
+// The slope of a query head in binades.
 template <class Args>
-__device__ __forceinline__ RowBias row_bias(const Args& a, const Sequence& seq, int token, int head) {
-  RowBias r{0.0f, 0, 0};
-  if constexpr (Args::kShaped) {
-    if (a.slopes) r.slope = a.slopes[head] * kLog2e;
-    r.at = Args::kPrefix ? seq.keys : seq.prefix + token;
-    r.row = (seq.first + token) * a.Hq + head;  // below 2^31
-  }
-  return r;
+__device__ __forceinline__ float slope_of(const Args& a, int head) {
+  if constexpr (Args::kScores)
+    if (a.slopes) return a.slopes[head] * kLog2e;
+  return 0.0f;
 }
+// The place of a token that distances count from: in the pass over a shared prefix its end, for all tokens.
+template <class Args>
+__device__ __forceinline__ int place_of_token(const Sequence& seq, int token) {
+  return Args::kPrefix ? seq.keys : seq.prefix + token;
+}
+
 // Capped scores of N times eight products, where |s| is at most cap.near, C tanh(x) = s K(s^2): 6 instructions a score.  Returns the
 // largest |s|.
 template <class Args, int N>
@@ -726,14 +721,25 @@ __device__ __forceinline__ void scale_scores(float factor, v4f (&s)[N][2]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] *= factor;
 }
-// The bias of keys key .. key + 7.
-template <int N>
-__device__ __forceinline__ void add_bias(const RowBias (&bias)[N], int key, v4f (&s)[N][2]) {
+// Scores without a cap, with the bias of keys key .. key + 7 that lie before their tokens (of later ones: any number).
+template <class Args, int N>
+__device__ __forceinline__ void scale_with_bias(const Sequence& seq, float factor, const float (&slope)[N], const int (&token)[N],
+                                                int key, v4f (&s)[N][2]) {
 #pragma unroll
   for (int r = 0; r < N; ++r) {
-    const float far = (float)(bias[r].at - key);
+    const float first = slope[r] * (float)(key - place_of_token<Args>(seq, token[r]));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = fmaf(-bias[r].slope, fabsf(far - (float)j), s[r][j / 4][j % 4]);
+    for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = fmaf(s[r][j / 4][j % 4], factor, fmaf(slope[r], (float)j, first));
+  }
+}
+// The bias of keys key .. key + 7.
+template <class Args, int N>
+__device__ __forceinline__ void add_bias(const Sequence& seq, const float (&slope)[N], const int (&token)[N], int key, v4f (&s)[N][2]) {
+#pragma unroll
+  for (int r = 0; r < N; ++r) {
+    const float far = (float)(place_of_token<Args>(seq, token[r]) - key);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[r][j / 4][j % 4] = fmaf(-slope[r], fabsf(far - (float)j), s[r][j / 4][j % 4]);
   }
 }
 

@@ -154,14 +154,14 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
     int token[kNr];  // of the sequence
-    RowBias bias[kNr];
+    float slope[kNr];
     v4i q[kNr][F::kSteps];
 #pragma unroll
     for (int r = 0; r < kNr; ++r) {
       const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
       token[r] = divide(ic, a.G);
       const int h = head * a.G + (ic - token[r] * a.G);
-      bias[r] = row_bias(a, seq, token[r], h);
+      slope[r] = slope_of(a, h);
       const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
 #pragma unroll
       for (int s = 0; s < F::kSteps; ++s) q[r][s] = reinterpret_cast<const v4i*>(p)[s];
@@ -186,9 +186,13 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
     if constexpr (Args::kShaped && !Args::kPrefix)
       if (part.first && shared_keys(a, seq) && row0 < rows) {  // a row begins with the pieces of the shared prefix
 #pragma unroll
-        for (int r = 0; r < kNr; ++r)
+        for (int r = 0; r < kNr; ++r) {
+          const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1, h = head * a.G + (ic - token[r] * a.G);
+          const int row = (seq.first + token[r]) * a.Hq + h;  // below 2^31
+          const float lower = slope[r] * (float)(seq.prefix + token[r] - a.shared);
           for (int k = 0; k < a.prefix_pieces; ++k)
-            add_piece<D>(a, k, bias[r].row, g, bias[r].slope * (float)(bias[r].at - a.shared), &ref[r], &sum[r], &sum16[r], acc[r]);
+            add_piece<D>(a, k, row, g, lower, &ref[r], &sum[r], &sum16[r], acc[r]);
+        }
       }
     const ScalarInts table = (ScalarInts)(uintptr_t)(a.page_table + (int64_t)range.b * a.max_pages);
     auto pages_of = [&](int key) { return key < part.end ? find_pages(a, table, key) : Pages{0, 0}; };
@@ -286,27 +290,36 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
         }
       };
       multiply();
-      if constexpr (Args::kShaped)
-        if (shape.on) {
-          if (a.cap.on) {
-            // As if all were near the cap's middle, between the products; where one is not, the products are formed again.  (Asked
-            // before: chunks of 1024 tokens behind a window of 1024 160 us instead of 148.)
-            float most = 0.0f;
+      if constexpr (Args::kScores) {
+        const int base = key0 + 8 * g;
+        if (a.cap.on) {
+          // As if all were near the cap's middle, between the products; where one is not, the products are formed again.  (Asked
+          // before: chunks of 1024 tokens behind a window of 1024 160 us instead of 148.)
+          float most = 0.0f;
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile) most = fmaxf(most, cap_near(a, s[tile]));
-            if (__any(most > a.cap.near)) {
-              multiply();
+          for (int tile = 0; tile < kTiles; ++tile) most = fmaxf(most, cap_near(a, s[tile]));
+          if (__any(most > a.cap.near)) {
+            multiply();
 #pragma unroll
-              for (int tile = 0; tile < kTiles; ++tile) cap_all(a, s[tile]);
-            }
-          } else {
-#pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile) scale_scores(shape.plain, s[tile]);
+            for (int tile = 0; tile < kTiles; ++tile) cap_all(a, s[tile]);
           }
           if (a.slopes)
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile) add_bias(bias, key0 + kTile * tile + 8 * g, s[tile]);
+            for (int tile = 0; tile < kTiles; ++tile) add_bias<Args>(seq, slope, token, base + kTile * tile, s[tile]);
+        } else if (a.slopes) {
+          if (a.open_keys) {
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile) {
+              scale_scores(shape.plain, s[tile]);
+              add_bias<Args>(seq, slope, token, base + kTile * tile, s[tile]);
+            }
+          } else {
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile)
+              scale_with_bias<Args>(seq, shape.plain, slope, token, base + kTile * tile, s[tile]);
+          }
         }
+      }
       bool all = !some_hidden(a, part, key0, kKeys);
 #pragma unroll
       for (int tile = 0; tile < kTiles; ++tile) all = all && is_page(a.c, pages[tile].p0) && is_page(a.c, pages[tile].p1);

@@ -1,4 +1,4 @@
-// Attention over the cache with capped or biased scores, a window or a prefix mask, or behind a shared prefix.
+// Attention over the cache with capped or biased scores, under any mask, also behind a shared prefix.
 #include "cache_attention_rows.hpp"
 #include "cache_attention_tiles.hpp"
 

@@ -137,14 +137,14 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 
     // this lane's rows (the same for the four lane groups) and its part of their queries
     int token[NR];  // of the sequence
-    RowBias bias[NR];
+    float slope[NR];
     v4i q[kSharedQ ? 1 : NR][F::kSteps];  // in LDS later: wave r has row tile r
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1;
       token[r] = divide(ic, a.G);
       const int h = head * a.G + (ic - token[r] * a.G);
-      bias[r] = row_bias(a, seq, token[r], h);
+      slope[r] = slope_of(a, h);
       const uint16_t* p = static_cast<const uint16_t*>(a.q) + (int64_t)(seq.first + token[r]) * a.q_stride + h * D + g * (D / 4);
       if (!kSharedQ || r == wave)
 #pragma unroll
@@ -187,9 +187,13 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
     if constexpr (Args::kShaped && !Args::kPrefix)
       if (part.first && shared_keys(a, seq)) {  // the waves begin with the pieces of the shared prefix
 #pragma unroll
-        for (int r = 0; r < NR; ++r)
+        for (int r = 0; r < NR; ++r) {
+          const int i = row0 + 16 * r + m, ic = i < rows ? i : rows - 1, h = head * a.G + (ic - token[r] * a.G);
+          const int row = (seq.first + token[r]) * a.Hq + h;  // below 2^31
+          const float lower = slope[r] * (float)(seq.prefix + token[r] - a.shared);
           for (int k = wave; k < a.prefix_pieces; k += kWaves)
-            add_piece<D>(a, k, bias[r].row, g, bias[r].slope * (float)(bias[r].at - a.shared), &ref[r], &sum[r], &sum16[r], acc[r]);
+            add_piece<D>(a, k, row, g, lower, &ref[r], &sum[r], &sum16[r], acc[r]);
+        }
       }
 
     // The wave's tiles.  One set of registers: a tile's K is loaded when the one before has
@@ -227,21 +231,26 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
           });
         }
         t.load_k(a.c, next, ahead, head, lane);
-        if constexpr (Args::kShaped)
-          if (shape.on) {
-            if (a.cap.on) {
-              float most = 0.0f;
+        if constexpr (Args::kScores) {
+          const int base = key0 + 8 * g;
+          if (a.cap.on) {
+            float most = 0.0f;
 #pragma unroll
-              for (int r = 0; r < NR; ++r)
+            for (int r = 0; r < NR; ++r)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(s[r][j / 4][j % 4]));
-              if (__any(most > a.cap.near)) cap_all(a, s);
-              else cap_near(a, s);
-            } else {
+              for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(s[r][j / 4][j % 4]));
+            if (__any(most > a.cap.near)) cap_all(a, s);
+            else cap_near(a, s);
+            if (a.slopes) add_bias<Args>(seq, slope, token, base, s);
+          } else if (a.slopes) {
+            if (a.open_keys) {
               scale_scores(shape.plain, s);
+              add_bias<Args>(seq, slope, token, base, s);
+            } else {
+              scale_with_bias<Args>(seq, shape.plain, slope, token, base, s);
             }
-            if (a.slopes) add_bias(bias, key0 + 8 * g, s);
           }
+        }
         if (masked) {
           // Hidden scores become -inf.  Keys that no row sees hold anything: their V codes and
           // scales become zero.  A non-finite V block that some row may see becomes zero too, and a NaN

@@ -86,7 +86,7 @@ hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream);
 struct CachePlan;  // cache_plan.hpp
 
 struct CacheAttentionArgs {
-  static constexpr bool kShaped = false, kPrefix = false;
+  static constexpr bool kShaped = false, kScores = false, kPrefix = false;
   CacheView c;
   const void* q;
   int64_t q_stride;  // of a token, in elements
@@ -130,7 +130,7 @@ inline CapShape cap_shape(double scale, double c) {
 
 // Attention with shaped scores, other masks, a shared prefix.
 struct ShapedAttentionArgs : CacheAttentionArgs {
-  static constexpr bool kShaped = true;
+  static constexpr bool kShaped = true, kScores = true;
   CapShape cap;
   int window;            // keys that a token sees up to its own, 0: all
   const float* slopes;   // [Hq] or null
@@ -141,6 +141,10 @@ struct ShapedAttentionArgs : CacheAttentionArgs {
   float4* prefix_stat;  // [pieces][n * Hq]
   float* prefix_acc;    // [pieces][n * Hq][d]
 };
+// The same without a cap and slopes.
+struct MaskedAttentionArgs : ShapedAttentionArgs {
+  static constexpr bool kScores = false;
+};
 // The pass over the shared prefix itself.
 struct PrefixAttentionArgs : ShapedAttentionArgs {
   static constexpr bool kPrefix = true;
@@ -148,6 +152,7 @@ struct PrefixAttentionArgs : ShapedAttentionArgs {
 
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 hipError_t launch_shaped_attention(const ShapedAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
+hipError_t launch_masked_attention(const MaskedAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 hipError_t launch_prefix_attention(const PrefixAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 
 }  // namespace fp4attn
