@@ -445,7 +445,7 @@ void fp4attn_cache_attention_options_init(fp4attn_cache_attention_options* opts)
  * fp4attn_cache_attention with options (NULL: none).  Without one the two are the same call.
  *
  * Errors: those of fp4attn_cache_attention; INVALID_ARG for a wrong struct_size, a softcap other than 0 outside
- * [2^-64, 2^64], a negative window, misaligned slopes or prefix, shared outside [0, max_pages * page_size]; UNSUPPORTED for a window
+ * [2^-64, 2^64] or so far below softmax_scale that their quotient is not finite, a negative window, misaligned slopes or prefix, shared outside [0, max_pages * page_size]; UNSUPPORTED for a window
  * above 2^30, and for slopes, a window or a prefix with a tree.
  */
 fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void* q, int64_t n, int64_t q_heads,
@@ -486,7 +486,8 @@ int64_t fp4attn_cache_attention_ex_workspace(const fp4attn_cache* cache, int64_t
  *
  * Pages go to the sequences in their order.  A sequence whose pages, together with all that the sequences before
  * it asked for, exceed the pool is refused, as is one of more than max_pages pages: it keeps its
- * row and its held[b] keys, which lengths_out tells, and takes nothing.  Pages returned in a step are for later
+ * row and its held[b] keys, which lengths_out tells, and takes nothing (a request that may not fit
+ * belongs behind those that must be served).  Pages returned in a step are for later
  * ones.  Negative numbers count as 0, held[b] and shared[b] past the table's end as its end.
  * Outputs must not overlap inputs or each other but for lengths_out and counts_out as above (a lengths_out that is
  * lengths, new_tokens or shared is refused).

@@ -12,6 +12,7 @@ goes through the checks here, with the same results and about 7 us more host tim
 """
 import ctypes
 import math
+import operator
 import warnings
 from typing import NamedTuple
 
@@ -595,8 +596,8 @@ def cache_assign(page_table, held, lengths, pool, page_size, tokens, new=None, s
     ``tokens / B`` each; tokens past their sum are padding.  ``shared`` (int32 [B]): keys at the start of a
     sequence whose whole pages belong to others.
 
-    Pages go out in the order of the sequences; one that the pool cannot serve keeps what it held: its
-    length in the result is ``held``, and its tokens have slot -1.  ``in_place`` writes the
+    Pages go out in the order of the sequences; one that the pool cannot serve, and every later one that asks
+    for pages, keeps what it held: its length in the result is ``held``, and its tokens have slot -1.  ``in_place`` writes the
     lengths and counts after the step into ``held`` and ``pool.counts``, for captured steps."""
     r = _binding.cache_assign(page_table, held, lengths, pool, page_size, tokens, new, shared, in_place)
     if r is not None:
@@ -607,8 +608,7 @@ def cache_assign(page_table, held, lengths, pool, page_size, tokens, new=None, s
     if len(pool) != 2:
         raise ValueError("a pool is (free, counts)")
     free, counts = pool
-    if not isinstance(page_size, int) or not isinstance(tokens, int):
-        raise TypeError("page_size and tokens must be integers")
+    page_size, tokens = operator.index(page_size), operator.index(tokens)
     named = ((held, "held", torch.int32, B), (lengths, "lengths", torch.int32, B), (new, "new", torch.int32, B),
              (shared, "shared", torch.int32, B), (free, "pool.free", torch.int32, None), (counts, "pool.counts", torch.int64, 2))
     used = [page_table]
@@ -698,12 +698,10 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
             raise ValueError(f"softcap={softcap} must be positive")
         o.softcap = softcap
     if window is not None:
-        if not isinstance(window, int) or window < 1:
-            raise ValueError(f"window={window} must be a positive integer")
-        o.window = min(window, 1 << 40)   # (above 2^30 the call refuses it)
-    if not isinstance(shared, int):
-        raise TypeError(f"shared={shared} must be an integer")
-    o.shared = max(-1, min(shared, 1 << 40))
+        if operator.index(window) < 1:
+            raise ValueError(f"window={window} must be positive")
+        o.window = min(operator.index(window), 1 << 40)   # (above 2^30 the call refuses it)
+    o.shared = max(-1, min(operator.index(shared), 1 << 40))
     if slopes is not None:
         _need(slopes, "slopes", torch.float32, 1)
         if slopes.numel() != Hq:

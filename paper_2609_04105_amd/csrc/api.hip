@@ -726,6 +726,8 @@ fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void
                 (long long)max_q);
   if (tree != nullptr && opts != nullptr && (opts->slopes != nullptr || opts->window != 0 || opts->prefix != nullptr))
     return fail(FP4ATTN_ERR_UNSUPPORTED, "a tree of tokens has no slopes, window or prefix: its tokens' places are not their order");
+  if (opts != nullptr && opts->softcap > 0.0f && !std::isfinite(softmax_scale / opts->softcap))
+    return fail(FP4ATTN_ERR_INVALID_ARG, "softmax_scale=%g over softcap=%g is not finite", (double)softmax_scale, (double)opts->softcap);
   REQUIRE_PTR(q);
   REQUIRE_PTR(out);
   REQUIRE_INDEX(page_table);

@@ -123,8 +123,9 @@ inline CapShape cap_shape(double scale, double c) {
   s.most = (float)most;
   double power = most * inside;
   for (int i = 0; i < 5; ++i, power *= inside * inside) s.k[i] = (float)(power * kTanh[i]);
-  // (caps above some hundred: a coefficient would leave fp32's normal numbers; near = 0 leaves all scores to the other form)
-  s.near = s.k[4] > 1e-36f ? (float)(kTanhNear / inside) : 0.0f;
+  // Outside fp32's normal numbers (caps above some hundred, caps far below the scale) no score counts as near: all take the other form.
+  const bool fits = s.k[4] > 1e-36f && s.k[4] < 1e30f && s.k[0] > 1e-36f && s.k[0] < 1e30f;
+  s.near = fits ? (float)(kTanhNear / inside) : -1.0f;
   return s;
 }
 

@@ -104,6 +104,18 @@ def test_softcap(fa, softcap, G, new, keys, idle, width, d, fp8):
         _run(fa, b, tree=tree, softcap=softcap)
 
 
+@pytest.mark.parametrize("d,fp8", [(64, True), (128, False)])
+@pytest.mark.parametrize("G,new,keys,idle,width", TILINGS[2:5])
+@pytest.mark.parametrize("softcap", [2.0 ** -64, 1e-6, 1e-3, 170.0, 2000.0, 2.0 ** 64])
+def test_caps_far_from_the_scores(fa, softcap, G, new, keys, idle, width, d, fp8):
+    """Caps far below and far above the scores, with queries that are zero (all scores are) among them."""
+    b = Batch(keys, new, 2, G, d, fp8, 32, seed=G + d)
+    b.q[::2] = 0.0
+    _beside_idle(b, idle, width)
+    out, _ = _run(fa, b, softcap=softcap)
+    assert torch.isfinite(out).all()
+
+
 @pytest.mark.parametrize("d,fp8", FORMATS)
 @pytest.mark.parametrize("G,new,keys,idle,width", TILINGS)
 @pytest.mark.parametrize("kind", ["geometric", "both signs", "with softcap"])
@@ -402,7 +414,7 @@ def test_refusals_and_the_python_path(fa, monkeypatch):
     slopes, prefix = torch.tensor(_slopes(4), device="cuda"), torch.tensor([5, 6], dtype=torch.int32, device="cuda")
     for o, error in ((dict(softcap=0.0), ValueError), (dict(softcap=-1.0), ValueError), (dict(softcap=float("nan")), ValueError),
                      (dict(softcap=float("inf")), fa.Fp4AttnError), (dict(window=0), ValueError), (dict(window=-3), ValueError),
-                     (dict(window=2.0), ValueError), (dict(window=(1 << 30) + 1), fa.Fp4AttnError), (dict(window=1 << 70), fa.Fp4AttnError),
+                     (dict(window=2.0), TypeError), (dict(window=(1 << 30) + 1), fa.Fp4AttnError), (dict(window=1 << 70), fa.Fp4AttnError),
                      (dict(slopes=slopes[:3]), ValueError), (dict(slopes=slopes.double()), TypeError), (dict(slopes=slopes.cpu()), ValueError),
                      (dict(slopes=slopes.clone().requires_grad_()), ValueError), (dict(prefix=prefix[:1]), ValueError),
                      (dict(prefix=prefix.long()), TypeError), (dict(shared=-1), fa.Fp4AttnError), (dict(shared=1 << 40), fa.Fp4AttnError),

@@ -46,6 +46,7 @@ def test_refusals(fa):
         assert status(o) == 1 and fa.lib.fp4attn_last_error(), o
         assert size(c, 2, 4, 2, 3, 1, _options(fa, **o)) == -1, o
     assert status(dict(window=(1 << 30) + 1)) == 2
+    assert status(dict(softcap=2.0 ** -60), scale=1e30, out=PTR[3]) == 1 and b"finite" in fa.lib.fp4attn_last_error()
     for o in (dict(window=5), dict(slopes=4096), dict(prefix=4096)):
         assert status(o, tree=PTR[4], words=1) == 2, o
     # accepted options come as far as the missing output
