@@ -177,10 +177,10 @@ __device__ __forceinline__ void find_last(const int* v, int n, const int (&x)[N]
 // sequence, k of all, and to(b, i, k) takes it.  (N loads in flight: a load behind a store to what may be the same place waits.)
 template <int N, class From, class To>
 __device__ __forceinline__ void move_pages(const int* before, int B, int first, int step, int total, From&& from, To&& to) {
-  for (int k0 = first; k0 < total; k0 += N * step) {
+  for (unsigned k0 = first; k0 < (unsigned)total; k0 += N * step) {  // (unsigned: may pass 2^31)
     int k[N], b[N], page[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) k[j] = k0 + j * step < total ? k0 + j * step : k0;
+    for (int j = 0; j < N; ++j) k[j] = (int)(k0 + j * step < (unsigned)total ? k0 + j * step : k0);
     find_last(before, B, k, b);
 #pragma unroll
     for (int j = 0; j < N; ++j) page[j] = from(b[j], k[j] - before[b[j]], k[j]);
