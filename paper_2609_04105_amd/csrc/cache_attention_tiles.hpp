@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
   // A CU serves the workgroups that came first, of the first half of the grid, before the others, which then end
   // later: those go first in every second tile.  64 sequences of 2768 keys 46.9 -> 45.7 us, of 16384
   // keys 210.3 -> 208.0; d = 64 119.4 -> 117.2; trees of 16 tokens over 8 of 2047 keys 22.6 -> 21.8.
-  const bool late = plan.split && blockIdx.x >= gridDim.x / 2;
+  const bool late = (plan.split || Args::kPrefix) && blockIdx.x >= gridDim.x / 2;
   Part part;
   while (open_part(a, plan, range, &part)) {
     const Sequence seq = range.seq;
