@@ -381,6 +381,54 @@ def test_shared_prefix_rows_of_no_sequence_stay(fa):
     assert (out[5:9] - want[5:9]).abs().max() <= 2 * 2.0 ** -8 * (1 + 2.0 ** -6) * 2 * most
 
 
+@pytest.mark.parametrize("o", [dict(window=70), dict(window=1200, softcap=4.0), dict(softcap=2.0, slopes=[0.5, 0.01]),
+                               dict(prefix=True), dict(prefix=True, window=300, slopes=[0.02, 0.1])])
+@pytest.mark.parametrize("B,H,G,T", [(300, 1, 2, 1), (130, 1, 2, 3)])
+def test_many_sequences(fa, B, H, G, T, o):
+    """More sequences than a wave has lanes, of very different lengths, some idle, cut and whole."""
+    rng = np.random.default_rng(B)
+    keys = [int(x) for x in rng.integers(T, 90, B)]
+    keys[3], keys[70], keys[B - 1] = 2600, 1500, 1100
+    new = [T] * B
+    if T > 1:
+        new[64] = new[10] = 0
+    else:
+        keys[64] = keys[10] = 0
+    o = dict(o)
+    if "prefix" in o:
+        o["prefix"] = [n - i % 5 for i, n in enumerate(keys)]
+    _run(fa, Batch(keys, new, H, G, 64, False, 32, seed=B), **o)
+
+
+@pytest.mark.parametrize("starts", [False, True])
+def test_the_first_sequences_are_idle(fa, starts):
+    """The prefix is taken from the first sequence that is behind it, past the first 64; the table's rows of the others hold
+    anything."""
+    keys = [0] * 66 + [900, 880, 0, 871, 890, 10]
+    b = _behind(fa, keys, [1] * len(keys), 2, 128, False, 16, 860, seed=4)
+    b.table[:66] = 10 ** 9
+    _run(fa, b, shared=860, starts=starts)
+    _run(fa, b, shared=860, starts=starts, slopes=_slopes(b.H * 2), softcap=9.0)
+
+
+@pytest.mark.parametrize("o", [dict(window=300, softcap=5.0), dict(shared=640)])
+def test_long_cache_offsets(fa, o):
+    """Pages whose bytes lie past 2^32 of the cache: the bits of a small cache's call."""
+    page, d = 128, 128
+    small = _behind(fa, [700 + i for i in range(40)], [1] * 40, 2, d, False, page, 640, seed=8)   # with a pass over the prefix
+    H = small.H
+    pages = (1 << 32) // (H * page * d // 2) + 64
+    cache = fa.kv_cache(pages, H, page, d)
+    n = small.cache[0].shape[0]
+    for big, t in zip(cache, small.cache):
+        big[pages - n:] = torch.from_numpy(t).cuda()
+    table = torch.from_numpy(np.where(small.table < 0, small.table, small.table + pages - n).astype(np.int32)).cuda()
+    lengths = torch.tensor(small.keys, dtype=torch.int32, device="cuda")
+    got = fa.cache_attention(small.q.cuda(), cache, table, lengths, **o)
+    assert torch.equal(got, small.call(fa, starts=False, **o))
+    del cache
+
+
 def test_graph_replays(fa):
     """Captured calls, each with a workspace of its own, replayed with the program's work between."""
     b = _behind(fa, [3000, 2400, 2500, 2900], [1] * 4, 4, 128, False, 64, 2300, seed=8)
