@@ -456,6 +456,26 @@ def test_graph_replays(fa):
         fa.cache_attention(q, cache, table, lengths, shared=2300).sum().item()
 
 
+def test_two_streams_at_once(fa):
+    """Calls behind prefixes on two streams, many in flight: each call's pieces are its own."""
+    batches = [_behind(fa, [1500 + 40 * i for i in range(5)], [1] * 5, 4, 128, fp8, 32, 1400, seed=i) for i, fp8 in enumerate((False, True))]
+    calls, want = [], []
+    for b in batches:
+        a = (b.q.cuda(), fa.KVCache(*(torch.from_numpy(t).cuda() for t in b.cache)), torch.from_numpy(b.table).cuda(),
+             torch.tensor(b.keys, dtype=torch.int32, device="cuda"))
+        calls.append(a)
+        want.append(fa.cache_attention(*a, shared=1400))
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in calls], [[], []]
+    for _ in range(20):
+        for a, stream, out in zip(calls, streams, outs):
+            with torch.cuda.stream(stream):
+                out.append(fa.cache_attention(*a, shared=1400))
+    torch.cuda.synchronize()
+    for out, w in zip(outs, want):
+        assert all(torch.equal(x, w) for x in out)
+
+
 def test_refusals_and_the_python_path(fa, monkeypatch):
     b = _share(Batch([300, 290], [2, 2], 2, 2, 64, False, 16, seed=1), 256)
     tree = np.full(4, 3, dtype=np.int64)
