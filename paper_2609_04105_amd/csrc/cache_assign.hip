@@ -7,7 +7,8 @@
 //   slot of token t: key j = length - new + t in page table[b][j / page]
 // Three prefix sums over the sequences, then every token and every page by itself: the sums go through one
 // workgroup, the rest over as many as there are tokens; a thread finds its sequence by bisection.
-// What bounds it: latency.  The data of a step are a few KB.
+// What bounds it: latency.  The data of a step are a few KB; 64 sequences with a token each take 4.2 us in a graph (a fill of one
+// word 1.6), 48 with 19 thousand tokens of prompts 7.5, 4096 with 35 thousand new tokens 13.5.
 #include "gfx950.hpp"
 #include "serving.hpp"
 

@@ -1,4 +1,12 @@
 // Attention over the cache with capped or biased scores, under any mask, also behind a shared prefix.
+//
+//   O_r = sum_j p_rj V_j / sum_j p_rj,  p_rj = exp(c tanh(s q_r . K_j / c) - slope_r |place_r - j|)
+//
+// The kernels of cache_attention_tiles.hpp and cache_attention_rows.hpp with their scores replaced between the two products; what
+// bounds them is as there, and the vector unit sooner: the cap takes six instructions a score, a bias two (three with a prefix mask).
+// Measured, 8 key heads of 4 query heads, d = 128, MXFP4: one token of 700 keys 9.0 us, with a cap 10.8, with slopes 10.9;
+// 838 row tiles of 128 rows behind a window of 1024 keys 112, with a cap 146; MXFP8, 4 key heads of 8 query heads, 48 tokens
+// of up to 16384 keys 48.5 us, with slopes 52.1.
 #include "cache_attention_rows.hpp"
 #include "cache_attention_tiles.hpp"
 
