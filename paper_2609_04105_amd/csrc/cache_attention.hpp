@@ -682,8 +682,12 @@ __device__ __forceinline__ int place_of_token(const Sequence& seq, int token) {
   return Args::kPrefix ? seq.keys : seq.prefix + token;
 }
 
-// Capped scores of N times eight products, where |s| is at most cap.near, C tanh(x) = s K(s^2): 6 instructions a score.  Returns the
-// largest |s|.
+// The cap's form near zero, y K(y^2).
+__device__ __forceinline__ float cap_form(const CapShape& c, float y) {
+  const float u = y * y;
+  return y * fmaf(fmaf(fmaf(fmaf(c.k[4], u, c.k[3]), u, c.k[2]), u, c.k[1]), u, c.k[0]);
+}
+// Capped scores of N times eight products, where |s| is at most cap.near: 7 instructions a score.  Returns the largest |s|.
 template <class Args, int N>
 __device__ __forceinline__ float cap_near(const Args& a, v4f (&s)[N][2]) {
   float most = 0.0f;
@@ -691,26 +695,30 @@ __device__ __forceinline__ float cap_near(const Args& a, v4f (&s)[N][2]) {
   for (int r = 0; r < N; ++r)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float x = s[r][j / 4][j % 4], u = x * x;
+      const float x = s[r][j / 4][j % 4];
       most = fmaxf(most, fabsf(x));
-      s[r][j / 4][j % 4] = x * fmaf(fmaf(fmaf(fmaf(a.cap.k[4], u, a.cap.k[3]), u, a.cap.k[2]), u, a.cap.k[1]), u, a.cap.k[0]);
+      s[r][j / 4][j % 4] = cap_form(a.cap, x);
     }
   return most;
 }
-// Of any products: x is formed, and beyond 0.6 C tanh(x) = C (1 - 2 / (e^2x + 1)), in which nothing cancels.
+// Of any products: the same value for those, and beyond the edge C tanh(x) = C (1 - 2 / (e^2x + 1)), in which nothing cancels.  A score
+// is what its own product makes it either way: which of the two a wave takes is decided by all its products, those with keys that no row sees
+// (whatever they hold, or LDS holds in their place) and of other rows among them.
 template <class Args, int N>
 __device__ __forceinline__ void cap_all(const Args& a, v4f (&s)[N][2]) {
-  constexpr float k0 = kTanh[0], k1 = kTanh[1], k2 = kTanh[2], k3 = kTanh[3], k4 = kTanh[4];
+  int on = a.cap.on;
+  asm volatile("" : "+s"(on));  // (unit and edge are formed here, not held in two scalar registers through the loop)
+  const float unit = on == 1 ? 1.0f : a.cap.inside, edge = on == 1 ? a.cap.near : (float)kTanhNear;
 #pragma unroll
   for (int r = 0; r < N; ++r)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float x = s[r][j / 4][j % 4] * a.cap.inside, u = x * x;
-      const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
-      float lo = x * a.cap.most * fmaf(fmaf(fmaf(fmaf(k4, u, k3), u, k2), u, k1), u, k0);
+      const float x = s[r][j / 4][j % 4], y = x * unit;
+      const float e = __builtin_amdgcn_exp2f(x * a.cap.inside * (2.0f * kLog2e));
+      float lo = cap_form(a.cap, y);
       float hi = fmaf(-2.0f * a.cap.most, __builtin_amdgcn_rcpf(e + 1.0f), a.cap.most);
       asm("" : "+v"(lo), "+v"(hi));  // both, and a choice: the compiler made a branch for every score of it
-      s[r][j / 4][j % 4] = fabsf(x) <= (float)kTanhNear ? lo : hi;
+      s[r][j / 4][j % 4] = fabsf(y) <= edge ? lo : hi;
     }
 }
 // Scores without a cap, in binades.

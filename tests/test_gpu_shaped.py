@@ -500,3 +500,96 @@ def test_refusals_and_the_python_path(fa, monkeypatch):
     monkeypatch.setattr(api, "_binding", api._NoBinding)
     for o, want in zip(calls, native):
         assert torch.equal(b.call(fa, **o), want)
+
+
+# ---------------------------------------------------------------- capped scores next to what no row sees
+
+NEAR = 50.0   # a cap of which the scores of these batches stay within 0.6, so that they take its polynomial
+
+
+def _page_zero_unused(b):
+    """Page 0, which is read in the place of pages that are not there, becomes one that no sequence holds."""
+    used = {int(p) for s in b.slots for p in np.unique(s // b.page)}
+    u = next(p for p in range(b.cache[0].shape[0]) if p not in used)
+    if 0 not in used:
+        return
+    b.table[b.table == 0] = u
+    b.slots = [np.where(s < b.page, s + u * b.page, s) for s in b.slots]
+    for t in b.cache:
+        t[[0, u]] = t[[u, 0]]
+
+
+def _put(b, slots, code, scale):
+    """Keys and values of one code and one scale in the given places of the cache."""
+    p, off = np.divmod(np.asarray(slots, dtype=np.int64), b.page)
+    for t, x in zip(b.cache[:2], (code, scale)):
+        t[p, :, off] = x
+    for t, x in zip(b.cache[2:], (code, scale)):
+        t[p, :, off // 8, :, off % 8] = x
+
+
+def _bits(x):
+    return x.view(torch.int32)
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("G,new,keys,idle,width", TILINGS)
+@pytest.mark.parametrize("window", [None, 33])
+def test_capped_scores_ignore_what_no_row_sees(fa, window, G, new, keys, idle, width, d, fp8):
+    """Large finite keys behind a sequence's end, behind its window and on pages that are not there leave every bit; those of
+    its last token leave the other tokens'."""
+    b = Batch(keys, new, 2, G, d, fp8, 16, seed=G + d)
+    _page_zero_unused(b)
+    _beside_idle(b, idle, width)
+    low = [0 if window is None else max(0, n - t + 1 - window) for t, n in zip(b.new, b.keys)]
+    for i, n in enumerate(low):
+        b.table[i, : n // 32] = -1   # (half of them, the others stay)
+    seen = np.unique(np.concatenate([s[n:] for s, n in zip(b.slots, low)]))
+    hidden = np.setdiff1d(np.arange(b.cache[0].shape[0] * 16), seen)
+    large = (0x7E if fp8 else 0x77, 140)
+    for slopes in (None, _slopes(2 * G)):
+        o = dict(softcap=NEAR, window=window, slopes=slopes)
+        _put(b, hidden, 0, 0)
+        want, norm = _run(fa, b, **o)
+        _put(b, hidden, *large)
+        out, lse = _run(fa, b, check=False, **o)
+        assert torch.equal(_bits(out), _bits(want)) and torch.equal(_bits(lse), _bits(norm))
+        saved = [t.copy() for t in b.cache]
+        last = [i for i, t in enumerate(b.new) if t > 1]
+        _put(b, [b.slots[i][-1] for i in last], *large)
+        out, lse = _run(fa, b, check=False, **o)
+        rest = torch.ones(len(out), dtype=torch.bool, device="cuda")
+        rest[[int(b.starts[i + 1]) - 1 for i in last]] = False
+        assert torch.equal(_bits(out[rest]), _bits(want[rest])) and torch.equal(_bits(lse[rest]), _bits(norm[rest]))
+        b.cache = saved
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+def test_capped_calls_repeat_after_other_work(fa, d, fp8):
+    """Row tiles of 128 rows whose keys end inside a step, in turn with calls that leave large and zero codes in the LDS of
+    every compute unit."""
+    b = Batch([40, 200, 9, 33], [40, 200, 9, 33], 2, 4, d, fp8, 16, seed=d)
+    _beside_idle(b, 512, 1)
+    other = Batch([256] * 8, [128] * 8, 16, 4, d, fp8, 16, seed=d)
+    want, norm = _run(fa, b, softcap=NEAR)
+    for i in range(4):
+        for code, scale in ((0x7E if fp8 else 0x77, 140), (0, 0)):
+            _put(other, np.concatenate(other.slots), code, scale)
+            _run(fa, other, softcap=NEAR, check=False)
+            out, lse = _run(fa, b, softcap=NEAR, check=False)
+            assert torch.equal(_bits(out), _bits(want)) and torch.equal(_bits(lse), _bits(norm)), i
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("tile", [None, 128])
+def test_capped_rows_behind_a_prefix_ignore_idle_ones(fa, tile, d, fp8):
+    """Queries of idle places hold anything: the rows beside them keep their bits."""
+    n = 32 if tile else 6
+    keys = [0 if i % 3 == 1 else 1103 + i % 9 for i in range(n)]
+    b = _behind(fa, keys, [1] * n, 8 if tile else 3, d, fp8, 16, 1100, tile=tile, seed=3)
+    idle = torch.tensor([i % 3 == 1 for i in range(n)])
+    b.q[idle] = 0.0
+    want, norm = _run(fa, b, shared=1100, starts=False, softcap=NEAR)
+    b.q[idle] = 1e4
+    out, lse = _run(fa, b, shared=1100, starts=False, softcap=NEAR, check=False)
+    assert torch.equal(_bits(out), _bits(want)) and torch.equal(_bits(lse), _bits(norm))
