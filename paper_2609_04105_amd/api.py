@@ -697,6 +697,8 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
         if not softcap > 0:
             raise ValueError(f"softcap={softcap} must be positive")
         o.softcap = softcap
+        if o.softcap == 0:   # (0 would be no cap)
+            raise ValueError(f"softcap={softcap} is not in [2^-64, 2^64]")
     if window is not None:
         if operator.index(window) < 1:
             raise ValueError(f"window={window} must be positive")

@@ -593,3 +593,11 @@ def test_capped_rows_behind_a_prefix_ignore_idle_ones(fa, tile, d, fp8):
     b.q[idle] = 1e4
     out, lse = _run(fa, b, shared=1100, starts=False, softcap=NEAR, check=False)
     assert torch.equal(_bits(out), _bits(want)) and torch.equal(_bits(lse), _bits(norm))
+
+
+@pytest.mark.parametrize("softcap", [1e-60, 1e-46, 5e-324, 2.0 ** -65])
+def test_caps_below_their_range_are_refused(fa, softcap):
+    """Also those that fp32 rounds to zero, which would be no cap."""
+    b = Batch([300], [2], 2, 2, 64, False, 16, seed=1)
+    with pytest.raises((ValueError, fa.Fp4AttnError), match="2\\^-64"):
+        b.call(fa, softcap=softcap)
