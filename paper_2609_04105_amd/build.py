@@ -19,6 +19,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libfp4attn.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["cache_attention_shaped.hip", "cache_attention_masked.hip", "cache_attention_prefix.hip", "cache_attention.hip",
+           "cache_attention_behind_shaped.hip", "cache_attention_behind_masked.hip",
            "fwd_mxfp4_guard.hip", "fwd_mxfp4_causal.hip", "fwd_mxfp4_ex2.hip", "fwd_mxfp4.hip", "fwd_mxfp4_ex2_dense.hip", "fwd_mxfp4_fp8pv.hip",
            "fwd_bf16.hip", "api.hip", "quantize.hip", "cache.hip", "cache_assign.hip", "rotary.hip", "mfma_stream.hip"]
 # The attention kernels never rely on NaN ordering in fmax; without this flag the
@@ -26,7 +27,8 @@ SOURCES = ["cache_attention_shaped.hip", "cache_attention_masked.hip", "cache_at
 EXTRA = {f: ["-fno-honor-nans"] for f in ("fwd_mxfp4.hip", "fwd_mxfp4_ex2.hip", "fwd_mxfp4_ex2_dense.hip",
                                           "fwd_mxfp4_guard.hip", "fwd_mxfp4_causal.hip", "fwd_mxfp4_fp8pv.hip",
                                           "fwd_bf16.hip", "cache_attention.hip", "cache_attention_shaped.hip",
-                                          "cache_attention_masked.hip", "cache_attention_prefix.hip")}
+                                          "cache_attention_masked.hip", "cache_attention_prefix.hip",
+                                          "cache_attention_behind_shaped.hip", "cache_attention_behind_masked.hip")}
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")

@@ -285,6 +285,7 @@ struct AttentionPlan {
   fp4attn::PrefixPlan prefix;
   bool shaped;  // some option is set
   int shared;   // keys of the prefix that has a pass of its own; 0: none
+  int crossings;  // row tiles that may be cut up beside direct ranges
   int64_t workspace;
 };
 fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int64_t q_heads, int64_t B, int64_t max_pages,
@@ -315,26 +316,23 @@ fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int6
     // few rows see the prefix: it gets no pass of its own
     const int64_t units = fp4attn::window_units(fp4attn::kRowsTile, (int)G, (int)opts->window);
     if (opts->prefix == nullptr && units * fp4attn::kUnit < span) span = units * fp4attn::kUnit;
-  } else if (n > 0 && n <= 0x7fffffff / q_heads && B > 1 && opts->shared >= fp4attn::kUnit) {
-    const int64_t keys = opts->shared / fp4attn::kUnit * fp4attn::kUnit;
-    const fp4attn::PrefixPlan prefix = fp4attn::prefix_plan(c.H, G, c.d, n, keys);
-    if (fp4attn::shares_prefix(p->plan, prefix, B, c.H, G, c.d, n, keys)) {
-      p->shared = (int)keys;
-      p->prefix = prefix;
-      span -= keys;
-    }
+  } else if (n <= 0x7fffffff / q_heads) {
+    const fp4attn::SharedPlan s = fp4attn::shared_plan(p->plan, B, c.H, G, c.d, c.fp8 != 0, max_q, n, max_keys, opts->shared);
+    p->shared = (int)s.shared;
+    p->prefix = s.prefix;
+    p->plan = s.plan;
   }
   if (!p->shaped && p->shared == 0) return FP4ATTN_OK;
   p->shaped = true;
-  if (span < 1) span = 1;
-  p->plan = fp4attn::cache_plan(B, c.H, G, c.d, c.fp8 != 0, max_q, span);
+  if (p->shared == 0) p->plan = fp4attn::cache_plan(B, c.H, G, c.d, c.fp8 != 0, max_q, span);
   // (a row tile smaller than the unshaped plan's, a sequence that does not join the shared prefix)
   const int64_t places = B * p->plan.row_tiles * ((max_keys + fp4attn::kUnit - 1) / fp4attn::kUnit + fp4attn::kSetup);
   if (!p->plan.fits || places + p->plan.ranges >= int64_t(1) << 31)
     return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_q=%lld max_pages=%lld: too many workgroups for one launch", (long long)B,
                 (long long)max_q, (long long)max_pages);
   p->workspace = p->plan.workspace;
-  if (p->shared > 0) p->workspace += p->prefix.pieces * p->prefix.rows * (16 + c.d * 4);
+  if (p->plan.direct > 0) p->crossings = (p->plan.ranges - p->plan.direct) * c.H;
+  if (p->shared > 0) p->workspace += p->prefix.pieces * p->prefix.rows * (16 + c.d * 4) + (p->crossings + 1) * int64_t(4);
   return FP4ATTN_OK;
 }
 
@@ -773,6 +771,12 @@ fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void
     a.prefix_stat = reinterpret_cast<float4*>(w);
     w += p.prefix.pieces * p.prefix.rows * 16;
     a.prefix_acc = reinterpret_cast<float*>(w);
+    if (p.plan.direct > 0) {
+      a.crossings = p.crossings;
+      a.own_tile = p.plan.tile;
+      a.direct_units = p.plan.direct_units;
+      a.arrived = reinterpret_cast<int*>(w + p.prefix.pieces * p.prefix.rows * a.c.d * 4);
+    }
     fp4attn::PrefixAttentionArgs pre{};
     static_cast<fp4attn::ShapedAttentionArgs&>(pre) = a;
     pre.tree = nullptr;  // its rows see the whole prefix
@@ -781,11 +785,15 @@ fp4attn_status fp4attn_cache_attention_ex(const fp4attn_cache* cache, const void
     st = from_hip(fp4attn::launch_prefix_attention(pre, p.prefix.plan, s), "shared prefix launch");
     if (st != FP4ATTN_OK) return st;
   }
-  if (!a.cap.on && a.slopes == nullptr) {
-    fp4attn::MaskedAttentionArgs masked{};
-    static_cast<fp4attn::ShapedAttentionArgs&>(masked) = a;
-    return from_hip(fp4attn::launch_masked_attention(masked, p.plan, s), "cache attention launch");
-  }
+  const bool scores = a.cap.on || a.slopes != nullptr;
+  auto launch = [&](auto args, auto launcher) {
+    static_cast<fp4attn::ShapedAttentionArgs&>(args) = a;
+    return from_hip(launcher(args, p.plan, s), "cache attention launch");
+  };
+  if (p.plan.direct > 0)
+    return scores ? launch(fp4attn::ShapedBehindArgs{}, fp4attn::launch_shaped_behind)
+                  : launch(fp4attn::MaskedBehindArgs{}, fp4attn::launch_masked_behind);
+  if (!scores) return launch(fp4attn::MaskedAttentionArgs{}, fp4attn::launch_masked_attention);
   return from_hip(fp4attn::launch_shaped_attention(a, p.plan, s), "cache attention launch");
 }
 

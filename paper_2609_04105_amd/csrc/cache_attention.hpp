@@ -154,6 +154,8 @@ struct Range {
   Sequence seq;
   int per;
   int piece;  // of the shared prefix
+  int rest;   // beside direct ranges: the first other range of its row tile, and the one in whose slots it leaves its own piece
+  int slot;
 };
 
 // Inclusive prefix sum over the wave's lanes: within rows of 16, then across them.
@@ -214,6 +216,50 @@ __device__ __forceinline__ Range find_range(const Args& a, const CachePlan& plan
   }
 }
 
+// Beside direct ranges: row tiles of more than direct_units units are cut after every `per` units, whose size leaves as many pieces as
+// there are other ranges.  The row tile's own range takes the first, the others the rest, in the order of the sequences.  The range of
+// piece w of those, or (w < 0) of the first piece of row tile `tile` of sequence b.
+template <class Args>
+__device__ __forceinline__ Range find_cut(const Args& a, const CachePlan& plan, int w, int b, int tile) {
+  const int lane = threadIdx.x & 63, ranges = plan.ranges - plan.direct;
+  Range r{};
+  Sequence seq{};  // the lane's
+  const int total = a.arrived[a.crossings];  // (look_for_long)
+  if (total == 0) return r;  // empty
+  r.per = divide(total + ranges - 1, ranges);
+  r.per = r.per < plan.min_units ? plan.min_units : r.per;
+  for (int b0 = 0, before = 0; b0 < a.B; b0 += 64) {
+    int units = 0, tiles = 0;
+    if (b0 + lane < a.B) {
+      seq = sequence(a, b0 + lane);
+      units = units_of(a, plan, seq);
+      tiles = units > a.direct_units ? row_tiles_of(a, plan, seq) : 0;
+    }
+    const int rests = divide(units + r.per - 1, r.per) - 1, own = tiles * rests, sum = prefix_sum(own);  // (units are at least 1 where tiles are)
+    const int from = before + sum - own;
+    const uint64_t found = __ballot(w < 0 ? b0 + lane == b : w >= from && w < from + own);
+    if (found) {
+      const int src = __ffsll((unsigned long long)found) - 1;
+      r.b = b0 + src;
+      r.seq.first = __builtin_amdgcn_readlane(seq.first, src);
+      r.seq.tokens = __builtin_amdgcn_readlane(seq.tokens, src);
+      r.seq.keys = __builtin_amdgcn_readlane(seq.keys, src);
+      r.seq.prefix = __builtin_amdgcn_readlane(seq.prefix, src);
+      r.units = __builtin_amdgcn_readlane(units, src);
+      const int start = __builtin_amdgcn_readlane(from, src), n = __builtin_amdgcn_readlane(rests, src);
+      r.tile = w < 0 ? tile : divide(w - start, n);
+      r.rest = start + r.tile * n;
+      r.slot = w < 0 ? r.rest : w;
+      r.begin = w < 0 ? 0 : (w - r.rest + 1) * r.per;
+      r.end = r.begin + r.per < r.units ? r.begin + r.per : r.units;
+      if (r.rest + n > ranges) r.end = r.begin;  // (only if the lengths were changed after the prefix's pass)
+      return r;
+    }
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  return r;  // empty
+}
+
 // Partial results in the workspace.  A row tile that crosses from range to range leaves a
 // piece in each: its first in slot 1 of its range, the others in slot 0 of theirs.  joins[w], of
 // the row tile whose first crossing is into range w: its pieces (0: there is none), its sequence's first
@@ -226,11 +272,12 @@ struct Partials {
 };
 __device__ __forceinline__ Partials partials(const CacheAttentionArgs& a, const CachePlan& p) {
   char* w = static_cast<char*>(a.workspace);
+  const int64_t ranges = p.ranges - p.direct;
   Partials r;
   r.joins = reinterpret_cast<int4*>(w);
-  w += (int64_t)p.ranges * 16;
+  w += ranges * 16;
   r.stat = reinterpret_cast<float4*>(w);
-  w += (int64_t)p.ranges * 2 * a.c.H * p.tile_rows * 16;
+  w += ranges * 2 * a.c.H * p.tile_rows * 16;
   r.acc = reinterpret_cast<float*>(w);
   return r;
 }
@@ -253,6 +300,21 @@ __device__ __forceinline__ void store_row(uint16_t* p, const float (&v)[N]) {
   for (int j = 0; j < N / 2; ++j) w[j] = __builtin_bit_cast(unsigned, v2bf{(__bf16)v[2 * j], (__bf16)v[2 * j + 1]});
   if constexpr (N == 8) *reinterpret_cast<uint4*>(p) = uint4{w[0], w[1], w[2], w[3]};
   else *reinterpret_cast<uint2*>(p) = uint2{w[0], w[1]};
+}
+
+// Values that workgroups of other XCDs read in the same launch: stores that go through to the memory that all XCDs share, loads from there.
+template <int N>
+__device__ __forceinline__ void store_through(float* p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i)
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p) + i, (uint64_t)as_uint(v[2 * i + 1]) << 32 | as_uint(v[2 * i]), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float4 load_through(const float* p) {
+  uint64_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) w[i] = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return float4{as_float((unsigned)w[0]), as_float((unsigned)(w[0] >> 32)), as_float((unsigned)w[1]), as_float((unsigned)(w[1] >> 32))};
 }
 
 // Of +0 and -0 only.  (The empty asm keeps it a test of bits: as a comparison of floats the compiler,
@@ -477,9 +539,53 @@ __device__ __forceinline__ void store_columns(const Args& a, const CachePlan& pl
       stat = p.stat;
       acc = p.acc;
     }
-    store_row<kCols>(acc + piece * D + c * kCols, x);
-    if (c == 0) stat[piece] = float4{ref, sum, rounded, 0.0f};
+    if constexpr (Args::kDirect) {
+      store_through(acc + piece * D + c * kCols, x);
+      if (c == 0) store_through(&stat[piece].x, {ref, sum, rounded, 0.0f});
+    } else {
+      store_row<kCols>(acc + piece * D + c * kCols, x);
+      if (c == 0) stat[piece] = float4{ref, sum, rounded, 0.0f};
+    }
   }
+}
+
+// A row's partial state {reference, sum, sum of the rounded values}, four columns in each lane.
+struct RowState {
+  float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
+  float4 acc = {0, 0, 0, 0};
+  __device__ __forceinline__ void add(const float4& s, const float4& o) {
+    const float top = fmaxf(ref, s.x);
+    const float mine = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
+    const float its = s.x == top ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
+    ref = top;
+    sum = sum * mine + s.y * its;
+    sum16 = sum16 * mine + s.z * its;
+    acc = float4{acc.x * mine + o.x * its, acc.y * mine + o.y * its, acc.z * mine + o.z * its, acc.w * mine + o.w * its};
+  }
+};
+// Adds pieces k, k + step .. of `pieces` of row `in_tile` of the row tile whose first crossing is into range w.
+template <int D>
+__device__ __forceinline__ void add_pieces(const CacheAttentionArgs& a, const CachePlan& plan, const Partials& part, int w, int head,
+                                           int in_tile, int lane, int k, int step, int pieces, RowState& state) {
+#pragma unroll 4
+  for (; k < pieces; k += step) {
+    const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? 1 : 0, head) + in_tile;
+    state.add(part.stat[at], reinterpret_cast<const float4*>(part.acc + at * D)[lane]);
+  }
+}
+// Stores row i of a sequence whose first token is `first`.
+template <int D, bool FP8>
+__device__ __forceinline__ void store_state(const CacheAttentionArgs& a, const RowState& s, int first, int i, int head, int lane) {
+  const int t = divide(i, a.G);
+  const int64_t at = (int64_t)(first + t) * a.Hq + head * a.G + (i - t * a.G);
+  const bool empty = is_zero(s.sum16);
+  const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / s.sum16;
+  const float o[4] = {empty ? 0.0f : s.acc.x * norm, empty ? 0.0f : s.acc.y * norm, empty ? 0.0f : s.acc.z * norm,
+                      empty ? 0.0f : s.acc.w * norm};
+  const int64_t to = at * D + lane * 4;
+  if (a.out_bf16) store_row<4>(static_cast<uint16_t*>(a.out) + to, o);
+  else store_row<4>(static_cast<float*>(a.out) + to, o);
+  if (a.lse && lane == 0) a.lse[at] = log_norm(s.ref, s.sum);
 }
 
 // Which range and key head a workgroup takes.  Workgroups are dealt round-robin to eight XCDs;
@@ -487,10 +593,51 @@ __device__ __forceinline__ void store_columns(const Args& a, const CachePlan& pl
 // sequence while its row tiles are at work.
 struct Place {
   int w, head;
+  bool tile;  // it is a row tile's own
 };
-__device__ __forceinline__ Place place_of(const CachePlan& plan) {
-  const int item = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, head = divide(item, plan.ranges);
-  return {item - head * plan.ranges, head};
+template <class Args>
+__device__ __forceinline__ Place place_of(const Args& a, const CachePlan& plan) {
+  int block = blockIdx.x, grid = gridDim.x, ranges = plan.ranges;
+  bool tile = !plan.split;
+  if constexpr (Args::kPrefix) {  // the last eight have no range
+    grid -= 8;
+    if (block >= grid) return {block - grid, a.c.H, false};
+  }
+  if constexpr (Args::kDirect) {  // those of each kind over all XCDs
+    const int direct = (plan.direct * a.c.H + 7) & ~7;
+    tile = block < direct;
+    block -= tile ? 0 : direct;
+    grid = tile ? direct : grid - direct;
+    ranges = tile ? plan.direct : ranges - plan.direct;
+  }
+  const int item = block % 8 * (grid / 8) + block / 8, head = divide(item, ranges);
+  return {item - head * ranges, head, tile};
+}
+// Whether a workgroup comes in the second half of those of its kind that fill the chip.
+template <class Args>
+__device__ __forceinline__ bool in_second_half(const Args& a, const CachePlan& plan) {
+  const unsigned all = Args::kDirect ? (unsigned)(plan.direct * a.c.H) : gridDim.x - (Args::kPrefix ? 8 : 0);
+  return blockIdx.x >= all / 2;
+}
+
+// For the sequences' own pass with direct ranges, by a workgroup of the shared prefix's that has no range: the units of its row tiles
+// of more than direct_units (mostly none: then the ranges beside the direct ones end at once), and no piece of them is there yet.
+template <class Args>
+__device__ __forceinline__ void look_for_long(const Args& a) {
+  if (a.arrived == nullptr) return;
+  __shared__ int lds[kWaves];
+  int units = 0;
+  for (int b = threadIdx.x; b < a.B; b += kThreads) {
+    const Sequence s = sequence(a, b);
+    const int its = (s.keys + kUnit - 1) / kUnit;
+    const bool joins = s.prefix >= a.shared && s.keys >= a.shared;  // (then it has at most direct_units of its own)
+    if (!joins && its > a.direct_units) units += divide(s.tokens * a.G + a.own_tile - 1, a.own_tile) * its;
+  }
+  units = prefix_sum(units);
+  if ((threadIdx.x & 63) == 63) lds[threadIdx.x / 64] = units;
+  for (int i = threadIdx.x; i < a.crossings; i += kThreads) a.arrived[i] = 0;
+  __syncthreads();
+  if (threadIdx.x == 0) a.arrived[a.crossings] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
 // The workgroup's range of the shared prefix: piece w / row_tiles of row tile w % row_tiles of all tokens
@@ -532,7 +679,9 @@ template <class Args>
 __device__ __forceinline__ Range open_range(const Args& a, const CachePlan& plan, const Place& p) {
   if constexpr (Args::kPrefix) return open_prefix(a, plan, p);
   Range range{};
-  if (plan.split) {
+  if constexpr (Args::kDirect)
+    if (!p.tile) return find_cut(a, plan, p.w, 0, 0);
+  if (!p.tile) {
     range = find_range(a, plan, p.w);
     if (p.head == 0 && threadIdx.x == 0) {
       int4 join = {0, 0, 0, 0};
@@ -547,6 +696,8 @@ __device__ __forceinline__ Range open_range(const Args& a, const CachePlan& plan
     range.tiles = row_tiles_of(a, plan, range.seq);
     range.units = units_of(a, plan, range.seq);
     range.end = range.tile < range.tiles ? range.units : 0;
+    if constexpr (Args::kDirect)
+      if (range.end > a.direct_units) return find_cut(a, plan, -1, range.b, range.tile);
   }
   return range;
 }
@@ -564,7 +715,7 @@ template <class Args>
 __device__ __forceinline__ int64_t piece_row(const Args& a, const CachePlan& plan, const Range& range, const Place& place,
                                              const Part& part, int row) {
   if constexpr (Args::kPrefix) return range.piece * a.n * a.Hq;
-  else return partial_row(a, plan, place.w, part.first ? 1 : 0, place.head) + row;
+  else return partial_row(a, plan, Args::kDirect ? range.slot : place.w, part.first ? 1 : 0, place.head) + row;
 }
 
 // Goes on to the next row tile, which begins at place `stop`; false at the end of the range.
@@ -652,6 +803,38 @@ __device__ __forceinline__ unsigned may_see(const Args& a, const Part& part, int
   return see;
 }
 
+// Beside direct ranges: the workgroup has stored a piece of its row tile, and the last of the row tile's to do so joins them, in their
+// order.  (A launch for it, as of a plan that is split, would take 4 us in every call; few have such a row tile.)
+template <int D, bool FP8, class Args>
+__device__ __forceinline__ void join_last(const Args& a, const CachePlan& plan, const Range& range, const Place& place, unsigned* lds) {
+  const int pieces = divide(range.units + range.per - 1, range.per);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // every wave's stores are through, before the count
+  __syncthreads();
+  if (threadIdx.x == 0) *lds = atomicAdd(a.arrived + range.rest * a.c.H + place.head, 1) == pieces - 1;
+  __syncthreads();
+  if (*lds == 0) return;
+  const Partials part = partials(a, plan);
+  const int lane = threadIdx.x % (D / 4), row0 = range.tile * plan.tile, rows = range.seq.tokens * a.G - row0;
+  constexpr int kAhead = 8;  // loads in flight
+  for (int row = threadIdx.x / (D / 4); row < rows && row < plan.tile; row += kThreads / (D / 4)) {
+    RowState state;
+    for (int k0 = 0; k0 < pieces; k0 += kAhead) {
+      float4 stat[kAhead], acc[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int k = k0 + j < pieces ? k0 + j : pieces - 1;
+        const int64_t at = partial_row(a, plan, range.rest + (k == 0 ? 0 : k - 1), k == 0 ? 1 : 0, place.head) + row;
+        stat[j] = load_through(&part.stat[at].x);
+        acc[j] = load_through(part.acc + at * D + 4 * lane);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+        if (k0 + j < pieces) state.add(stat[j], acc[j]);
+    }
+    store_state<D, FP8>(a, state, range.seq.first, row0 + row, place.head, lane);
+  }
+}
+
 // How a product of codes s = q . k becomes the exponent of a probability, in binades.  Plain: times `factor`.  Shaped, scores
 // are replaced by y = C tanh(x) - slope |distance| with x = z / c, z = softmax_scale q . k, C = c log2(e) (capped), or by z log2(e)
 // less the bias; their factor is then 1.
@@ -706,9 +889,9 @@ __device__ __forceinline__ float cap_near(const Args& a, v4f (&s)[N][2]) {
 // (whatever they hold, or LDS holds in their place) and of other rows among them.
 template <class Args, int N>
 __device__ __forceinline__ void cap_all(const Args& a, v4f (&s)[N][2]) {
-  int on = a.cap.on;
-  asm volatile("" : "+s"(on));  // (unit and edge are formed here, not held in two scalar registers through the loop)
-  const float unit = on == 1 ? 1.0f : a.cap.inside, edge = on == 1 ? a.cap.near : (float)kTanhNear;
+  int near = (int)as_uint(a.cap.near);
+  asm volatile("" : "+s"(near));  // (unit and edge are formed here, not held in scalar registers through the loop)
+  const float unit = near >= 0 ? 1.0f : a.cap.inside, edge = near >= 0 ? as_float(near) : (float)kTanhNear;
 #pragma unroll
   for (int r = 0; r < N; ++r)
 #pragma unroll

@@ -135,9 +135,13 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   fetch_arguments(a, plan);
-  const Place place = place_of(plan);
+  const Place place = place_of(a, plan);
   const int head = place.head;
-  if (head >= a.c.H) return;
+  if (head >= a.c.H) {
+    if constexpr (Args::kPrefix)
+      if (head == a.c.H && place.w == 0) look_for_long(a);
+    return;
+  }
   Range range = open_range(a, plan, place);
   if (range.begin >= range.end) return;
   const ScoreShape shape = score_shape<FP8>(a);
@@ -146,7 +150,7 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
   // Of a CU's two workgroups the one that came first, of the first half of the grid, is served first: a step took it
   // 2.17 us and the other 2.62, and it ended 60 us of 370 earlier.  The later one goes before it in every
   // second step: 373 -> 357 us, 8 of 512-token chunks 293 -> 282.
-  const bool late = blockIdx.x >= gridDim.x / 2;
+  const bool late = in_second_half(a, plan);
   Part part;
   while (open_part(a, plan, range, &part)) {
     const Sequence seq = range.seq;
@@ -467,6 +471,8 @@ __global__ __launch_bounds__(kThreads, kRowsPerCu) void cache_rows_kernel(const 
                               odd_marks.template of<F::kDTiles>(r, j), o);
       }
     }
+    if constexpr (Args::kDirect)
+      if (!part.whole) join_last<D, FP8>(a, plan, range, place, &odd_lds[0][0]);
     if (!next_tile(a, plan, part.stop, range)) break;
     __syncthreads();
   }

@@ -118,9 +118,13 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
 
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
   fetch_arguments(a, plan);
-  const Place place = place_of(plan);
+  const Place place = place_of(a, plan);
   const int head = place.head;
-  if (head >= a.c.H) return;
+  if (head >= a.c.H) {
+    if constexpr (Args::kPrefix)
+      if (head == a.c.H && place.w == 0) look_for_long(a);
+    return;
+  }
   Range range = open_range(a, plan, place);
   if (range.begin >= range.end) return;
   const ScoreShape shape = score_shape<FP8>(a);
@@ -129,7 +133,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
   // A CU serves the workgroups that came first, of the first half of the grid, before the others, which then end
   // later: those go first in every second tile.  64 sequences of 2768 keys 46.9 -> 45.7 us, of 16384
   // keys 210.3 -> 208.0; d = 64 119.4 -> 117.2; trees of 16 tokens over 8 of 2047 keys 22.6 -> 21.8.
-  const bool late = (plan.split || Args::kPrefix) && blockIdx.x >= gridDim.x / 2;
+  const bool late = (plan.split || Args::kPrefix) && in_second_half(a, plan);
   Part part;
   while (open_part(a, plan, range, &part)) {
     const Sequence seq = range.seq;
@@ -372,6 +376,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(D, NR)) void cache_attenti
                          !Args::kPrefix && part.whole,
                          piece_row(a, plan, range, place, part, 16 * r + row));
     }
+    if constexpr (Args::kDirect)
+      if (!part.whole) join_last<D, FP8>(a, plan, range, place, &lds_odd[0][0]);
     if (!next_tile(a, plan, part.stop, range)) break;
     __syncthreads();
   }
@@ -396,45 +402,19 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(const CacheAtt
   const int head = divide(row, plan.tile_rows), in_tile = row - head * plan.tile_rows;
   const int i = job.w * plan.tile + in_tile;
   const bool there = head < a.c.H && i < rows;
-  float ref = -__builtin_inff(), sum = 0.0f, sum16 = 0.0f;
-  float4 acc = {0, 0, 0, 0};
-  auto join = [&](const float4& s, const float4& o) {
-    const float top = fmaxf(ref, s.x);
-    const float mine = ref == top ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
-    const float its = s.x == top ? 1.0f : __builtin_amdgcn_exp2f(s.x - top);
-    ref = top;
-    sum = sum * mine + s.y * its;
-    sum16 = sum16 * mine + s.z * its;
-    acc = float4{acc.x * mine + o.x * its, acc.y * mine + o.y * its, acc.z * mine + o.z * its, acc.w * mine + o.w * its};
-  };
-  if (there) {
-#pragma unroll 4
-    for (int k = SPREAD ? group : 0; k < pieces; k += SPREAD ? kGroups : 1) {
-      const int64_t at = partial_row(a, plan, w - 1 + k, k == 0 ? 1 : 0, head) + in_tile;
-      join(part.stat[at], reinterpret_cast<const float4*>(part.acc + at * D)[lane]);
-    }
-  }
+  RowState state;
+  if (there) add_pieces<D>(a, plan, part, w, head, in_tile, lane, SPREAD ? group : 0, SPREAD ? kGroups : 1, pieces, state);
   if constexpr (SPREAD) {
     __shared__ float4 acc_lds[kGroups][kLanes];
     __shared__ float4 stat_lds[kGroups];
-    acc_lds[group][lane] = acc;
-    if (lane == 0) stat_lds[group] = float4{ref, sum, sum16, 0.0f};
+    acc_lds[group][lane] = state.acc;
+    if (lane == 0) stat_lds[group] = float4{state.ref, state.sum, state.sum16, 0.0f};
     __syncthreads();
     if (group != 0) return;
     const int used = pieces < kGroups ? pieces : kGroups;
-    for (int k = 1; k < used; ++k) join(stat_lds[k], acc_lds[k][lane]);
+    for (int k = 1; k < used; ++k) state.add(stat_lds[k], acc_lds[k][lane]);
   }
-  if (!there) return;
-  const int t = divide(i, a.G);
-  const int64_t at = (int64_t)(first + t) * a.Hq + head * a.G + (i - t * a.G);
-  const bool empty = is_zero(sum16);
-  const float norm = (FP8 ? 1.0f : 1.0f / 6.0f) / sum16;
-  const float o[4] = {empty ? 0.0f : acc.x * norm, empty ? 0.0f : acc.y * norm, empty ? 0.0f : acc.z * norm,
-                      empty ? 0.0f : acc.w * norm};
-  const int64_t to = at * D + lane * 4;
-  if (a.out_bf16) store_row<4>(static_cast<uint16_t*>(a.out) + to, o);
-  else store_row<4>(static_cast<float*>(a.out) + to, o);
-  if (a.lse && lane == 0) a.lse[at] = log_norm(ref, sum);
+  if (there) store_state<D, FP8>(a, state, first, i, head, lane);
 }
 
 template <int D, bool FP8, class Args>

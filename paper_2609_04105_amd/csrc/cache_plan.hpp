@@ -10,13 +10,15 @@ namespace fp4attn {
 // waves split the rows).  With split, the row tiles of all sequences, each with its keys in
 // units of 128, lie end to end (with a few places between them), and each of `ranges` workgroups
 // per key head takes an equal part of that line (fewer ranges if that leaves less than
-// min_units each); lengths are known on the device only.  Without, a range is a row tile.
+// min_units each); lengths are known on the device only.  Without, a range is a row tile; beside `direct` ones of that kind
+// there may be others, for the rest of row tiles of more than direct_units units (own_plan).
 struct CachePlan {
   int tile;       // rows of a row tile
   int row_tiles;  // of the longest sequence and one key head
   int tile_rows;  // rows of a tile that can be in use
   int split, ranges, min_units;
   bool fits;           // the line's places and the workgroups are in range
+  int direct, direct_units;
   int64_t workgroups;  // of the first launch
   int64_t workspace;   // bytes
 };
@@ -127,7 +129,7 @@ inline PrefixPlan prefix_plan(int64_t H, int64_t G, int64_t d, int64_t n, int64_
   p.units = (int)per;
   p.pieces = (int)((units + per - 1) / per);
   c.ranges = (int)(row_tiles * p.pieces);
-  c.workgroups = (row_tiles * p.pieces * H + 7) / 8 * 8;
+  c.workgroups = (row_tiles * p.pieces * H + 7) / 8 * 8 + 8;  // the last eight without a range (place_of, look_for_long)
   p.rows = rows * H;
   p.fits = c.workgroups <= 1 << 24;
   return p;
@@ -146,6 +148,49 @@ inline bool shares_prefix(const CachePlan& plan, const PrefixPlan& prefix, int64
   const double gain = plan.tile == kRowsTile ? 0.8 : 1.0;
   return prefix.fits && walk_time(prefix.plan.tile, d, prefix.plan.row_tiles * H, keys, true) <
                             gain * walk_time(plan.tile, d, tiles * H, keys, false);
+}
+
+// The plan of the sequences' own pass behind a shared prefix: for `own` keys, which those that join the prefix have at most.
+// One that does not join it may have max_keys.  If these would be cut up without the prefix and `own` keys are not, every row tile has a
+// direct range, and beside those are others for what is beyond the first pieces of row tiles with more than `own` keys (find_cut,
+// join_last in cache_attention.hpp).  us uncut / so / one by one, 8 key heads, d = 128, one token each, one sequence ending after 15/16 of the
+// prefix: 16 sequences, 4 query heads a key head, MXFP4, behind 65536 keys 393 / 61 / 128; 96, 8 query heads, MXFP8, 632 / 327 / 1158; 24,
+// 8 query heads, MXFP4, behind 16384 keys 121 / 46 / 56; with all sequences behind the prefix uncut 49, 282, 37, so 50, 281, 36.  (Cutting all
+// as without a prefix, with a launch that joins, 69, 311, 45, and with all behind 51, 287, 40; over 160 batches 11 % longer, so 1 %.)
+inline CachePlan own_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t own, int64_t max_keys) {
+  CachePlan p = cache_plan(B, H, G, d, fp8, max_q, own);
+  if (p.split || !cache_plan(B, H, G, d, fp8, max_q, max_keys).split) return p;
+  const int64_t units = (max_keys + kUnit - 1) / kUnit, places = B * p.row_tiles * units;
+  // A unit takes a workgroup 0.7 us, a piece the workgroup that joins them 0.45.
+  while (1.6 * p.min_units * p.min_units < (double)units) ++p.min_units;
+  int64_t others = 512 / H;  // (half as many: batches of which half ends inside the prefix 8 % slower; as many as the chip holds: the same)
+  if (others > (places + p.min_units - 1) / p.min_units) others = (places + p.min_units - 1) / p.min_units;
+  if (others < 2) return p;
+  p.direct = p.ranges;
+  p.direct_units = (int)((own + kUnit - 1) / kUnit);
+  p.ranges += (int)others;
+  p.workgroups += (others * H + 7) / 8 * 8;
+  p.fits = p.fits && p.workgroups <= 1 << 24;
+  p.workspace = others * 16 + others * 2 * H * p.tile_rows * (d * 4 + 16);
+  return p;
+}
+
+// The plan of a call that may pass over the first `shared` keys by themselves, of n tokens; `plan` serves it without.
+struct SharedPlan {
+  CachePlan plan;  // of the sequences' own pass
+  PrefixPlan prefix;
+  int64_t shared;  // keys that have a pass of their own; 0: none
+};
+inline SharedPlan shared_plan(const CachePlan& plan, int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, int64_t max_q, int64_t n,
+                              int64_t max_keys, int64_t shared) {
+  SharedPlan p{plan, {}, 0};
+  const int64_t keys = shared / kUnit * kUnit;
+  if (n < 1 || B < 2 || keys < 1) return p;
+  p.prefix = prefix_plan(H, G, d, n, keys);
+  if (!shares_prefix(plan, p.prefix, B, H, G, d, n, keys)) return p;
+  p.shared = keys;
+  p.plan = own_plan(B, H, G, d, fp8, max_q, max_keys > keys ? max_keys - keys : 1, max_keys);
+  return p;
 }
 
 }  // namespace fp4attn

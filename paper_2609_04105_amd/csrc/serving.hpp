@@ -86,7 +86,7 @@ hipError_t launch_cache_assign(const CacheAssignArgs& a, hipStream_t stream);
 struct CachePlan;  // cache_plan.hpp
 
 struct CacheAttentionArgs {
-  static constexpr bool kShaped = false, kScores = false, kPrefix = false;
+  static constexpr bool kShaped = false, kScores = false, kPrefix = false, kDirect = false;
   CacheView c;
   const void* q;
   int64_t q_stride;  // of a token, in elements
@@ -108,9 +108,9 @@ struct CacheAttentionArgs {
 // equal, 7.3e-8, 1.2 half steps of fp32.
 constexpr double kTanhNear = 0.6, kTanh[5] = {0.99999992687, -0.333323099773, 0.133101736776, -0.0521014805221, 0.0154754275956};
 // c tanh(z / c) in binades, of a product s of codes with z = scale s, with inside = scale / c and C = c log2(e): near zero
-// y K(y^2), beyond it C tanh(inside s) by an exponential.  on = 1: y = s, K's coefficients k_i = C inside^(2 i + 1) p_i, up to |s| = near.
-// Where these leave fp32's normal numbers (caps above some hundred, caps far below the scale) on = 2: y = inside s, k_i = C p_i, up to
-// |y| = kTanhNear, and no |s| is at most near.
+// y K(y^2), beyond it C tanh(inside s) by an exponential.  y = s, K's coefficients are k_i = C inside^(2 i + 1) p_i, up to |s| = near.
+// Where these leave fp32's normal numbers (caps above some hundred, caps far below the scale) near is -1, which no |s| is at
+// most: y = inside s, k_i = C p_i, up to |y| = kTanhNear.
 struct CapShape {
   int on;
   float inside, most;  // scale / c, C
@@ -120,15 +120,16 @@ inline CapShape cap_shape(double scale, double c) {
   CapShape s{};
   if (c == 0.0) return s;
   const double inside = scale / c, most = c * 1.4426950408889634;
+  s.on = 1;
   s.inside = (float)inside;
   s.most = (float)most;
   auto coefficients = [&](double first, double step) {
     for (int i = 0; i < 5; ++i, first *= step) s.k[i] = (float)(first * kTanh[i]);
   };
   coefficients(most * inside, inside * inside);
-  s.on = s.k[4] > 1e-36f && s.k[4] < 1e30f && s.k[0] > 1e-36f && s.k[0] < 1e30f ? 1 : 2;
-  if (s.on == 2) coefficients(most, 1.0);
-  s.near = s.on == 1 ? (float)(kTanhNear / inside) : -1.0f;
+  const bool fits = s.k[4] > 1e-36f && s.k[4] < 1e30f && s.k[0] > 1e-36f && s.k[0] < 1e30f;
+  if (!fits) coefficients(most, 1.0);
+  s.near = fits ? (float)(kTanhNear / inside) : -1.0f;
   return s;
 }
 
@@ -142,12 +143,22 @@ struct ShapedAttentionArgs : CacheAttentionArgs {
   // the shared prefix: its keys (a multiple of kUnit; 0: none), passed over in pieces of prefix_units units; of every
   // piece and row of q {reference, sum, sum of the rounded values} and the accumulators
   int shared, prefix_pieces, prefix_units;
+  // beside direct ranges: row tiles that may be cut; the row tile and direct_units of the sequences' own pass
+  int crossings, own_tile, direct_units;
   float4* prefix_stat;  // [pieces][n * Hq]
   float* prefix_acc;    // [pieces][n * Hq][d]
+  int* arrived;         // of each of these the pieces that are there, then the units of all; or null (look_for_long)
 };
 // The same without a cap and slopes.
 struct MaskedAttentionArgs : ShapedAttentionArgs {
   static constexpr bool kScores = false;
+};
+// Either behind a shared prefix, with a plan that has direct ranges.
+struct ShapedBehindArgs : ShapedAttentionArgs {
+  static constexpr bool kDirect = true;
+};
+struct MaskedBehindArgs : MaskedAttentionArgs {
+  static constexpr bool kDirect = true;
 };
 // The pass over the shared prefix itself.
 struct PrefixAttentionArgs : ShapedAttentionArgs {
@@ -157,6 +168,8 @@ struct PrefixAttentionArgs : ShapedAttentionArgs {
 hipError_t launch_cache_attention(const CacheAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 hipError_t launch_shaped_attention(const ShapedAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 hipError_t launch_masked_attention(const MaskedAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
+hipError_t launch_shaped_behind(const ShapedBehindArgs& a, const CachePlan& plan, hipStream_t stream);
+hipError_t launch_masked_behind(const MaskedBehindArgs& a, const CachePlan& plan, hipStream_t stream);
 hipError_t launch_prefix_attention(const PrefixAttentionArgs& a, const CachePlan& plan, hipStream_t stream);
 
 }  // namespace fp4attn

@@ -19,6 +19,7 @@ import torch
 
 from oracle import serving
 from test_gpu_serving import FORMATS, HALF_STEP, U, Batch, _beside_idle, _f64, _tree
+from test_shaped import INSIDE
 
 pytestmark = pytest.mark.gpu
 
@@ -601,3 +602,81 @@ def test_caps_below_their_range_are_refused(fa, softcap):
     b = Batch([300], [2], 2, 2, 64, False, 16, seed=1)
     with pytest.raises((ValueError, fa.Fp4AttnError), match="2\\^-64"):
         b.call(fa, softcap=softcap)
+
+
+# ---------------------------------------------------------------- members that end inside a shared prefix
+
+def _inside(case, d, fp8):
+    _, _, new, keys, B, H, G, shared = case
+    b = _share(Batch(keys, new, H, G, d, fp8, 16, seed=d + len(new)), shared)
+    return _beside_idle(b, (B - len(new)) * H, 1), shared
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("case,d", [(case, d) for case in INSIDE for d in case[1]])
+def test_members_inside_a_long_prefix(fa, case, d, fp8):
+    """Their keys are cut up beside the other sequences' row tiles (test_shaped.py has these plans), and the pieces joined in one order."""
+    b, shared = _inside(case, d, fp8)
+    out, lse = _run(fa, b, shared=shared)
+    for _ in range(3):
+        again, norm = _run(fa, b, shared=shared, check=False)
+        assert torch.equal(again, out) and torch.equal(norm, lse)
+    _run(fa, b, shared=shared, softcap=3.0, slopes=_slopes(b.H * b.G))
+    if max(b.new) > 1:
+        _run(fa, b, tree=_tree(b.new, 1, d), shared=shared, softcap=8.0)
+        _run(fa, b, tree=_tree(b.new, 2, d), shared=shared)
+    _run(fa, b, shared=shared, prefix=[n - t // 2 for t, n in zip(b.new, b.keys)], slopes=_slopes(b.H * b.G))
+    _run(fa, b, shared=shared, prefix=[n // 2 for n in b.keys])
+
+
+@pytest.mark.parametrize("d,fp8", [(64, True), (128, False)])
+def test_no_member_behind_the_prefix(fa, d, fp8):
+    """All of them are cut up, of a table as long as the prefix; values that are no numbers reach the rows that see them."""
+    case = next(c for c in INSIDE if c[0] == 16)
+    b, shared = _inside(case, d, fp8)
+    b.keys = [min(n, shared - 1) for n in b.keys]
+    b.slots = [s[:n] for s, n in zip(b.slots, b.keys)]
+    clean, _ = _run(fa, b, shared=shared)
+    p, off = divmod(int(b.slots[3][777]), 16)    # (a key of the third sequence and of all behind as long)
+    b.cache[3][p, 0, off // 8, 1, off % 8] = 255
+    out, _ = _run(fa, b, shared=shared, check=False)
+    bad = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    bad[[i for i, n in enumerate(b.keys) if n > 777 and b.slots[i][777] == b.slots[3][777]], 0, 32:64] = True
+    assert bool(bad.any()) and torch.equal(torch.isnan(out), bad) and torch.equal(out[~bad], clean[~bad])
+
+
+def test_members_inside_on_two_streams_and_in_graphs(fa):
+    """Calls at once, each with counts of its own, and captured ones whose lengths change from replay to replay."""
+    case = next(c for c in INSIDE if c[0] == 16)
+    calls, want = [], []
+    for d, fp8 in ((64, True), (128, False)):
+        b, shared = _inside(case, d, fp8)
+        lengths = torch.tensor(b.keys, dtype=torch.int32, device="cuda")
+        a = (b.q.cuda(), fa.KVCache(*(torch.from_numpy(t).cuda() for t in b.cache)), torch.from_numpy(b.table).cuda(), lengths)
+        calls.append(a)
+        want.append([fa.cache_attention(*a[:3], n, shared=shared) for n in (lengths, (lengths - 300).clamp(min=0))])
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in calls], [[], []]
+    for _ in range(20):
+        for a, stream, out in zip(calls, streams, outs):
+            with torch.cuda.stream(stream):
+                out.append(fa.cache_attention(*a, shared=shared))
+    torch.cuda.synchronize()
+    for out, w in zip(outs, want):
+        assert all(torch.equal(x, w[0]) for x in out)
+    side, graphs = torch.cuda.Stream(), []
+    side.wait_stream(torch.cuda.current_stream())
+    for a in calls:
+        graph, out = torch.cuda.CUDAGraph(), torch.empty_like(a[0], dtype=torch.float32)
+        with torch.cuda.graph(graph, stream=side):
+            fa.cache_attention(*a, out=out, shared=shared)
+        graphs.append((graph, out))
+    for i in range(6):
+        for a in calls:
+            a[3].copy_((torch.tensor(case[3], dtype=torch.int32) - 300 * (i % 2)).clamp(min=0))
+        for graph, _ in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (_, out), w in zip(graphs, want):
+            assert torch.equal(out, w[i % 2]), i
+        fa.cache_attention(*calls[0], shared=shared).sum().item()

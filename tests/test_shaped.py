@@ -141,3 +141,83 @@ def test_python_refusals_without_a_gpu(fa):
         fa.cache_attention(x, fa.kv_cache(2, 4, 16, 64, device="cpu"), at.view(2, 1), at, softcap=3.0)
     with pytest.raises(ValueError, match="no gradient"):
         fa.cache_attention(x, None, at, at, slopes=torch.ones(4, requires_grad=True))
+
+
+# Batches behind a shared prefix with members that end inside it: row tile of the sequences' own pass, head dimensions, new
+# tokens, keys, sequences with idle ones, key heads, query heads to each, shared keys (in pages of 16).
+INSIDE = [(16, (64, 128), [1] * 16, [2660, 2650, 2400, 1500, 2561, 2600, 0, 200, 2559, 2560, 2570, 5, 2590, 2580, 2660, 2401], 16, 4, 1, 2560),
+          (16, (64, 128), [1] * 9, [2690, 2400, 2600, 2560, 3, 2561, 1200, 2650, 2559], 9, 32, 5, 2560),
+          (32, (64,), [33, 20, 1, 33, 0, 12, 5], [2660, 2600, 2590, 2500, 0, 1700, 40], 7, 8, 1, 2560),
+          (32, (128,), [17, 17, 15, 17, 17, 17, 3, 17, 17, 16], [4180, 4150, 4000, 2050, 4120, 4100, 4099, 4130, 900, 4111], 10, 4, 2, 4096),
+          (128, (128,), [33, 30, 33, 9], [2640, 2600, 2500, 2570], 132, 2, 4, 2560),
+          (128, (64,), [20, 17, 20, 13], [2640, 2600, 2500, 1000], 88, 8, 5, 2560)]
+
+
+def _compiled(tmp_path_factory, source):
+    exe = tmp_path_factory.mktemp("plan") / "plan"
+    res = subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Wextra", "-Werror", os.path.join(ROOT, "tests", source), "-o", str(exe)],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+
+    def ask(calls):
+        run = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True, text=True, timeout=60)
+        assert run.returncode == 0
+        return [tuple(map(int, line.split())) for line in run.stdout.splitlines()]
+    return ask
+
+
+@pytest.fixture(scope="module")
+def shared_plans(tmp_path_factory):
+    return _compiled(tmp_path_factory, "shared_call_plan.cpp")
+
+
+@needs_compiler
+def test_a_member_inside_a_shared_prefix_is_cut_up(fa, plans):
+    """Where a call without the hint cuts sequences up, one with it has room for their pieces beside those of the prefix."""
+    c = ctypes.byref(_cache(fa, heads=8, head_dim=128, page_size=64))
+    size = fa.lib.fp4attn_cache_attention_ex_workspace
+    for B in (8, 16, 24, 48, 96):
+        for shared in (16384, 65536):
+            for own in (64, 512, 1024):
+                pages = (shared + own) // 64
+                (_, _, pieces, _, _, _, rows, _), = plans([f"P 8 4 128 {B} {shared}"])
+                assert size(c, B, 32, B, pages, 1, None) > 0
+                assert size(c, B, 32, B, pages, 1, _options(fa, shared=shared)) > pieces * rows * (128 * 4 + 16), (B, shared, own)
+
+
+@needs_compiler
+def test_shared_call_plans(fa, shared_plans):
+    """The own pass: direct ranges for every row tile, others in number and workspace as the kernels take them."""
+    rng = np.random.default_rng(5)
+    calls = []
+    for _ in range(3000):
+        B, T, own, shared = (int(np.exp(rng.uniform(0, np.log(m)))) for m in (300, 100, 2500, 100000))
+        calls.append((B, int(rng.integers(1, 300)), int(rng.integers(1, 17)), int(rng.choice((64, 128))), int(rng.integers(0, 2)), T,
+                      int(rng.integers(1, B * T + 1)), shared + own, shared))
+    direct_calls = 0
+    for call, (keys, _, pieces, rows, tile, row_tiles, split, ranges, least, fits, direct, units, workgroups, work) in zip(
+            calls, shared_plans(calls)):
+        B, H, G, d, _, T, n, most, shared = call
+        assert keys in (0, shared // 128 * 128) and fits
+        assert (row_tiles - 1) * tile < T * G <= row_tiles * tile
+        if not direct:
+            assert workgroups == -(-ranges * H // 8) * 8 and (split or ranges == B * row_tiles)
+            continue
+        direct_calls += 1
+        others = ranges - direct
+        assert keys and not split and direct == B * row_tiles and others >= 2 and units == -(-(most - keys) // 128)
+        assert workgroups == -(-direct * H // 8) * 8 + -(-others * H // 8) * 8
+        assert work == others * 16 + others * 2 * H * min(tile, T * G) * (d * 4 + 16)
+        # a sequence that may end inside the prefix is walked in pieces
+        assert least >= 4 and (least - 1) ** 2 * 1.6 < max(-(-most // 128), 16)
+    assert direct_calls > 500
+
+
+@needs_compiler
+def test_plans_of_the_batches_with_members_inside(shared_plans):
+    for tile, dims, new, keys, B, H, G, shared in INSIDE:
+        for d in dims:
+            for fp8 in (0, 1):
+                most = (-(-max(keys) // 16) + 2) * 16
+                (got, _, _, _, own_tile, _, _, _, _, _, direct, _, _, _), = shared_plans([(B, H, G, d, fp8, max(new), sum(new), most, shared)])
+                assert (got, own_tile) == (shared, tile) and direct > 0, (tile, d, fp8)
