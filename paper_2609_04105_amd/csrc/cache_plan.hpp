@@ -89,7 +89,8 @@ inline CachePlan cache_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8
 
 // Microseconds of walking `keys` keys for `tiles` row tiles, all key heads counted, in a chip that they fill, with the
 // launch and its start: from the times of 400 batches of 2 to 200 sequences, 1 to 16 tokens, 1 to 8 query heads a key head,
-// behind 1024 to 65536 keys (8 heads of d = 128 in MXFP4, 2 of d = 64 in MXFP8), by least squares; the worst are off by a quarter.
+// behind 1024 to 65536 keys (8 heads of d = 128 in MXFP4, 2 of d = 64 in MXFP8), by least squares.  A rough model: d = 128 in MXFP8
+// and d = 64 in MXFP4 were not in it, and it knows nothing of a last round that leaves workgroups idle.
 inline double walk_time(int tile, int64_t d, int64_t tiles, int64_t keys, bool prefix) {
   const double walks = (double)tiles * (double)keys * 1e-6;
   if (tile == 16) return prefix ? 14 + 30 * walks : 12 + 15 * walks;  // (a pass over a prefix has one tile a key head)
@@ -138,14 +139,16 @@ inline PrefixPlan prefix_plan(int64_t H, int64_t G, int64_t d, int64_t n, int64_
 // Whether n tokens of B sequences, which a call with `plan` serves one by one, gain by a pass over their shared prefix.  us without it /
 // with it, 8 key heads of 4 query heads, d = 128, MXFP4, one token each: 2 sequences behind 65536 keys 29 / 29; 4 31 / 29 of
 // 32768; 16 behind 1024 keys 12.9 / 16.9, 4096 keys 21.9 / 18.2; 48 behind 4096 keys 39 / 23, 65536 keys 363 / 94; 16 tokens each: 8
-// behind 65536 keys 190 / 177, 48 behind 16384 keys 281 / 314.  (Of the 400 batches the choice costs 1 % on average, 27 % at most.)
+// behind 65536 keys 190 / 177, 48 behind 16384 keys 281 / 314.  The model has to promise a tenth: of 320 other random batches (2 to 128
+// sequences, 2 or 8 key heads, both head dimensions and formats, 1 to 16 tokens) that it says gain anything the pass made 52 more than 3 % longer,
+// of those that it says gain a tenth 14, 1.43 times at most; on average the calls take 0.622 and 0.618 of what they take one by one.
 inline bool shares_prefix(const CachePlan& plan, const PrefixPlan& prefix, int64_t B, int64_t H, int64_t G, int64_t d, int64_t n,
                           int64_t keys) {
   int64_t tiles = n * G / plan.tile + B;  // at most, of ragged sequences
   if (tiles > B * plan.row_tiles) tiles = B * plan.row_tiles;
   // (where row tiles of 128 rows serve the sequences one by one, their own keys lose by the smaller tiles that fewer keys get: trees of
   // 32 tokens, 24 sequences of up to 2048 keys behind 4096, 94 us without the pass, 112 with it)
-  const double gain = plan.tile == kRowsTile ? 0.8 : 1.0;
+  const double gain = 0.9 * (plan.tile == kRowsTile ? 0.8 : 1.0);
   return prefix.fits && walk_time(prefix.plan.tile, d, prefix.plan.row_tiles * H, keys, true) <
                             gain * walk_time(plan.tile, d, tiles * H, keys, false);
 }

@@ -145,10 +145,10 @@ def test_python_refusals_without_a_gpu(fa):
 
 # Batches behind a shared prefix with members that end inside it: row tile of the sequences' own pass, head dimensions, new
 # tokens, keys, sequences with idle ones, key heads, query heads to each, shared keys (in pages of 16).
-INSIDE = [(16, (64, 128), [1] * 16, [2660, 2650, 2400, 1500, 2561, 2600, 0, 200, 2559, 2560, 2570, 5, 2590, 2580, 2660, 2401], 16, 4, 1, 2560),
-          (16, (64, 128), [1] * 9, [2690, 2400, 2600, 2560, 3, 2561, 1200, 2650, 2559], 9, 32, 5, 2560),
-          (32, (64,), [33, 20, 1, 33, 0, 12, 5], [2660, 2600, 2590, 2500, 0, 1700, 40], 7, 8, 1, 2560),
-          (32, (128,), [17, 17, 15, 17, 17, 17, 3, 17, 17, 16], [4180, 4150, 4000, 2050, 4120, 4100, 4099, 4130, 900, 4111], 10, 4, 2, 4096),
+INSIDE = [(16, (64, 128), [1] * 16, [2660, 2650, 2400, 1500, 2561, 2600, 0, 200, 2559, 2560, 2570, 5, 2590, 2580, 2660, 2401], 16, 8, 1, 2560),
+          (16, (64, 128), [1] * 9, [2690, 2400, 2600, 2560, 3, 2561, 1200, 2650, 2559], 18, 32, 5, 2560),
+          (32, (64,), [33, 20, 1, 33, 0, 12, 5], [2660, 2600, 2590, 2500, 0, 1700, 40], 7, 16, 1, 2560),
+          (32, (128,), [17, 17, 15, 17, 17, 17, 3, 17, 17, 16], [4180, 4150, 4000, 2050, 4120, 4100, 4099, 4130, 900, 4111], 10, 8, 2, 4096),
           (128, (128,), [33, 30, 33, 9], [2640, 2600, 2500, 2570], 132, 2, 4, 2560),
           (128, (64,), [20, 17, 20, 13], [2640, 2600, 2500, 1000], 88, 8, 5, 2560)]
 
@@ -221,3 +221,13 @@ def test_plans_of_the_batches_with_members_inside(shared_plans):
                 most = (-(-max(keys) // 16) + 2) * 16
                 (got, _, _, _, own_tile, _, _, _, _, _, direct, _, _, _), = shared_plans([(B, H, G, d, fp8, max(new), sum(new), most, shared)])
                 assert (got, own_tile) == (shared, tile) and direct > 0, (tile, d, fp8)
+
+
+@needs_compiler
+def test_a_pass_that_promises_little_is_not_taken(shared_plans):
+    """Batches that a pass over their prefix of its own made longer (measured, us with it / without), and ones that it makes shorter."""
+    longer = [(7, 2, 2, 128, 0, 1, 7, 16576, 14495), (4, 8, 2, 64, 1, 1, 4, 11840, 10615), (80, 8, 4, 64, 0, 1, 80, 1024, 913),   # 23/14, 21/15, 19/14
+              (35, 8, 8, 128, 1, 8, 207, 2368, 1503), (72, 8, 8, 128, 0, 8, 436, 2432, 1700)]                                     # 61/46, 85/67
+    shorter = [(64, 8, 4, 128, 0, 1, 64, 9216, 8192), (96, 8, 8, 128, 1, 1, 96, 66048, 65536), (48, 8, 4, 128, 0, 1, 48, 4608, 4096),
+               (24, 8, 8, 128, 0, 1, 24, 16896, 16384), (9, 8, 1, 128, 0, 2, 18, 60928, 60843)]                                   # 33/75, 280/1156, 24/36 ..
+    assert all(s[0] == 0 for s in shared_plans(longer)) and all(s[0] > 0 for s in shared_plans(shorter))
