@@ -325,9 +325,7 @@ fp4attn_status plan_cache_attention(const fp4attn::CacheView& c, int64_t n, int6
   if (!p->shaped && p->shared == 0) return FP4ATTN_OK;
   p->shaped = true;
   if (p->shared == 0) p->plan = fp4attn::cache_plan(B, c.H, G, c.d, c.fp8 != 0, max_q, span);
-  // (a row tile smaller than the unshaped plan's, a sequence that does not join the shared prefix)
-  const int64_t places = B * p->plan.row_tiles * ((max_keys + fp4attn::kUnit - 1) / fp4attn::kUnit + fp4attn::kSetup);
-  if (!p->plan.fits || places + p->plan.ranges >= int64_t(1) << 31)
+  if (!p->plan.fits)
     return fail(FP4ATTN_ERR_UNSUPPORTED, "B=%lld max_q=%lld max_pages=%lld: too many workgroups for one launch", (long long)B,
                 (long long)max_q, (long long)max_pages);
   p->workspace = p->plan.workspace;

@@ -193,6 +193,9 @@ inline SharedPlan shared_plan(const CachePlan& plan, int64_t B, int64_t H, int64
   if (!shares_prefix(plan, p.prefix, B, H, G, d, n, keys)) return p;
   p.shared = keys;
   p.plan = own_plan(B, H, G, d, fp8, max_q, max_keys > keys ? max_keys - keys : 1, max_keys);
+  // (smaller row tiles than the call's without the pass, and sequences that do not join the prefix)
+  const int64_t places = B * p.plan.row_tiles * ((max_keys + kUnit - 1) / kUnit + kSetup);
+  if (!p.plan.fits || places + p.plan.ranges >= int64_t(1) << 31) return SharedPlan{plan, {}, 0};
   return p;
 }
 

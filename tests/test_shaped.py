@@ -231,3 +231,16 @@ def test_a_pass_that_promises_little_is_not_taken(shared_plans):
     shorter = [(64, 8, 4, 128, 0, 1, 64, 9216, 8192), (96, 8, 8, 128, 1, 1, 96, 66048, 65536), (48, 8, 4, 128, 0, 1, 48, 4608, 4096),
                (24, 8, 8, 128, 0, 1, 24, 16896, 16384), (9, 8, 1, 128, 0, 2, 18, 60928, 60843)]                                   # 33/75, 280/1156, 24/36 ..
     assert all(s[0] == 0 for s in shared_plans(longer)) and all(s[0] > 0 for s in shared_plans(shorter))
+
+
+def test_options_refuse_no_size_that_goes_without_them(fa):
+    """A hint and a window choose smaller row tiles for the fewer keys that are left; where tables are huge, more of these than fit."""
+    size = fa.lib.fp4attn_cache_attention_ex_workspace
+    for B, H, G, T, n, page, pages, shared in ((64, 1, 2, 187, 6797, 128, 1 << 23, (1 << 30) - 639), (50, 1, 2, 326, 3416, 1 << 20, 256, 268432716),
+                                               (50, 2, 8, 28, 244, 2048, 1 << 19, (1 << 30) - 586)):
+        c = ctypes.byref(_cache(fa, heads=H, head_dim=128, page_size=page))
+        plain = size(c, n, H * G, B, pages, T, None)
+        assert plain >= 0
+        assert size(c, n, H * G, B, pages, T, _options(fa, shared=shared)) == plain
+        for window in (1, 300, 1 << 20):
+            assert size(c, n, H * G, B, pages, T, _options(fa, window=window)) >= 0, window
