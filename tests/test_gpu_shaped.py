@@ -19,7 +19,7 @@ import torch
 
 from oracle import serving
 from test_gpu_serving import FORMATS, HALF_STEP, U, Batch, _beside_idle, _f64, _tree
-from test_shaped import INSIDE
+from test_shaped import INSIDE, WIDE
 
 pytestmark = pytest.mark.gpu
 
@@ -680,3 +680,16 @@ def test_members_inside_on_two_streams_and_in_graphs(fa):
         for (_, out), w in zip(graphs, want):
             assert torch.equal(out, w[i % 2]), i
         fa.cache_attention(*calls[0], shared=shared).sum().item()
+
+
+@pytest.mark.parametrize("d,fp8", FORMATS)
+@pytest.mark.parametrize("new,keys,B,H,G,shared,cut", WIDE)
+def test_wide_row_tiles_behind_a_prefix(fa, new, keys, B, H, G, shared, cut, d, fp8):
+    """Row tiles of 128 rows that begin with the pieces of the prefix (test_shaped.py has these plans): ragged new tokens, the last row
+    tile of a sequence half in use, a member that does not join."""
+    b = _beside_idle(_share(Batch(keys, new, H, G, d, fp8, 16, seed=d), shared), (B - len(new)) * H, 1)
+    _run(fa, b, shared=shared)
+    _run(fa, b, shared=shared, slopes=_slopes(H * G), softcap=3.0)
+    _run(fa, b, shared=shared, prefix=[n - t // 2 for t, n in zip(b.new, b.keys)], slopes=_slopes(H * G))
+    _run(fa, b, shared=shared, tree=_tree(b.new, 1, d), softcap=8.0)
+    _run(fa, b, shared=shared, tree=_tree(b.new, 2, d))

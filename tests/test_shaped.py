@@ -244,3 +244,18 @@ def test_options_refuse_no_size_that_goes_without_them(fa):
         assert size(c, n, H * G, B, pages, T, _options(fa, shared=shared)) == plain
         for window in (1, 300, 1 << 20):
             assert size(c, n, H * G, B, pages, T, _options(fa, window=window)) >= 0, window
+
+
+# Batches whose own pass takes row tiles of 128 rows behind a pass over their prefix, whole and cut into ranges: new tokens, keys, sequences
+# with idle ones, key heads, query heads to each, shared keys, cut (in pages of 16).
+WIDE = [([40, 33, 40, 17], [556, 500, 300, 200], 208, 1, 8, 256, False), ([40, 33, 40, 17], [3200, 2600, 1064, 900], 208, 1, 8, 1024, True)]
+
+
+@needs_compiler
+def test_plans_of_wide_row_tiles_behind_a_prefix(shared_plans):
+    for new, keys, B, H, G, shared, cut in WIDE:
+        for d in (64, 128):
+            for fp8 in (0, 1):
+                most = (-(-max(keys) // 16) + 2) * 16
+                (got, _, _, _, tile, tiles, split, _, _, _, direct, _, _, _), = shared_plans([(B, H, G, d, fp8, max(new), sum(new), most, shared)])
+                assert (got, tile, tiles, split, direct) == (shared, 128, 3, int(cut), 0), (d, fp8, cut)
