@@ -424,8 +424,8 @@ int64_t fp4attn_cache_attention_workspace(const fp4attn_cache* cache, int64_t q_
  *   prefix   [B] int32 or NULL: the first prefix[b] keys are seen by every new token of sequence b
  *   shared   the first `shared` keys (and their values) of every sequence are the same, whose pages need not be.  A hint: the
  *            result is that of shared = 0 but for the order of sums.  Keys that all rows read once are taken from
- *            the pages of one sequence whose new tokens come after them; sequences with fewer keys are
- *            served by themselves.
+ *            the pages of one sequence whose new tokens come after them; sequences with fewer keys (which need not be the
+ *            same) are served by themselves, and where they are half of the batch the call gains nothing.
  *
  * Initialise with fp4attn_cache_attention_options_init (no option set); struct_size must equal
  * sizeof(fp4attn_cache_attention_options).

@@ -655,7 +655,8 @@ def cache_attention(q, cache, page_table, lengths, q_starts=None, max_q=None, tr
     (int32 [B]) shows the first keys of a sequence to all of its new tokens.  A tree goes with ``softcap`` only.
 
     ``shared``: the first ``shared`` keys of every sequence are the same (a system prompt, in the same pages or in
-    copies).  They are then read once for the batch where that is faster; the result is the same but for the order of sums."""
+    copies).  They are then read once for the batch where that is faster; the result is the same but for the order of sums.
+    Sequences that end inside them are served by themselves."""
     if slopes is not None and getattr(slopes, "requires_grad", False) and torch.is_grad_enabled():
         raise ValueError("slopes get no gradient here: detach them, or call under torch.no_grad()")
     r = _binding.cache_attention(q, cache, page_table, lengths, q_starts, max_q, tree, softmax_scale, out, lse, out_dtype,

@@ -24,7 +24,7 @@ struct CachePlan {
 };
 constexpr int kUnit = 128;  // keys that ranges are counted in
 constexpr int kSetup = 4;   // places of the line that starting a row tile takes (cache_attention.hpp)
-constexpr int kRowsTile = 128, kRowsPerCu = 2;  // cache_attention_rows.hip: rows of a workgroup, workgroups of a CU
+constexpr int kRowsTile = 128, kRowsPerCu = 2;  // cache_attention_rows.hpp: rows of a workgroup, workgroups of a CU
 
 constexpr int64_t kMaxCacheKeys = int64_t(1) << 30;  // keys of one sequence
 
