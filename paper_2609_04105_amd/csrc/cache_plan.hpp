@@ -132,7 +132,7 @@ inline PrefixPlan prefix_plan(int64_t H, int64_t G, int64_t d, int64_t n, int64_
   c.ranges = (int)(row_tiles * p.pieces);
   c.workgroups = (row_tiles * p.pieces * H + 7) / 8 * 8 + 8;  // the last eight without a range (place_of, look_for_long)
   p.rows = rows * H;
-  p.fits = c.workgroups <= 1 << 24;
+  p.fits = c.workgroups < 1 << 24;
   return p;
 }
 
@@ -173,7 +173,7 @@ inline CachePlan own_plan(int64_t B, int64_t H, int64_t G, int64_t d, bool fp8, 
   p.direct_units = (int)((own + kUnit - 1) / kUnit);
   p.ranges += (int)others;
   p.workgroups += (others * H + 7) / 8 * 8;
-  p.fits = p.fits && p.workgroups <= 1 << 24;
+  p.fits = p.fits && p.workgroups < 1 << 24;
   p.workspace = others * 16 + others * 2 * H * p.tile_rows * (d * 4 + 16);
   return p;
 }

@@ -259,3 +259,13 @@ def test_plans_of_wide_row_tiles_behind_a_prefix(shared_plans):
                 most = (-(-max(keys) // 16) + 2) * 16
                 (got, _, _, _, tile, tiles, split, _, _, _, direct, _, _, _), = shared_plans([(B, H, G, d, fp8, max(new), sum(new), most, shared)])
                 assert (got, tile, tiles, split, direct) == (shared, 128, 3, int(cut), 0), (d, fp8, cut)
+
+
+@needs_compiler
+def test_a_launch_has_fewer_than_2_to_32_threads(plans, shared_plans):
+    """256 to a workgroup; plans at the edge."""
+    calls = [(H, 1, 64, (1 << 24) // H * 128 - off, 128) for H in (1, 8, 64, 4096) for off in (0, 1, 127, 128, 300, 128 * 8, 128 * 9)]
+    sizes = plans(["P %d %d %d %d %d" % c for c in calls])
+    assert all(workgroups < 1 << 24 for *_, workgroups, _, fits in sizes if fits) and any(not s[-1] for s in sizes)
+    calls = [(65535, H, 1, 64, 0, 1, 65535, 4096, 4000) for H in (128, 255, 256)]
+    assert all(p[12] < 1 << 24 for p in shared_plans(calls) if p[0])
