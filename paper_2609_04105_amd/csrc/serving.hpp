@@ -77,9 +77,9 @@ struct CacheAssignArgs {
 
 // Steps of up to so many sequences and tokens are served by one workgroup, without a workspace.  In one launch / in two, us in a graph:
 // 64 sequences, one token each 4.3 / 6.6; 1000 sequences 8.3 / 12.7; 2000 tokens of 256 sequences 7.1 / 8.9.  20 thousand tokens of
-// prompts take 8.1 in two.  A step that moves many pages (which the host does not know) is the worse for it, us a call of 64 sequences that return
-// 4 thousand pages 5.8 / 8.4, 16 thousand 9.4 / 8.5, 64 thousand 28 / 8.5, 300 thousand 119 / 8.5, a million 401 / 8.9: pages of 16 keys of requests with
-// a million keys in all end in one step for the third.  A rule on the pages that may move would charge every step with a wide table 2.3 us.
+// prompts take 8.1 in two.  A step that moves many pages is the worse for it, us a call of 64 sequences that return 4 thousand pages 5.8 / 8.4,
+// 16 thousand 9.4 / 8.5, 64 thousand (of 16 keys, a million keys) 28 / 8.5, 300 thousand 119 / 8.5.  How many move only the device knows; a rule on
+// those that may would charge every step with a wide table 2.3 us.
 constexpr int kAssignOne = 1024, kAssignOneTokens = 4096;
 constexpr bool assign_in_one(int64_t B, int64_t tokens) { return B <= kAssignOne && tokens <= kAssignOneTokens; }
 constexpr int64_t cache_assign_workspace(int64_t B, int64_t tokens) { return assign_in_one(B, tokens) ? 0 : 16 + 16 * B; }
